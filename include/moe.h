@@ -384,6 +384,109 @@ int moe_placement_anticorrelation(const float *A, int32_t E, int32_t B, int32_t 
 int moe_placement_loads(const float *A, int32_t E, int32_t B, const int32_t *device_of, int32_t n_devices,
                         double *max_load, double *avg_max_load);
 
+/* ---- A decoder layer's other half: attention over a paged 8-bit cache, and the next token (not in the ----
+ * ---- paper, whose subject is the layer above; what a program that decodes with it needs beside it)   ---- */
+
+/* The cache of one layer.  A page holds page_size tokens of one sequence; every (page, key head) has a scale of its
+ * own for its keys and one for its values:
+ *   k, v               [num_pages, n_kv_heads, page_size, head_dim] OCP e4m3 bytes
+ *   k_scale, v_scale   [num_pages, n_kv_heads] fp32, powers of two;  key = k_scale * k, value = v_scale * v
+ * Nothing in it has to be initialised: pages hold what moe_kv_append has written, and rows that it has not written
+ * are not used.  A page's rows lie in order, so pages may be copied or shared as bytes with their scales. */
+typedef struct moe_kv_cache {
+    void *k;
+    void *v;
+    float *k_scale;
+    float *v_scale;
+} moe_kv_cache_t;
+
+/* Supported: dtype in {F32, BF16} (queries, new keys and values, outputs); head_dim 64, 128 or 256; n_heads a multiple
+ * of n_kv_heads (query head h reads key head h / (n_heads / n_kv_heads)), at most MOE_ATTN_MAX_HEADS; page_size a
+ * power of two, 16 .. 128; 1 <= B_max <= MOE_ATTN_MAX_B sequences; 0 <= T_max < 2^24 new tokens a call; num_pages >= 1
+ * pages in the cache; 1 <= max_pages pages of a sequence with max_pages * page_size < 2^30; rot_dim rotated dimensions
+ * of a head: 0 or a multiple of 16 up to head_dim. */
+#define MOE_ATTN_MAX_HEADS 256
+#define MOE_ATTN_MAX_B 4096
+typedef struct moe_attn_config {
+    int32_t B_max;
+    int32_t T_max;
+    int32_t n_heads;
+    int32_t n_kv_heads;
+    int32_t head_dim;
+    int32_t page_size;
+    int32_t num_pages;
+    int32_t max_pages;
+    int32_t dtype;
+    int32_t rot_dim;
+    int32_t rot_interleaved; /* 0: dimension j turns with j + rot_dim/2; 1: dimension 2j with 2j + 1 */
+} moe_attn_config_t;
+typedef struct moe_attn_handle moe_attn_handle_t; /* opaque: the config plus device properties */
+
+/* As moe_create / moe_destroy / moe_workspace_bytes.  One handle and one workspace serve every layer of the same
+ * geometry.  Only moe_attn_forward takes the workspace. */
+int moe_attn_create(const moe_attn_config_t *cfg, moe_attn_handle_t **out);
+int moe_attn_destroy(moe_attn_handle_t *h);
+int64_t moe_attn_workspace_bytes(const moe_attn_handle_t *h);
+
+/* What the two calls below share.  A batch is B sequences; sequence b has the new tokens q_offsets[b] ..
+ * q_offsets[b + 1] - 1 of the T new tokens (q_offsets [B+1] ascending from 0 to T; none is fine), n_b of them, and
+ * kv_len[b] tokens in the cache, the new ones among them: new token i is at position kv_len[b] - n_b + i.
+ * page_table [B, max_pages]: position p is row p % page_size of page page_table[b][p / page_size]; entries past a
+ * sequence's length are not read.  All three int32 on the device.  max_q (and max_kv) are bounds of n_b (of kv_len)
+ * that the host knows; they size the launch, tokens past them are left out.  Lengths outside [0, max_pages * page_size]
+ * and offsets outside [0, T] are clamped into the range, and a position whose table entry is outside [0, num_pages)
+ * holds nothing: it is neither written nor attended to.
+ * q [T, n_heads, head_dim], k and v [T, n_kv_heads, head_dim] elem: a token's heads lie together; from one token to
+ * the next it is q_stride (k_stride, v_stride) elements, a multiple of 16 bytes, so q, k and v may be parts of one
+ * projection's output.  Outputs are dense. */
+
+/* Position rotation and append.  With a = position * inv_freq[j] (inv_freq [rot_dim / 2] fp64 on the device; NULL
+ * only with rot_dim = 0), dimensions (x1, x2) of a pair of every query and key become
+ *   (x1 cos a - x2 sin a, x2 cos a + x1 sin a);
+ * dimensions past rot_dim stay.  The angles and the rotation are computed in 64 bits.  Queries are rounded to elem in
+ * q_out [T, n_heads, head_dim] (q and q_out NULL: only keys and values).  Keys, rotated and rounded to fp32, and
+ * values go into the cache: with need = the smallest power of two, at least 2^-126, that is no less than the largest
+ * new element of the (page, head) over 448, its scale s becomes need where the first new row of the page is its row 0,
+ * and max(s, need) else; where it grows, rows below the first new one are rounded to e4m3 anew, q <- e4m3(q * s_old / s).
+ * New rows are e4m3(x / s), to nearest even.  A page may receive new tokens of one sequence only; rewriting positions
+ * (tokens that were rejected) is fine. */
+int moe_kv_append(moe_attn_handle_t *h, const moe_kv_cache_t *cache, const void *q, int64_t q_stride, const void *k,
+                  int64_t k_stride, const void *v, int64_t v_stride, const double *inv_freq, const int32_t *q_offsets,
+                  const int32_t *kv_len, const int32_t *page_table, int32_t B, int32_t T, int32_t max_q, void *q_out,
+                  void *stream);
+
+/* Attention of the new tokens' (rotated) queries over the cache, for decoding, prefill and cross attention alike, and
+ * for batches of all of them:
+ *   out[t, h] = sum_p softmax_p(scale * q[t, h] . key[p]) value[p]
+ * over the positions p < kv_len[b] with p <= pos(t) if causal, and pos(t) - p < window if window > 0.  Scores, softmax
+ * and sums in fp32 (bf16: the weights are rounded to bf16 for the product with the values).  lse [T, n_heads] fp32, NULL or
+ * the natural logarithm of the softmax's denominator, which lets outputs over parts of a sequence be joined.  A query
+ * that sees nothing gets zeros, and -infinity.  Cache bytes of rows that nothing was written to may hold anything.
+ * Needs the workspace. */
+int moe_attn_forward(moe_attn_handle_t *h, const moe_kv_cache_t *cache, const void *q, int64_t q_stride,
+                     const int32_t *q_offsets, const int32_t *kv_len, const int32_t *page_table, int32_t B, int32_t T,
+                     int32_t max_q, int32_t max_kv, float scale, int32_t causal, int32_t window, void *out, float *lse,
+                     void *workspace, int64_t workspace_bytes, void *stream);
+
+/* The next token of every row of logits [B, V] (dtype F32 or BF16, row_stride elements from row to row, aligned to its
+ * elements only) with the random numbers u [B] in [0, 1).  temperature, top_p, min_p [B] fp32 and top_k [B] int32 hold every
+ * row's settings; each may be NULL (1, 1, 0 and 0: off).  A row's tokens are ordered by descending logit, equal ones by
+ * ascending index; NaN counts as -infinity, and -infinity is never drawn.  With w = exp((logit - largest) / temperature):
+ *   top_k > 0    the first top_k of the order stay;
+ *   top_p < 1    of those, the shortest beginning whose w sum to at least top_p times the sum over all of those;
+ *   min_p > 0    of those, the ones with w >= min_p;  the first of the order always stays;
+ *   token        the first, in ascending index, at which the running sum of the remaining w exceeds u times their sum;
+ *   temperature <= 0: the first of the order.
+ * logprob [B] fp32 (may be NULL): the logarithm of the drawn token's share of the remaining w.  A row with nothing but
+ * -infinity gives token -1 and logprob -infinity; where the largest logit is +infinity, w is 1 for those and 0 else.
+ * w and all sums are held in 64 bits, and sums do not depend on the order in which they are formed.  1 <= V <= 2^19.
+ * Workspace: moe_sample_workspace_bytes(B, V). */
+#define MOE_SAMPLE_MAX_V (1 << 19)
+int64_t moe_sample_workspace_bytes(int32_t B, int32_t V);
+int moe_sample(const void *logits, int32_t dtype, int64_t row_stride, int32_t B, int32_t V, const float *u,
+               const float *temperature, const int32_t *top_k, const float *top_p, const float *min_p, int32_t *token,
+               float *logprob, void *workspace, int64_t workspace_bytes, void *stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -38,6 +38,8 @@ EXPORTS = [
     "moe_quantize_e4m3", "moe_expert_ffn_w8", "moe_layer_forward_w8",
     "moe_mxfp4_scale_bytes", "moe_quantize_mxfp4", "moe_expert_ffn_w4", "moe_layer_forward_w4",
     "moe_expert_cache_bytes_q", "moe_expert_cache_create_q", "moe_layer_forward_noalloc",
+    "moe_attn_create", "moe_attn_destroy", "moe_attn_workspace_bytes", "moe_kv_append", "moe_attn_forward",
+    "moe_sample", "moe_sample_workspace_bytes",
 ]
 MOE_NOALLOC_SCRATCH_BYTES = 8 * 1024 * 1024
 
@@ -51,6 +53,15 @@ class MoeRouting(ctypes.Structure):
     _fields_ = [("logits", ctypes.c_void_p), ("topk_idx", ctypes.c_void_p), ("topk_w", ctypes.c_void_p),
                 ("counts", ctypes.c_void_p), ("offsets", ctypes.c_void_p), ("dst_row", ctypes.c_void_p),
                 ("src_tok", ctypes.c_void_p)]
+
+
+class MoeKvCache(ctypes.Structure):
+    _fields_ = [("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("k_scale", ctypes.c_void_p), ("v_scale", ctypes.c_void_p)]
+
+
+class MoeAttnConfig(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("B_max", "T_max", "n_heads", "n_kv_heads", "head_dim", "page_size", "num_pages",
+                                              "max_pages", "dtype", "rot_dim", "rot_interleaved")]
 
 
 class MoeError(RuntimeError):
@@ -158,6 +169,21 @@ def load_library() -> ctypes.CDLL:
     lib.moe_expert_cache_bytes_q.restype = i64
     lib.moe_expert_cache_create_q.argtypes = [vp, i32, i32, vp, vp, vp, vp, vp, i64, ctypes.POINTER(vp)]
     lib.moe_expert_cache_create_q.restype = ctypes.c_int
+    lib.moe_attn_create.argtypes = [ctypes.POINTER(MoeAttnConfig), ctypes.POINTER(vp)]
+    lib.moe_attn_create.restype = ctypes.c_int
+    lib.moe_attn_destroy.argtypes = [vp]
+    lib.moe_attn_destroy.restype = ctypes.c_int
+    lib.moe_attn_workspace_bytes.argtypes = [vp]
+    lib.moe_attn_workspace_bytes.restype = i64
+    lib.moe_kv_append.argtypes = [vp, ctypes.POINTER(MoeKvCache), vp, i64, vp, i64, vp, i64, vp, vp, vp, vp, i32, i32, i32, vp, vp]
+    lib.moe_kv_append.restype = ctypes.c_int
+    lib.moe_attn_forward.argtypes = [vp, ctypes.POINTER(MoeKvCache), vp, i64, vp, vp, vp, i32, i32, i32, i32, ctypes.c_float, i32, i32,
+                                     vp, vp, vp, i64, vp]
+    lib.moe_attn_forward.restype = ctypes.c_int
+    lib.moe_sample_workspace_bytes.argtypes = [i32, i32]
+    lib.moe_sample_workspace_bytes.restype = i64
+    lib.moe_sample.argtypes = [vp, i32, i64, i32, i32, vp, vp, vp, vp, vp, vp, vp, vp, i64, vp]
+    lib.moe_sample.restype = ctypes.c_int
     _lib = lib
     return lib
 
@@ -512,3 +538,131 @@ def moe_placement_loads(A, device_of, n_devices: int):
     mx, av = ctypes.c_double(0), ctypes.c_double(0)
     _check(load_library().moe_placement_loads(flat, E, B, d, n_devices, ctypes.byref(mx), ctypes.byref(av)))
     return mx.value, av.value
+
+
+class KvCache:
+    """One layer's paged cache (moe_kv_cache_t): k and v [num_pages, n_kv_heads, page_size, head_dim] in torch.float8_e4m3fn (or
+    uint8), k_scale and v_scale [num_pages, n_kv_heads] fp32, on the device.  PagedAttention.new_cache allocates one."""
+
+    def __init__(self, k: torch.Tensor, v: torch.Tensor, k_scale: torch.Tensor, v_scale: torch.Tensor):
+        for name, t in (("k", k), ("v", v)):
+            if t.dim() != 4 or t.element_size() != 1:
+                raise ValueError("%s must be [num_pages, n_kv_heads, page_size, head_dim] of one byte each" % name)
+        if k.shape != v.shape or tuple(k_scale.shape) != tuple(k.shape[:2]) or tuple(v_scale.shape) != tuple(k.shape[:2]):
+            raise ValueError("k and v must have the same shape, the scales their first two dimensions")
+        if k_scale.dtype != torch.float32 or v_scale.dtype != torch.float32:
+            raise ValueError("scales must be float32")
+        self.k, self.v, self.k_scale, self.v_scale = k, v, k_scale, v_scale
+        self.struct = MoeKvCache(_ptr(k), _ptr(v), _ptr(k_scale), _ptr(v_scale))
+
+
+class PagedAttention:
+    """A handle (moe_attn_create) plus a workspace tensor, for every layer of one geometry.  Methods mirror the C entry
+    points; q, k and v may be views of one projection's output (a token's heads together, any stride from token to token)."""
+
+    def __init__(self, B_max: int, T_max: int, n_heads: int, n_kv_heads: int, head_dim: int, page_size: int, num_pages: int, max_pages: int,
+                 dtype: str = "bf16", rot_dim: int = 0, interleaved: bool = False, device: str = "cuda:0"):
+        self.lib = load_library()
+        self.cfg = MoeAttnConfig(B_max, T_max, n_heads, n_kv_heads, head_dim, page_size, num_pages, max_pages,
+                                 MOE_DTYPE_BF16 if dtype == "bf16" else MOE_DTYPE_F32, rot_dim, int(interleaved))
+        self.torch_dtype = torch.bfloat16 if dtype == "bf16" else torch.float32
+        self.device = torch.device(device)
+        h = ctypes.c_void_p()
+        with torch.cuda.device(self.device):
+            _check(self.lib.moe_attn_create(ctypes.byref(self.cfg), ctypes.byref(h)))
+        self.h = h
+        self.workspace = torch.empty(int(self.lib.moe_attn_workspace_bytes(h)), dtype=torch.uint8, device=self.device)
+
+    def __del__(self):
+        try:
+            if getattr(self, "h", None):
+                self.lib.moe_attn_destroy(self.h)
+                self.h = None
+        except Exception:
+            pass
+
+    def new_cache(self) -> KvCache:
+        c = self.cfg
+        shape = (c.num_pages, c.n_kv_heads, c.page_size, c.head_dim)
+        k, v = (torch.empty(shape, dtype=torch.uint8, device=self.device).view(torch.float8_e4m3fn) for _ in range(2))
+        ks, vs = (torch.empty(shape[:2], dtype=torch.float32, device=self.device) for _ in range(2))
+        return KvCache(k, v, ks, vs)
+
+    def _rows(self, t: Optional[torch.Tensor], heads: int, name: str):
+        """(pointer, elements from token to token) of [T, heads, head_dim]."""
+        if t is None:
+            return None, 0
+        if t.dim() != 3 or t.shape[1] != heads or t.shape[2] != self.cfg.head_dim or t.dtype != self.torch_dtype:
+            raise ValueError("%s must be [T, %d, %d] of %s" % (name, heads, self.cfg.head_dim, self.torch_dtype))
+        if t.shape[0] and (t.stride(2) != 1 or (heads > 1 and t.stride(1) != self.cfg.head_dim)):
+            raise ValueError("%s: the heads of a token must lie together" % name)
+        stride = t.stride(0) if t.shape[0] > 1 else heads * self.cfg.head_dim
+        return ctypes.c_void_p(t.data_ptr()), stride
+
+    def _batch(self, cache: KvCache, q_offsets, kv_len, page_table):
+        c = self.cfg
+        if tuple(cache.k.shape) != (c.num_pages, c.n_kv_heads, c.page_size, c.head_dim):
+            raise ValueError("the cache has shape %s, the handle another geometry" % (tuple(cache.k.shape),))
+        B = kv_len.shape[0]
+        if q_offsets.shape[0] != B + 1 or tuple(page_table.shape) != (B, c.max_pages):
+            raise ValueError("q_offsets must be [B + 1], kv_len [B] and page_table [B, max_pages]")
+        for t in (q_offsets, kv_len, page_table):
+            if t.dtype != torch.int32:
+                raise ValueError("q_offsets, kv_len and page_table must be int32")
+        return B
+
+    def moe_kv_append(self, cache: KvCache, q, k, v, inv_freq, q_offsets, kv_len, page_table, max_q: int, q_out=None):
+        """Rotates q (None: only keys and values) and k, and appends k and v to the cache; returns the rotated queries."""
+        B, T, c = self._batch(cache, q_offsets, kv_len, page_table), k.shape[0], self.cfg
+        if v.shape[0] != T or (q is not None and q.shape[0] != T):
+            raise ValueError("q, k and v must have the same number of tokens")
+        if inv_freq is not None and (inv_freq.dtype != torch.float64 or inv_freq.numel() != c.rot_dim // 2):
+            raise ValueError("inv_freq must be [rot_dim / 2] float64")
+        if q is not None and q_out is None:
+            q_out = torch.empty((T, c.n_heads, c.head_dim), dtype=self.torch_dtype, device=self.device)
+        (qp, qs), (kp, ks), (vp, vs) = self._rows(q, c.n_heads, "q"), self._rows(k, c.n_kv_heads, "k"), self._rows(v, c.n_kv_heads, "v")
+        _check(self.lib.moe_kv_append(self.h, ctypes.byref(cache.struct), qp, qs, kp, ks, vp, vs, _ptr(inv_freq), _ptr(q_offsets), _ptr(kv_len),
+                                      _ptr(page_table), B, T, max_q, _ptr(q_out), _stream()))
+        return q_out
+
+    def moe_attn_forward(self, cache: KvCache, q, q_offsets, kv_len, page_table, max_q: int, max_kv: int, scale: Optional[float] = None,
+                         causal: bool = True, window: int = 0, out=None, lse=None, want_lse: bool = True):
+        """-> (out [T, n_heads, head_dim], lse [T, n_heads] fp32 or None).  scale: 1 / sqrt(head_dim) where not given."""
+        B, T, c = self._batch(cache, q_offsets, kv_len, page_table), q.shape[0], self.cfg
+        if out is None:
+            out = torch.empty((T, c.n_heads, c.head_dim), dtype=self.torch_dtype, device=self.device)
+        if lse is None and want_lse:
+            lse = torch.empty((T, c.n_heads), dtype=torch.float32, device=self.device)
+        qp, qs = self._rows(q, c.n_heads, "q")
+        _check(self.lib.moe_attn_forward(self.h, ctypes.byref(cache.struct), qp, qs, _ptr(q_offsets), _ptr(kv_len), _ptr(page_table), B, T, max_q,
+                                         max_kv, c.head_dim ** -0.5 if scale is None else scale, int(causal), window, _ptr(out), _ptr(lse),
+                                         _ptr(self.workspace), self.workspace.numel(), _stream()))
+        return out, lse
+
+
+def moe_sample_workspace_bytes(B: int, V: int) -> int:
+    n = int(load_library().moe_sample_workspace_bytes(B, V))
+    if n < 0:
+        _check(n)
+    return n
+
+
+def moe_sample(logits, u, temperature=None, top_k=None, top_p=None, min_p=None, token=None, logprob=None, workspace=None):
+    """logits [B, V] (float32 or bfloat16, rows at any stride), u [B] in [0, 1), every row's settings or None
+    -> (token [B] int32, logprob [B] fp32)."""
+    lib = load_library()
+    if logits.dim() != 2 or logits.dtype not in (torch.float32, torch.bfloat16) or (logits.shape[1] > 1 and logits.stride(1) != 1):
+        raise ValueError("logits must be [B, V] of float32 or bfloat16 with dense rows")
+    B, V = logits.shape
+    for t, dtype in ((u, torch.float32), (temperature, torch.float32), (top_k, torch.int32), (top_p, torch.float32), (min_p, torch.float32)):
+        if t is not None and (t.dtype != dtype or t.numel() != B):
+            raise ValueError("u, temperature, top_p and min_p must be [B] float32, top_k [B] int32")
+    new = lambda dtype: torch.empty((B,), dtype=dtype, device=logits.device)  # noqa: E731
+    token = new(torch.int32) if token is None else token
+    logprob = new(torch.float32) if logprob is None else logprob
+    if workspace is None:
+        workspace = torch.empty(moe_sample_workspace_bytes(B, V), dtype=torch.uint8, device=logits.device)
+    _check(lib.moe_sample(ctypes.c_void_p(logits.data_ptr()), MOE_DTYPE_BF16 if logits.dtype == torch.bfloat16 else MOE_DTYPE_F32,
+                          logits.stride(0) if B > 1 else V, B, V, _ptr(u), _ptr(temperature), _ptr(top_k), _ptr(top_p), _ptr(min_p), _ptr(token),
+                          _ptr(logprob), _ptr(workspace), workspace.numel(), _stream()))
+    return token, logprob

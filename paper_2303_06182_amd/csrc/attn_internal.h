@@ -1,0 +1,61 @@
+// Internal declarations of the attention half of a decoder step (attn_api.hip, kv_append.hip, attn_decode.hip, attn_prefill.hip).
+#pragma once
+
+#include "moe_internal.h"
+
+struct moe_attn_handle {
+    moe_attn_config_t cfg;
+    int device;
+    int num_cus;
+};
+
+namespace moe355 {
+
+// Everything the kernels know of a call.  Pointers are device pointers; see include/moe.h for their meaning.
+struct AttnParams {
+    uint8_t *k, *v;
+    float *k_scale, *v_scale;
+    const int32_t *q_offsets, *kv_len, *page_table;
+    int B, T, n_heads, n_kv_heads, group;  // group: query heads of a key head
+    int page_shift, num_pages, max_pages;
+    int max_q, max_kv;                     // clamped to what the handle can hold
+    // attention
+    const void *q;
+    int64_t q_stride;
+    float scale_log2e;                     // scale * log2(e): scores are kept as powers of two
+    int causal, window;
+    void *out;
+    float *lse;
+    // partial results of units that several blocks share, and where the sequences begin in the tile space
+    float *part;
+    int64_t *seq_tiles;
+    int n_blocks;
+};
+
+// A sequence's new tokens and length, clamped to what can exist, so that no index derived from them leaves its array.
+struct Seq {
+    int first, n, kv;
+};
+__device__ __forceinline__ Seq load_seq(const AttnParams &p, int b)
+{
+    int lo = p.q_offsets[b], hi = p.q_offsets[b + 1], kv = p.kv_len[b];
+    lo = min(max(lo, 0), p.T);
+    hi = min(max(hi, lo), p.T);
+    kv = min(max(kv, 0), p.max_kv);
+    return {lo, min(hi - lo, p.max_q), kv};
+}
+
+struct AppendParams {
+    AttnParams a;
+    const void *k_new, *v_new;
+    int64_t k_stride, v_stride;
+    const double *inv_freq;
+    int rot_dim, interleaved;
+    void *q_out;
+};
+
+int launch_kv_append(int dtype, int head_dim, const AppendParams &p, int num_cus, hipStream_t s);
+int launch_attn_decode(int dtype, int head_dim, AttnParams p, int num_cus, hipStream_t s);
+int64_t attn_decode_workspace(int head_dim, int B_max, int num_cus);
+
+}  // namespace moe355

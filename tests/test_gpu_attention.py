@@ -1,0 +1,361 @@
+"""moe_kv_append and moe_attn_forward against the 64-bit oracle.
+
+Tolerances of the attention, per output element, from the roundings on the way (A = sum_p softmax_p |value_p|, K = scale * max_p
+sum_d |q_d key_pd|, half a step of bf16 2^-8 and of fp32 2^-24 relative to the value):
+    scores      dim products added in fp32, then two factors and a difference: |ds| <= (dim + 8) 2^-24 K, which moves a weight by as
+                much, numerator and denominator: 2 ds A
+    sums        of weights and of weighted values, at most kv terms each in fp32: 2 kv 2^-24 A; exp2 and rescaling: 16 * 2^-24 A
+    weights     bf16: rounded once, 2^-8 A.  fp32: as three bf16 numbers, 2^-24 A
+    output      rounded once: half a step |out|
+    range       a weight times its value's scale below the smallest normal fp32 number may be lost, 2^-126 * 448 for each key
+lse: ds + (kv + 16) 2^-24 + 4 * 2^-24 |lse|.  Appending: bytes and scales are equal; queries are off by one rounding of the value
+(bf16: after one to fp32) and 1e-11 of the pair's size for the angle.
+"""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+from oracle import decoder_step as od
+from paper_2303_06182_amd import binding
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda:0"
+
+
+def ints(v):
+    return torch.tensor(v, dtype=torch.int32, device=DEV)
+
+
+class Batch:
+    """Sequences with kv[b] cached tokens, n[b] of them new, pages in a shuffled order, every unwritten byte NaN."""
+
+    def __init__(self, n, kv, heads, kv_heads, dim, page, dtype="bf16", rot=0, interleaved=False, seed=0, spare=2):
+        self.n, self.kv, self.page, self.dtype = n, kv, page, dtype
+        rng = np.random.default_rng(seed)
+        held = [-(-v // page) for v in kv]
+        self.max_pages, self.pages = max(1, max(held)), max(1, sum(held)) + spare
+        order = list(rng.permutation(self.pages))
+        self.table = [[int(order.pop()) for _ in range(h)] + [-1] * (self.max_pages - h) for h in held]
+        self.offsets = [0] + list(np.cumsum(n).astype(int))
+        self.T = self.offsets[-1]
+        self.att = binding.PagedAttention(len(n), max(1, self.T), heads, kv_heads, dim, page, self.pages, self.max_pages, dtype, rot, interleaved)
+        self.td = torch.bfloat16 if dtype == "bf16" else torch.float32
+        self.inv_freq = 10000.0 ** (-np.arange(rot // 2) / max(1, rot // 2))
+        self.rng, self.heads, self.kv_heads, self.dim, self.interleaved = rng, heads, kv_heads, dim, interleaved
+        shape = (self.pages, kv_heads, page, dim)
+        self.cache = dict(k=np.full(shape, 0x7F, np.uint8), v=np.full(shape, 0xFF, np.uint8), k_scale=np.full(shape[:2], np.nan, np.float32),
+                          v_scale=np.full(shape[:2], np.nan, np.float32))
+
+    def fill(self):
+        """What earlier steps would have written."""
+        for b, kv in enumerate(self.kv):
+            for s, pg in enumerate(self.table[b]):
+                rows = min(self.page, kv - s * self.page)
+                if not 0 <= pg < self.pages or rows <= 0:
+                    continue
+                for name in "kv":
+                    codes = self.rng.integers(0, 0x7F, (self.kv_heads, rows, self.dim)).astype(np.uint8)
+                    self.cache[name][pg, :, :rows] = codes | (self.rng.integers(0, 2, codes.shape) << 7).astype(np.uint8)
+                    self.cache[name + "_scale"][pg] = 2.0 ** self.rng.integers(-9, -5, self.kv_heads)
+        return self
+
+    def device_cache(self):
+        t = {n: torch.from_numpy(a.copy()).to(DEV) for n, a in self.cache.items()}
+        return binding.KvCache(t["k"], t["v"], t["k_scale"], t["v_scale"])
+
+    def rows(self, heads, std=1.0, pad=0):
+        """[T, heads, dim] on the device, pad elements between tokens, and the same numbers in 64 bits."""
+        x = torch.from_numpy(self.rng.standard_normal((self.T, heads * self.dim + pad)) * std).to(self.td)
+        return x.to(DEV)[:, :heads * self.dim].unflatten(1, (heads, self.dim)), x[:, :heads * self.dim].double().reshape(self.T, heads, self.dim).numpy()
+
+    def args(self, table=None):
+        return ints(self.offsets), ints(self.kv), ints(table if table is not None else self.table)
+
+    def attend(self, pad=0, max_q=None, max_kv=None, scale=None, table=None, **kw):
+        scale = self.dim ** -0.5 if scale is None else scale
+        q, q64 = self.rows(self.heads, 1.5, pad)
+        out, lse = self.att.moe_attn_forward(self.device_cache(), q, *self.args(table), max(self.n + [1]) if max_q is None else max_q,
+                                             max(self.kv) if max_kv is None else max_kv, scale=scale, **kw)
+        ref = od.attend(self.cache, q64, self.offsets, self.kv, self.table if table is None else table, self.page, np.float32(scale), kw.get("causal", True),
+                        kw.get("window", 0))
+        self.check(out, lse, ref)
+        return q, out, lse
+
+    def check(self, out, lse, ref):
+        out, lse = out.double().cpu().numpy(), lse.double().cpu().numpy()
+        want, want_lse, A, K = ref
+        ulp, kv = 2.0 ** -24, max(self.kv)
+        ds = (self.dim + 8) * ulp * K[..., None]
+        half = 2.0 ** -8 if self.dtype == "bf16" else ulp
+        tol = A * (2 * ds + (2 * kv + 16) * ulp + half) + np.abs(want) * half + kv * 449 * 2.0 ** -126
+        assert np.isfinite(out).all()
+        over = np.abs(out - want) > tol
+        assert not over.any(), "%d of %d outputs, worst %.3g times the bound, rows %s" % (
+            over.sum(), over.size, (np.abs(out - want) / np.maximum(tol, 1e-300)).max(), sorted(set(np.argwhere(over)[:, 0]))[:10])
+        empty = np.isneginf(want_lse)
+        assert np.array_equal(empty, np.isneginf(lse)) and not out[empty].any()
+        far = np.abs(lse[~empty] - want_lse[~empty])
+        assert (far <= (ds[..., 0] + (kv + 16) * ulp + 4 * ulp * np.abs(want_lse))[~empty]).all(), far.max()
+
+
+@pytest.mark.parametrize("dim", [64, 128, 256])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("page", [16, 64])
+def test_decode(dim, dtype, page):
+    """Lengths around pages and tiles, from none to several tiles for each wave."""
+    kv = [1, 0, 15, 16, 17, 31, 63, 64, 65, 300, 700]
+    Batch([1] * len(kv), kv, 8, 2, dim, page, dtype).fill().attend()
+
+
+@pytest.mark.parametrize("heads,kv_heads", [(1, 1), (4, 4), (6, 2), (16, 1), (20, 1), (34, 2)])
+@pytest.mark.parametrize("page", [32, 128])
+def test_head_layouts(heads, kv_heads, page):
+    """Groups of one, odd groups, groups over the 16 columns of a tile."""
+    Batch([1, 1, 1], [130, 5, 1], heads, kv_heads, 128, page).fill().attend()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("dim", [64, 128, 256])
+@pytest.mark.parametrize("causal", [True, False])
+def test_prefill(dim, dtype, causal):
+    """Chunks with and without history, ragged, one sequence without new tokens, one without any."""
+    Batch([37, 0, 65, 1, 130, 0], [37, 50, 100, 9, 131, 0], 4, 2, dim, 16, dtype).fill().attend(causal=causal)
+
+
+@pytest.mark.parametrize("window", [1, 16, 50, 64, 1000])
+@pytest.mark.parametrize("n", [1, 5, 70])
+@pytest.mark.parametrize("causal", [True, False])
+def test_window(window, n, causal):
+    Batch([n, 1, min(n, 3)], [200 + n, 90, 3], 4, 2, 64, 32).fill().attend(window=window, causal=causal)
+
+
+def test_window_with_released_pages():
+    """Pages in front of every query's window may be gone from the table."""
+    b = Batch([2, 3], [400, 37], 4, 2, 64, 16).fill()
+    table = [list(r) for r in b.table]
+    table[0][:20] = [-1] * 20                       # positions 0 .. 319; the window begins at 399 - 69
+    b.attend(window=70, table=table)
+
+
+def test_rows_that_see_nothing():
+    """More new tokens than cached ones (the first positions are negative), and pages that are missing altogether."""
+    b = Batch([5, 3, 40], [2, 3, 33], 4, 4, 64, 16).fill()
+    b.attend(max_q=40)
+    table = [list(r) for r in b.table]
+    table[1] = [-1] * b.max_pages
+    table[2][1] = b.pages + 5                       # a number past the cache: as missing
+    b.attend(table=table, max_q=40)
+    b.attend(table=table, max_q=40, causal=False)
+
+
+@pytest.mark.parametrize("n", [1, 4])
+def test_long_sequences_are_shared_by_blocks(n):
+    """Few sequences: every unit is cut between blocks and joined."""
+    Batch([n, 1, 1], [9000 + n, 3, 5000], 4, 1, 64, 64).fill().attend()
+
+
+def test_prefill_behind_a_long_history():
+    Batch([33, 20], [3000, 2500], 4, 1, 128, 64).fill().attend()
+
+
+@pytest.mark.parametrize("n", [1, 40])
+def test_strided_queries_other_scale_and_no_lse(n):
+    b = Batch([n, 2], [n + 60, 100], 8, 2, 128, 32).fill()
+    b.attend(pad=8, scale=0.3)
+    b.attend(pad=1024, scale=-0.05)
+    q, out, _ = b.attend(scale=0.1)
+    again, none = b.att.moe_attn_forward(b.device_cache(), q, *b.args(), max(b.n), max(b.kv), scale=0.1, want_lse=False)
+    assert none is None and torch.equal(again, out)
+
+
+@pytest.mark.parametrize("n,kv", [(1, 900), (90, 400)])
+def test_large_scores_and_scales(n, kv):
+    """Scores of some hundreds: all weight on single keys; scales far from one."""
+    b = Batch([n, 1], [kv, 70], 4, 2, 64, 16).fill()
+    b.cache["k_scale"][:] = np.where(np.isnan(b.cache["k_scale"]), np.nan, b.cache["k_scale"] * 16)
+    b.cache["v_scale"][:] = np.where(np.isnan(b.cache["v_scale"]), np.nan, b.cache["v_scale"] * 2.0 ** 60)
+    b.attend()
+    b.cache["v_scale"][:] *= np.float32(2.0 ** -120)
+    b.attend()
+
+
+@pytest.mark.parametrize("n", [1, 64])
+def test_parts_joined_by_lse_are_the_whole(n):
+    """Two calls over halves of the keys, joined with their lse, against one over all of them (cross attention)."""
+    b = Batch([n], [256], 4, 2, 64, 64, "f32").fill()
+    q, out, lse = b.attend(causal=False)
+    cache, parts = b.device_cache(), []
+    for half in (0, 1):
+        table = [b.table[0][2 * half:2 * half + 2] + [-1, -1]]
+        parts.append(b.att.moe_attn_forward(cache, q, ints(b.offsets), ints([128]), ints(table), n, 128, causal=False))
+    both = torch.stack([p[1] for p in parts])
+    share = torch.softmax(both, 0)[..., None]
+    joined = share[0] * parts[0][0] + share[1] * parts[1][0]
+    # the halves' outputs and lse are within their bounds of 1e-5; a joined output within three of them
+    assert torch.allclose(joined, out, atol=3e-5 * float(out.abs().max()), rtol=0)
+    assert torch.allclose(torch.logsumexp(both, 0), lse, atol=3e-5, rtol=0)
+
+
+@pytest.mark.parametrize("n", [1, 70])
+def test_another_stream_and_a_graph(n):
+    """On a stream of its own, and captured: replays follow the lengths and inputs on the device."""
+    b = Batch([n, n], [n + 200, n + 7], 8, 2, 128, 32, rot=128).fill()
+    cache = b.device_cache()
+    q, _ = b.rows(8)
+    k, _ = b.rows(2)
+    v, _ = b.rows(2)
+    f = torch.from_numpy(b.inv_freq).to(DEV)
+    offsets, kv, table = b.args()
+    q_out, out, lse = torch.empty_like(q), torch.empty_like(q), torch.empty((b.T, 8), device=DEV)
+
+    def step():
+        b.att.moe_kv_append(cache, q, k, v, f, offsets, kv, table, n, q_out=q_out)
+        b.att.moe_attn_forward(cache, q_out, offsets, kv, table, n, n + 256, out=out, lse=lse)
+
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        step()
+    side.synchronize()
+    first = out.clone()
+    step()
+    torch.cuda.synchronize()
+    assert torch.equal(first, out)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step()
+    for round_ in range(3):
+        q.mul_(-0.5 if round_ else 1.0)
+        if round_ == 2:
+            kv.copy_(ints([n + 180, n + 3]))
+        out.zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        got, got_lse = out.clone(), lse.clone()
+        step()
+        torch.cuda.synchronize()
+        assert torch.equal(got, out) and torch.equal(got_lse, lse)
+
+
+def append_and_check(b, pad=0, std=1.0, q_too=True, max_q=None, table=None):
+    q, q64 = b.rows(b.heads, 1.0, pad) if q_too else (None, None)
+    k, k64 = b.rows(b.kv_heads, std, pad)
+    v, v64 = b.rows(b.kv_heads, std, pad)
+    dev = b.device_cache()
+    f = torch.from_numpy(b.inv_freq).to(DEV) if len(b.inv_freq) else None
+    got = b.att.moe_kv_append(dev, q, k, v, f, *b.args(table), max(b.n + [1]) if max_q is None else max_q)
+    want = od.append(b.cache, q64, k64, v64, b.inv_freq, b.interleaved, b.offsets, b.kv, b.table if table is None else table, b.page)
+    for name in ("k", "v", "k_scale", "v_scale"):
+        assert np.array_equal(getattr(dev, name).cpu().numpy(), b.cache[name], equal_nan=name.endswith("scale")), name
+    if q_too:
+        half = (2.0 ** -8 if b.dtype == "bf16" else 0) + 2.0 ** -24
+        assert (np.abs(got.double().cpu().numpy() - want) <= half * np.abs(want) + 1e-11 * np.abs(q64).max()).all()
+
+
+@pytest.mark.parametrize("dim,page", [(64, 16), (128, 64), (256, 128)])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("interleaved", [False, True])
+def test_append(dim, page, dtype, interleaved):
+    """A step of single tokens, chunks that begin and end inside pages, sequences without new tokens or none at all."""
+    b = Batch([1, 0, 1, 1, 1], [1, 7, page, page + 1, 2 * page + 3], 4, 2, dim, page, dtype, dim, interleaved).fill()
+    append_and_check(b)
+    b = Batch([page + 5, 0, 3, 2 * page, 1], [page + 9, 0, 3, 3 * page - 1, 40], 6, 3, dim, page, dtype, dim // 2, interleaved).fill()
+    append_and_check(b, pad=16)
+
+
+@pytest.mark.parametrize("rot", [0, 16, 64])
+def test_append_rotated_dimensions(rot):
+    b = Batch([9, 1], [30, 5], 2, 1, 64, 16, rot=rot).fill()
+    append_and_check(b)
+    append_and_check(b, q_too=False)
+
+
+@pytest.mark.parametrize("n", [1, 3, 20])
+def test_append_grows_scales(n):
+    """New tokens far above what the page holds, far below it, and all zero."""
+    for std in (1e4, 1e-6, 0.0, 1e30):
+        append_and_check(Batch([n, n], [n + 5, n + 40], 2, 2, 64, 32, rot=64, seed=n).fill(), std=std)
+
+
+def test_append_zeros_first():
+    """A page whose first rows are all zero takes the scale of what comes after them."""
+    b = Batch([1], [1], 2, 2, 64, 16)
+    append_and_check(b, std=0.0)
+    assert (b.cache["k_scale"][b.table[0][0]] == 2.0 ** -126).all()
+    b.kv = [2]
+    append_and_check(b)
+    assert (b.cache["k_scale"][b.table[0][0]] > 2.0 ** -10).all()
+
+
+def test_append_far_positions():
+    """A million tokens in: angles in 64 bits."""
+    b = Batch([2], [20], 2, 1, 128, 64, "f32", 128).fill()
+    b.inv_freq = b.inv_freq * 2.0 ** 16                                   # as at position 1.2 million
+    append_and_check(b)
+
+
+def test_append_token_by_token_equals_a_chunk():
+    """Where no scale grows below the normal range, the order of arrival does not show."""
+    one, all_ = (Batch([40], [40], 2, 2, 64, 16, rot=64, seed=4) for _ in range(2))
+    k, _ = one.rows(2)
+    v, _ = one.rows(2)
+    f = torch.from_numpy(one.inv_freq).to(DEV)
+    a, c = one.device_cache(), all_.device_cache()
+    all_.att.moe_kv_append(c, None, k, v, f, *one.args(), 40)
+    for i in range(40):
+        one.att.moe_kv_append(a, None, k[i:i + 1], v[i:i + 1], f, ints([0, 1]), ints([i + 1]), ints(one.table), 1)
+    for name in "kv":
+        x, y = (getattr(z, name).view(torch.float8_e4m3fn).float()[one.table[0]] * getattr(z, name + "_scale")[one.table[0]][..., None, None] for z in (a, c))
+        x, y = (z.permute(1, 0, 2, 3).reshape(2, -1, 64)[:, :40] for z in (x, y))
+        s = getattr(c, name + "_scale")[one.table[0]].max()
+        # rounding anew costs at most half the smallest step, 2^-10 of the scale
+        assert ((x - y).abs() <= s * 2.0 ** -10).all() and torch.equal(getattr(a, name + "_scale")[one.table[0]], getattr(c, name + "_scale")[one.table[0]])
+
+
+def test_append_to_pages_that_are_missing():
+    """Table entries outside the cache: those tokens are left out, the others land."""
+    b = Batch([40, 3], [45, 3], 2, 2, 64, 16, rot=64).fill()
+    table = [list(r) for r in b.table]
+    table[0][1], table[1][0] = -1, b.pages
+    append_and_check(b, table=table)
+
+
+def test_append_more_tokens_than_the_length():
+    append_and_check(Batch([6, 1], [4, 9], 2, 1, 64, 16, rot=64).fill())
+
+
+def test_refusals():
+    b = Batch([1, 1], [20, 30], 4, 2, 64, 16, rot=64).fill()
+    cache, (q, _), (k, _), (v, _) = b.device_cache(), b.rows(4), b.rows(2), b.rows(2)
+    f = torch.from_numpy(b.inv_freq).to(DEV)
+    batch = b.args()
+
+    def code(call):
+        with pytest.raises(binding.MoeError) as e:
+            call()
+        return e.value.code
+
+    bad = binding.MOE_ERR_INVALID_ARG
+    assert code(lambda: b.att.moe_kv_append(cache, q, k, v, None, *batch, 1)) == bad
+    assert code(lambda: b.att.moe_kv_append(cache, q, k, v, f, *batch, -1)) == bad
+    assert code(lambda: b.att.moe_attn_forward(cache, q, *batch, 1, 30, window=-1)) == bad
+    assert code(lambda: b.att.moe_attn_forward(cache, q, *batch, 1, -1)) == bad
+    assert code(lambda: b.att.moe_attn_forward(cache, q, *batch, 1, 30, scale=math.inf)) == bad
+    assert code(lambda: b.att.moe_attn_forward(cache, q, *batch, 1, 30, causal=2)) == bad
+    many = ints([0, 1, 2, 2]), ints([20, 30, 1]), ints(b.table + [b.table[0]])
+    assert code(lambda: b.att.moe_attn_forward(cache, q, *many, 1, 30)) == bad        # B > B_max
+    wide = torch.zeros((2, 4 * 64 + 4), dtype=torch.bfloat16, device=DEV)[:, :256].unflatten(1, (4, 64))
+    assert code(lambda: b.att.moe_attn_forward(cache, wide, *batch, 1, 30)) == bad    # rows at no multiple of 16 bytes
+    ws = b.att.workspace
+    b.att.workspace = ws[:256]
+    assert code(lambda: b.att.moe_attn_forward(cache, q, *batch, 1, 30)) == binding.MOE_ERR_WORKSPACE
+    b.att.workspace = ws
+    for call in (lambda: b.att.moe_attn_forward(cache, q.float(), *batch, 1, 30), lambda: b.att.moe_attn_forward(cache, q[:, :2], *batch, 1, 30),
+                 lambda: b.att.moe_kv_append(cache, q, k[:, :1], v, f, *batch, 1), lambda: b.att.moe_kv_append(cache, q, k, v, f.float(), *batch, 1),
+                 lambda: b.att.moe_attn_forward(cache, q, batch[0], batch[1].long(), batch[2], 1, 30)):
+        with pytest.raises(ValueError):
+            call()
+    out, lse = b.att.moe_attn_forward(cache, q[:0], ints([0, 0, 0]), ints([20, 30]), batch[2], 1, 30)   # nothing to do
+    assert out.shape[0] == 0 and lse.shape[0] == 0
