@@ -1,12 +1,17 @@
 // The next token of every row of logits: temperature, top-k, top-p, min-p, and a draw from given random numbers.
 //
-// All filters keep a beginning of one order (descending logit, ascending index), so a row's kept set is a threshold: a key (the
-// logit's bits, made to order like the logit) and how many of the tokens with just that key stay.  It is found by radix
-// selection on the keys, over counts for top-k and over weights for top-p, without sorting the row.
+// All filters keep a beginning of one order (descending logit, ascending index), so a row's kept set is one threshold on the pair
+// (key: the logit's bits, made to order like the logit; index).  It is found without sorting the row: a histogram over 2048 steps of
+// 1/32 in (largest - logit) / temperature, of counts for top-k and of weights for top-p, says which step holds the border.  Where the
+// tokens down to that step are few (kCandidates), they alone are sorted, and all that is left happens on them; where they are many, the
+// ones of the border step alone; where these are too many as well (a flat or a very wide row), a radix walk over the pairs settles
+// it, 8 bits a pass over the row.
 //
-// Weights are exp in 64 bits, summed as whole numbers of 2^-f (f = 62 - ceil(log2 V)): sums of whole numbers do not depend on
-// their order, so the parallel sums give one result, and an error of V 2^-(f+1) at most, under 1e-11 of the sum for the usual V.
+// Weights are exp in 64 bits, summed as whole numbers of 2^-f (f = 62 - ceil(log2 V), at most 50): sums of whole numbers do not depend on
+// their order, so atomic sums give one result, and an error of V 2^-(f+1) at most, under 1e-11 of the sum for the usual V.
 // The token at the border of a cumulative sum then is the one that sums in 64 bits choose.
+#include <mutex>
+
 #include "moe_internal.h"
 
 namespace moe355 {
@@ -27,17 +32,48 @@ struct SampleParams {
 
 static constexpr uint32_t kLowest = 0x007fffffu;  // key of -infinity
 
+// NaN is -infinity (the larger of a number and a NaN is the number)
+__device__ __forceinline__ float clean(float v) { return fmaxf(v, -INFINITY); }
 template <bool BF16>
 __device__ __forceinline__ float logit_at(const void *row, int i)
 {
-    float v = BF16 ? __uint_as_float((uint32_t)static_cast<const uint16_t *>(row)[i] << 16) : static_cast<const float *>(row)[i];
-    v += 0.f;  // -0 is 0
-    return v != v ? -INFINITY : v;
+    return clean(BF16 ? __uint_as_float((uint32_t)static_cast<const uint16_t *>(row)[i] << 16) : static_cast<const float *>(row)[i]);
 }
-// orders like the logit
+// 16 bytes of a row at a time.  Rows lie at any element, so the load is told nothing about its alignment (the hardware needs none).
+template <bool BF16>
+struct Vec {
+    static constexpr int kN = BF16 ? 8 : 4;
+    uint32_t w[4];
+    __device__ __forceinline__ float raw(int j) const
+    {
+        return BF16 ? __uint_as_float(j & 1 ? w[j >> 1] & 0xffff0000u : w[j >> 1] << 16) : __uint_as_float(w[j & 3]);
+    }
+    __device__ __forceinline__ float operator[](int j) const { return clean(raw(j)); }
+};
+template <bool BF16>
+__device__ __forceinline__ Vec<BF16> load_vec(const char *row, int i, int V)
+{
+    Vec<BF16> v;
+    if (i + Vec<BF16>::kN <= V) {
+        __builtin_memcpy(v.w, row + (int64_t)i * (BF16 ? 2 : 4), 16);
+    } else {  // past the end: -infinity
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            if (BF16) {
+                const uint32_t lo = i + 2 * j < V ? reinterpret_cast<const uint16_t *>(row)[i + 2 * j] : 0xff80u;
+                const uint32_t hi = i + 2 * j + 1 < V ? reinterpret_cast<const uint16_t *>(row)[i + 2 * j + 1] : 0xff80u;
+                v.w[j] = lo | hi << 16;
+            } else {
+                v.w[j] = i + j < V ? reinterpret_cast<const uint32_t *>(row)[i + j] : 0xff800000u;
+            }
+        }
+    }
+    return v;
+}
+// orders like the logit; -0 is 0
 __device__ __forceinline__ uint32_t key_of(float v)
 {
-    const uint32_t u = __float_as_uint(v);
+    const uint32_t u = __float_as_uint(v + 0.f);
     return u & 0x80000000u ? ~u : u | 0x80000000u;
 }
 __device__ __forceinline__ float logit_of(uint32_t key)
@@ -46,123 +82,185 @@ __device__ __forceinline__ float logit_of(uint32_t key)
 }
 
 struct Row {
-    double top, temperature;
-    double unit;  // 2^f
+    float largest, steps;  // steps of the histogram in one unit of the logit
+    double top, rate;      // log2(e) / temperature
+    double unit;           // 2^f
 };
-__device__ __forceinline__ double weight(const Row &r, float v)
-{
-    return (double)v == r.top ? 1.0 : exp(((double)v - r.top) / r.temperature);
-}
-__device__ __forceinline__ u64 whole(const Row &r, double w) { return (u64)rint(w * r.unit); }
 
-static constexpr int kThreads = 1024;
+// 2^(i / 32)
+__constant__ static const double kRoots[32] = {
+    1.0, 1.0218971486541166, 1.0442737824274138, 1.0671404006768237,
+    1.0905077326652577, 1.1143867425958924, 1.1387886347566916, 1.1637248587775775,
+    1.189207115002721, 1.215247359980469, 1.241857812073484, 1.2690509571917332,
+    1.2968395546510096, 1.3252366431597413, 1.3542555469368927, 1.383909881963832,
+    1.4142135623730951, 1.4451808069770467, 1.4768261459394993, 1.5091644275934228,
+    1.5422108254079407, 1.5759808451078865, 1.6104903319492543, 1.645755478153965,
+    1.681792830507429, 1.718619298122478, 1.7562521603732995, 1.7947090750031072,
+    1.8340080864093424, 1.8741676341103, 1.9152065613971474, 1.9571441241754002,
+};
+
+// exp((v - largest) / temperature) = 2^y, y <= 0: y = n / 32 + rest, |rest| <= 1/64, 2^(n/32) from the table and the exponent, 2^rest by
+// its series (the first term left out is (ln 2 / 64)^6 / 720 = 2e-15 of it).  17 operations in 64 bits with whole(), a third of what exp() and a
+// division by the temperature take, and the kernel is bound by them. 
+// Without a branch: -infinity gives 2^-1000, and where the largest logit is infinite, top is 1e300 and infinity gives 1.
+__device__ __forceinline__ double weight(const Row &r, float v, const double *roots)
+{
+    const double y = fmin(fmax(((double)v - r.top) * r.rate, -1000.0), 0.0);
+    const double magic = 6755399441055744.0;  // 1.5 * 2^52: a sum with it is rounded to a whole number, held in its low word
+    const double t = fma(y, 32.0, magic);
+    const int n = (int)(uint32_t)__double_as_longlong(t);
+    const double rest = fma(t - magic, -0.03125, y);
+    double e = 0.0013333558146428443;
+    e = fma(e, rest, 0.009618129107628477);
+    e = fma(e, rest, 0.05550410866482158);
+    e = fma(e, rest, 0.24022650695910072);
+    e = fma(e, rest, 0.6931471805599453);
+    e = fma(e, rest, 1.0);
+    e *= roots[n & 31];
+    // y > -1000: the exponent stays that of a normal number
+    return __longlong_as_double(__double_as_longlong(e) + ((long long)(n >> 5) << 52));
+}
+// w * 2^f to the nearest whole number; f <= 50 and w <= 1, so that the sum with 2^52 holds it in its low bits
+__device__ __forceinline__ u64 whole(const Row &r, double w)
+{
+    return (u64)__double_as_longlong(fma(w, r.unit, 4503599627370496.0)) - 0x4330000000000000ull;
+}
+
+static constexpr int kThreads = 1024, kWaves = kThreads / 64, kSteps = 2048, kCandidates = 4096, kSegments = MOE_SAMPLE_MAX_V / 256;
+// Copies of the histogram, a lane's by its number: the logits of a wave crowd into few steps, and atomic sums on one address queue
+// (131072 sums of 64 bits over 8 steps by one block: 32 us with one copy, 16 with four, 13 with eight; 12 over 64 steps and more.  fp32 sums
+// would take 164 us wherever they go: the LDS adds fp32 a lane at a time.)
+static constexpr int kCopies = 4;
 
 struct Shared {
-    u64 mass[256];
-    uint32_t count[256];
-    u64 sum[kThreads / 64];
-    uint32_t ties[kThreads / 64];
-    uint32_t best_key;
-    int best_index;
+    union {
+        u64 histogram[kSteps * kCopies];  // counts or weights; then
+        u64 segment[kSegments];           // the kept weights of every 64 vectors of the row
+    };
+    u64 candidate[kCandidates];
+    u64 sum[kWaves];
+    double roots[32];                     // kRoots: lanes ask for different ones
+    uint32_t n, digit;
     u64 before;
-    uint32_t digit, before_count;
     int token;
-    u64 token_mass;
 };
 
-__device__ __forceinline__ u64 shfl_xor_u64(u64 v, int off) { return __shfl_xor(v, off, 64); }
+// The block's LDS.  Every function is inlined and asks for it itself: behind a reference the compiler may not know that it is LDS and
+// go through flat instructions, which are slower and not kept in order.
+extern __shared__ __align__(16) uint8_t lds[];
+__device__ __forceinline__ Shared &shared() { return *reinterpret_cast<Shared *>(lds); }
 
-__device__ u64 block_sum(u64 v, Shared &sh)
+__device__ __forceinline__ u64 pack(uint32_t key, int i) { return (u64)key << 32 | (uint32_t)~i; }  // orders like (logit, -index)
+
+// Step of the histogram, ascending as the logit descends, equal for equal logits.
+__device__ __forceinline__ int step_of(const Row &r, float v)
 {
+    const float d = r.largest - v;
+    return d > 0.f ? (int)fminf(d * r.steps, (float)(kSteps - 1)) : 0;
+}
+
+__device__ __forceinline__ u64 block_sum(u64 v)
+{
+    Shared &sh = shared();
 #pragma unroll
-    for (int off = 32; off >= 1; off >>= 1) v += shfl_xor_u64(v, off);
+    for (int off = 32; off >= 1; off >>= 1) v += __shfl_xor(v, off, 64);
     __syncthreads();
     if ((threadIdx.x & 63) == 0) sh.sum[threadIdx.x >> 6] = v;
     __syncthreads();
     u64 all = 0;
-    for (int w = 0; w < kThreads / 64; ++w) all += sh.sum[w];
+#pragma unroll
+    for (int w = 0; w < kWaves; ++w) all += sh.sum[w];
     return all;
 }
 
-// exclusive prefix over the block of (ties, mass), and their totals
-__device__ void block_scan(uint32_t &ties, u64 &mass, uint32_t &all_ties, u64 &all_mass, Shared &sh)
+// Exclusive prefix over the block's threads.
+__device__ __forceinline__ u64 block_scan(u64 mine)
 {
+    Shared &sh = shared();
     const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
-    uint32_t t = ties;
-    u64 m = mass;
+    u64 x = mine;
 #pragma unroll
     for (int off = 1; off < 64; off <<= 1) {
-        const uint32_t ot = __shfl_up(t, off, 64);
-        const u64 om = __shfl_up(m, off, 64);
-        if (lane >= off) {
-            t += ot;
-            m += om;
-        }
+        const u64 o = __shfl_up(x, off, 64);
+        if (lane >= off) x += o;
     }
     __syncthreads();
-    if (lane == 63) {
-        sh.ties[w] = t;
-        sh.sum[w] = m;
-    }
+    if (lane == 63) sh.sum[w] = x;
     __syncthreads();
-    uint32_t bt = 0;
-    u64 bm = 0;
-    all_ties = 0;
-    all_mass = 0;
-    for (int i = 0; i < kThreads / 64; ++i) {
-        if (i < w) {
-            bt += sh.ties[i];
-            bm += sh.sum[i];
-        }
-        all_ties += sh.ties[i];
-        all_mass += sh.sum[i];
-    }
-    ties = bt + t - ties;
-    mass = bm + m - mass;
+    u64 front = 0;
+#pragma unroll
+    for (int i = 0; i < kWaves; ++i) front += i < w ? sh.sum[i] : 0;
+    return front + x - mine;
 }
 
-// A beginning of the order: all tokens with a greater key, and the first `ties` with this one.
-struct Cut {
-    uint32_t key;
-    uint32_t ties;
-};
-
-// Radix walk from the top digit down: the key at which the running count (or mass) of the tokens within `in`, in descending order of
-// keys, reaches `target`; `before`: the running value in front of that key.
-template <bool BF16, bool MASS>
-__device__ void walk(const void *row, int V, const Row &r, const Cut &in, u64 in_tie_mass, double target, uint32_t &key, u64 &before, Shared &sh)
+// f(v, index) for every token of the row (-infinity for places past its end); after each vector done(its number).  A thread has the next
+// two vectors in flight, and the work of four tokens at most is mixed by the compiler: with more of it in registers the 64-bit arithmetic
+// spills.  skip(largest logit of a vector): whether f need not see the vector; where few tokens matter, a branch a token would cost six times
+// as much as all else (a 128000-token row by one block: 30 us, a branch a vector 5).
+template <bool BF16, typename S, typename F, typename G>
+__device__ __forceinline__ void over_row(const char *row, int V, S skip, F f, G done)
 {
-    const int tid = threadIdx.x;
-    uint32_t prefix = 0;
-    before = 0;
-    for (int shift = 24; shift >= 0; shift -= 8) {
-        __syncthreads();
-        if (tid < 256) sh.mass[tid] = 0;
-        __syncthreads();
-        for (int i = tid; i < V; i += kThreads) {
-            const float v = logit_at<BF16>(row, i);
-            const uint32_t k = key_of(v);
-            if (k <= kLowest || k <= in.key || (shift < 24 && (k >> (shift + 8)) != prefix)) continue;
-            atomicAdd(&sh.mass[(k >> shift) & 255], MASS ? whole(r, weight(r, v)) : 1ull);
+    static constexpr int kN = Vec<BF16>::kN, kFlight = 2;
+    const int vectors = (V + kN - 1) / kN;
+    Vec<BF16> x[kFlight];
+#pragma unroll
+    for (int u = 0; u < kFlight; ++u) x[u] = load_vec<BF16>(row, min((int)threadIdx.x + u * kThreads, vectors) * kN, V);
+#pragma unroll 1
+    for (int base = 0; base < vectors; base += kFlight * kThreads) {  // the same count for all threads: done() may use the whole wave
+#pragma unroll
+        for (int u = 0; u < kFlight; ++u) {
+            const int at = base + u * kThreads + threadIdx.x;
+            const Vec<BF16> now = x[u];
+            x[u] = load_vec<BF16>(row, min(at + kFlight * kThreads, vectors) * kN, V);
+            float most = now.raw(0);
+#pragma unroll
+            for (int j = 1; j < kN; ++j) most = fmaxf(most, now.raw(j));
+            if (!skip(most)) {
+#pragma unroll
+                for (int j = 0; j < kN; ++j) {
+                    f(now[j], at * kN + j);
+                    if (j % 4 == 3) __builtin_amdgcn_sched_barrier(0);
+                }
+            }
+            done(at);
         }
+    }
+}
+
+// The border of a step that holds too many tokens to sort, `before` in front of the step: walks the step's pairs from the cut on, 8 bits
+// a pass from the top, to the one at which the running value reaches the target; that pair is the last that stays.
+template <bool BF16>
+__device__ __forceinline__ u64 walk(const char *row, int V, const Row &r, bool by_mass, int step, u64 cut, u64 before, double target)
+{
+    Shared &sh = shared();
+    const int tid = threadIdx.x;
+    u64 prefix = 0;
+#pragma unroll 1
+    for (int shift = 56; shift >= 0; shift -= 8) {
+        __syncthreads();
+        if (tid < 512) sh.candidate[tid] = 0;
+        __syncthreads();
+        over_row<BF16>(row, V, [](float) { return false; }, [&](float v, int i) {
+            if (v == -INFINITY || step_of(r, v) != step) return;
+            const u64 c = pack(key_of(v), i);
+            if (c < cut || (shift < 56 && (c >> (shift + 8)) != prefix)) return;
+            const int digit = (int)(c >> shift) & 255;
+            atomicAdd(&sh.candidate[digit], by_mass ? whole(r, weight(r, v, sh.roots)) : 1ull);
+            atomicAdd(&sh.candidate[256 + digit], 1ull);  // a digit whose tokens weigh nothing is a digit all the same
+        }, [](int) {});
         __syncthreads();
         if (tid == 0) {
-            // tokens with the border key of `in`, which are not all within it
-            if (in.key > kLowest && (shift == 24 || (in.key >> (shift + 8)) == prefix))
-                sh.mass[(in.key >> shift) & 255] += MASS ? in_tie_mass * in.ties : in.ties;
-            u64 run = before;
+            u64 run = before, last_run = run;
             int digit = -1, last = 0;
-            u64 last_run = run;
             for (int d = 255; d >= 0; --d) {
-                if (!sh.mass[d]) continue;
-                // the first digit at which the running value reaches the target
-                if ((double)(run + sh.mass[d]) >= target) {
+                if (!sh.candidate[256 + d]) continue;
+                last = d;
+                last_run = run;
+                if ((double)(run + sh.candidate[d]) >= target) {
                     digit = d;
                     break;
                 }
-                last = d;
-                last_run = run;
-                run += sh.mass[d];
+                run += sh.candidate[d];
             }
             sh.digit = digit < 0 ? last : digit;
             sh.before = digit < 0 ? last_run : run;
@@ -171,117 +269,336 @@ __device__ void walk(const void *row, int V, const Row &r, const Cut &in, u64 in
         prefix = prefix << 8 | sh.digit;
         before = sh.before;
     }
-    key = prefix;
+    return prefix;
 }
 
+// The candidates, descending (bitonic over the next power of two; the places behind them are 0, below every pair).  Exchanges over
+// less than 128 places stay inside a wave's own 128, without a barrier.
+__device__ __forceinline__ void sort_candidates(int n)
+{
+    Shared &sh = shared();
+    int m = 128;
+    while (m < n) m <<= 1;
+    for (int i = n + threadIdx.x; i < m; i += kThreads) sh.candidate[i] = 0;
+    const auto exchange = [&](int i, int gap, int size) {
+        const int lo = 2 * i - (i & (gap - 1)), hi = lo + gap;
+        const u64 a = sh.candidate[lo], b = sh.candidate[hi];
+        if ((a < b) == ((lo & size) == 0)) {
+            sh.candidate[lo] = b;
+            sh.candidate[hi] = a;
+        }
+    };
+    __syncthreads();
+    for (int size = 2; size <= m; size <<= 1) {
+        int gap = size >> 1;
+        for (; gap >= 128; gap >>= 1) {
+            for (int i = threadIdx.x; i < m / 2; i += kThreads) exchange(i, gap, size);
+            __syncthreads();
+        }
+        for (; gap > 0; gap >>= 1) {
+            // threads 64 k .. 64 k + 63 exchange inside places 128 k .. 128 k + 127
+            for (int i = threadIdx.x; i < m / 2; i += kThreads) exchange(i, gap, size);
+            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "workgroup");  // waits for the wave's own accesses
+            __builtin_amdgcn_wave_barrier();
+        }
+        if (size >= 128) __syncthreads();
+    }
+    __syncthreads();
+}
+
+// The step in which the running value of the histogram reaches the target, and the running value in front of it; kSteps where it
+// never does.  upto: how many tokens the steps up to it hold, by weight only about: a token of step i weighs 2^f exp(-(i + 1/2) / 32), two per
+// cent more or less.
+__device__ __forceinline__ int border_step(const Row &r, bool by_mass, double target, u64 &before, float &upto)
+{
+    static constexpr int kEach = kSteps / kThreads;
+    Shared &sh = shared();
+    const int at = threadIdx.x * kEach;
+    u64 own[kEach], mine = 0;
+#pragma unroll
+    for (int i = 0; i < kEach; ++i) {
+        own[i] = 0;
+#pragma unroll
+        for (int c = 0; c < kCopies; ++c) own[i] += sh.histogram[(at + i) * kCopies + c];
+        mine += own[i];
+    }
+    u64 run = block_scan(mine);
+    if (threadIdx.x == 0) sh.digit = kSteps;
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < kEach; ++i) {
+        if ((double)run < target && (double)(run + own[i]) >= target) {  // one place at most
+            sh.digit = at + i;
+            sh.before = run;
+        }
+        run += own[i];
+    }
+    __syncthreads();
+    const int s = sh.digit;
+    before = sh.before;
+    float tokens = 0.f;
+#pragma unroll
+    for (int i = 0; i < kEach; ++i)
+        if (at + i <= s) tokens += by_mass ? (float)own[i] / (float)r.unit * __expf(fminf((float)(at + i) * 0.03125f + 0.015625f, 80.f)) : (float)own[i];
+    tokens = fminf(tokens, 1e9f);
+    upto = (float)block_sum((u64)tokens);
+    return s;
+}
+
+// The last of the n sorted candidates in front of which the running value, `before` in front of the first, is below the target.
+__device__ __forceinline__ u64 border_candidate(const Row &r, bool by_mass, int n, double target, u64 before)
+{
+    Shared &sh = shared();
+    int last = 0;
+    for (int base = 0; base < n; base += kThreads) {
+        const int i = base + threadIdx.x;
+        const u64 mine = i >= n ? 0 : by_mass ? whole(r, weight(r, logit_of((uint32_t)(sh.candidate[i] >> 32)), sh.roots)) : 1;
+        const u64 at = before + block_scan(mine);
+        const int stay = (int)block_sum(i < n && (double)at < target ? 1 : 0);
+        if (stay > 0) last = base + stay - 1;
+        if (stay < min(n - base, kThreads)) break;
+        before += block_sum(mine);
+    }
+    return sh.candidate[last];
+}
+
+// A block a row.
 template <bool BF16>
 __global__ __launch_bounds__(kThreads) void sample_kernel(SampleParams p)
 {
-    __shared__ Shared sh;
-    const int b = blockIdx.x, tid = threadIdx.x;
+    Shared &sh = shared();
+    const int b = blockIdx.x, tid = threadIdx.x, lane = tid & 63;
     const char *row = static_cast<const char *>(p.logits) + (int64_t)b * p.stride * (BF16 ? 2 : 4);
-    // the first of the order
-    u64 best = 0;
-    for (int i = tid; i < p.V; i += kThreads) {
-        const u64 c = (u64)key_of(logit_at<BF16>(row, i)) << 32 | (uint32_t)~i;
-        best = c > best ? c : best;
+    const auto nothing = [](int) {};
+
+    if (tid < 32) sh.roots[tid] = kRoots[tid];
+    // the largest logit: four vectors of a thread in flight, an instruction a token
+    float largest = -INFINITY;
+    {
+        static constexpr int kN = Vec<BF16>::kN, kFlight = 4;
+        const int vectors = (p.V + kN - 1) / kN;
+        for (int base = tid; base < vectors; base += kThreads * kFlight) {
+            Vec<BF16> x[kFlight];
+#pragma unroll
+            for (int u = 0; u < kFlight; ++u) x[u] = load_vec<BF16>(row, min(base + u * kThreads, vectors) * kN, p.V);
+#pragma unroll
+            for (int u = 0; u < kFlight; ++u)
+#pragma unroll
+                for (int j = 0; j < kN; ++j) largest = fmaxf(largest, x[u].raw(j));  // of a number and a NaN the number
+        }
     }
 #pragma unroll
-    for (int off = 32; off >= 1; off >>= 1) {
-        const u64 o = shfl_xor_u64(best, off);
-        best = o > best ? o : best;
-    }
-    if ((tid & 63) == 0) sh.sum[tid >> 6] = best;
+    for (int off = 32; off >= 1; off >>= 1) largest = fmaxf(largest, __shfl_xor(largest, off, 64));
+    float *wave_top = reinterpret_cast<float *>(sh.sum);
+    if (lane == 0) wave_top[tid >> 6] = largest;
+    if (tid == 0) sh.token = 0x7fffffff;
     __syncthreads();
-    for (int w = 0; w < kThreads / 64; ++w) best = sh.sum[w] > best ? sh.sum[w] : best;
-    const uint32_t top_key = (uint32_t)(best >> 32);
-    const int first = (int)~(uint32_t)best;
+#pragma unroll
+    for (int w = 0; w < kWaves; ++w) largest = fmaxf(largest, wave_top[w]);
+    largest += 0.f;
     const float temperature = p.temperature ? p.temperature[b] : 1.f;
-    if (top_key <= kLowest || !(temperature > 0.f)) {
+    const bool greedy = !(temperature > 0.f), none = largest == -INFINITY;
+    const int top_k = p.top_k ? p.top_k[b] : 0;
+    const double top_p = p.top_p ? p.top_p[b] : 1.f, min_p = p.min_p ? p.min_p[b] : 0.f;
+    const bool only_first = greedy || min_p > 1.0 || top_k == 1 || !(top_p > 0.0);  // the first of the order alone stays
+    if (none || only_first) {
+        if (!none) {
+            int first = 0x7fffffff;
+            over_row<BF16>(row, p.V, [&](float most) { return most < largest; }, [&](float v, int i) { first = v == largest && i < first ? i : first; }, nothing);
+            if (first != 0x7fffffff) atomicMin(&sh.token, first);
+        }
+        __syncthreads();
         if (tid == 0) {
-            p.token[b] = top_key <= kLowest ? -1 : first;
-            if (p.logprob) p.logprob[b] = top_key <= kLowest ? -INFINITY : 0.f;
+            p.token[b] = none ? -1 : sh.token;
+            if (p.logprob) p.logprob[b] = none ? -INFINITY : 0.f;
         }
         return;
     }
-    const Row r = {(double)logit_of(top_key), (double)temperature, (double)(1ull << p.bits)};
-    const int top_k = p.top_k ? p.top_k[b] : 0;
-    const double top_p = p.top_p ? p.top_p[b] : 1.f, min_p = p.min_p ? p.min_p[b] : 0.f;
+    const Row r = {largest, fminf(32.f / temperature, 3e38f), largest < INFINITY ? (double)largest : 1e300, 1.44269504088896340736 / (double)temperature, (double)(1ull << p.bits)};
+    const int segments = ceil_div(p.V, 64 * Vec<BF16>::kN);
+    u64 cut = 0;        // tokens from this pair on stay
+    int n = 0;          // candidates
+    bool all = false;   // they are all that may stay
+    const auto below = [&](float most) { return !(most > -INFINITY) || (cut && most < logit_of((uint32_t)(cut >> 32))); };  // all below the cut
+    // The tokens of step hi, or of all up to it, from the cut on as candidates; their number may be more than there is room for.  What is not a
+    // candidate and surely stays by weight is summed by segments of the row on the way.
+    const auto gather = [&](int hi, bool only_hi, bool sum_up) {
+        __syncthreads();
+        if (tid == 0) sh.n = 0;
+        __syncthreads();
+        u64 kept = 0;
+        const auto beyond = [&](float most) { return hi < kSteps - 1 && (r.largest - most) * r.steps >= (float)(hi + 1); };  // in a step after hi
+        over_row<BF16>(row, p.V, beyond, [&](float v, int i) {
+            const int s = step_of(r, v);
+            const u64 c = pack(key_of(v), i);
+            const bool in = v > -INFINITY && s <= hi && c >= cut;
+            if (in && (s == hi || !only_hi)) {
+                const uint32_t at = atomicAdd(&sh.n, 1u);
+                if (at < (uint32_t)kCandidates) sh.candidate[at] = c;
+            } else if (sum_up) {
+                const double w = weight(r, v, sh.roots);
+                kept += in && w >= min_p ? whole(r, w) : 0;
+            }
+        }, [&](int at) {
+            if (!sum_up) return;
+            u64 sum = kept;
+#pragma unroll
+            for (int off = 32; off >= 1; off >>= 1) sum += __shfl_xor(sum, off, 64);
+            if (lane == 0 && at / 64 < segments) sh.segment[at / 64] = sum;
+            kept = 0;
+        });
+        __syncthreads();
+        return (int)sh.n;
+    };
+    const auto weigh = [&](u64 c) { return weight(r, logit_of((uint32_t)(c >> 32)), sh.roots); };
 
-    Cut cut = {kLowest, 0};
-    u64 tie_mass = 0;
-    if (top_k > 0 && top_k < p.V) {
-        uint32_t key;
-        u64 before;
-        walk<BF16, false>(row, p.V, r, cut, 0, (double)top_k, key, before, sh);
-        cut = {key, (uint32_t)(top_k - (int64_t)before)};
-        tie_mass = whole(r, weight(r, logit_of(key)));
-        // fewer tokens than top_k: the last key found has fewer ties than asked for, which the pass below counts out
-    }
-    if (top_p < 1.0) {
-        u64 mass = 0;
-        uint32_t ties = 0;
-        for (int i = tid; i < p.V; i += kThreads) {
-            const float v = logit_at<BF16>(row, i);
-            const uint32_t k = key_of(v);
-            if (k > cut.key && k > kLowest) mass += whole(r, weight(r, v));
-            ties += cut.key > kLowest && k == cut.key;
-        }
-        mass = block_sum(mass, sh);
-        const u64 all_ties = block_sum(ties, sh);
-        if (cut.key > kLowest && cut.ties > all_ties) cut.ties = (uint32_t)all_ties;
-        const double target = top_p * (double)(mass + tie_mass * cut.ties);
-        uint32_t key;
-        u64 before;
-        walk<BF16, true>(row, p.V, r, cut, tie_mass, target, key, before, sh);
-        const u64 one = whole(r, weight(r, logit_of(key)));
-        // ties stay while the sum in front of them is below the target
-        double n = one ? ceil((target - (double)before) / (double)one) : 1.0;
-        n = n < 1.0 ? 1.0 : n;
-        uint32_t keep = n > 4e9 ? 0xffffffffu : (uint32_t)n;
-        if (key == cut.key) keep = keep < cut.ties ? keep : cut.ties;
-        cut = {key, keep};
-        tie_mass = one;
-    }
-    // the kept tokens in ascending index: their sum, then the one at which the running sum passes u times it
-    const int last_tile = ceil_div(p.V, kThreads);
-    u64 total = 0;
-    double goal = 0.0;
-    for (int pass = 0; pass < 2; ++pass) {
-        u64 run = 0;
-        uint32_t run_ties = 0;
-        if (pass) goal = (double)p.u[b] * (double)total;
-        if (tid == 0) sh.token = 0x7fffffff;
-        for (int tile = 0; tile < last_tile; ++tile) {
-            const int i = tile * kThreads + tid;
-            const float v = i < p.V ? logit_at<BF16>(row, i) : -INFINITY;
-            const uint32_t k = key_of(v);
-            const bool tie = cut.key > kLowest && k == cut.key;
-            const double w = k > kLowest && (tie || k > cut.key) ? weight(r, v) : 0.0;
-            const bool big = w > 0.0 && (w >= min_p || i == first);
-            uint32_t ties = tie, all_ties;
-            u64 none = 0, all;
-            block_scan(ties, none, all_ties, all, sh);
-            const bool keep = big && (!tie || run_ties + ties < cut.ties);
-            const u64 mine = keep ? whole(r, w) : 0;
-            u64 before = mine;
-            uint32_t zero = 0, zeros;
-            block_scan(zero, before, zeros, all, sh);
-            if (pass && keep && (double)(run + before + mine) > goal) atomicMin(&sh.token, i);
-            run += all;
-            run_ties += all_ties;
+    bool summed = false;  // the segments hold what stays in front of the border step
+    // first by count, then by weight; in one loop, so that there is one copy of what they share
+#pragma unroll 1
+    for (int stage = 0; stage < 2; ++stage) {
+        const bool by_mass = stage == 1;
+        if (by_mass ? !(top_p < 1.0) : !(top_k > 0 && top_k < p.V)) continue;
+        double target = (double)top_k;
+        u64 before = 0, mine = 0;
+        int s = 0;
+        if (all) {  // by weight, of the candidates that top-k left
+            for (int i = tid; i < n; i += kThreads) mine += sh.candidate[i] >= cut ? whole(r, weigh(sh.candidate[i])) : 0;
+            target = top_p * (double)block_sum(mine);
+        } else {
             __syncthreads();
-            if (pass && sh.token != 0x7fffffff) break;
+            for (int i = tid; i < kSteps * kCopies; i += kThreads) sh.histogram[i] = 0;
+            __syncthreads();
+            u64 *const own = sh.histogram + (lane & (kCopies - 1));
+            if (by_mass)
+                over_row<BF16>(row, p.V, below, [&](float v, int i) {
+                    u64 w = whole(r, weight(r, v, sh.roots));
+                    w = pack(key_of(v), i) < cut ? 0 : w;
+                    mine += w;
+                    atomicAdd(own + step_of(r, v) * kCopies, w);
+                }, nothing);
+            else
+                // -infinity counts in the last step: where that makes it the border, it holds fewer candidates, and all stay
+                over_row<BF16>(row, p.V, below, [&](float v, int) { atomicAdd(own + step_of(r, v) * kCopies, 1ull); }, nothing);
+            const u64 sum = block_sum(mine);
+            if (by_mass) target = top_p * (double)sum;
+            float upto;
+            s = border_step(r, by_mass, target, before, upto);
+            if (s == kSteps) continue;  // fewer tokens than top_k
+            all = upto <= 0.95f * kCandidates;
+            summed = !all && by_mass;
+            n = gather(s, !all, summed);
+            if (all && n > kCandidates) {  // the estimate was wrong
+                all = false;
+                summed = by_mass;
+                n = gather(s, true, summed);
+            }
+            if (all) before = 0;
+            if (n == 0) continue;
+            if (n <= kCandidates) sort_candidates(n);
         }
-        total = pass ? total : run;
+        cut = n <= kCandidates ? border_candidate(r, by_mass, n, target, before) : walk<BF16>(row, p.V, r, by_mass, s, cut, before, target);
+    }
+
+    // what stays, by segments of the row
+    __syncthreads();
+    if (all || (summed && n <= kCandidates)) {
+        if (all) {
+            for (int i = tid; i < segments; i += kThreads) sh.segment[i] = 0;
+            __syncthreads();
+        }
+        for (int i = tid; i < n; i += kThreads) {
+            const u64 c = sh.candidate[i];
+            const double w = weigh(c);
+            if (c >= cut && w >= min_p) atomicAdd(&sh.segment[(int)~(uint32_t)c / (64 * Vec<BF16>::kN)], whole(r, w));
+        }
+    } else {
+        u64 kept = 0;
+        over_row<BF16>(row, p.V, below, [&](float v, int i) {
+            if (v == -INFINITY || pack(key_of(v), i) < cut) return;
+            const double w = weight(r, v, sh.roots);
+            if (w >= min_p) kept += whole(r, w);
+        }, [&](int at) {
+            u64 sum = kept;
+#pragma unroll
+            for (int off = 32; off >= 1; off >>= 1) sum += __shfl_xor(sum, off, 64);
+            if (lane == 0 && at / 64 < segments) sh.segment[at / 64] = sum;
+            kept = 0;
+        });
+    }
+    __syncthreads();
+    // the segment, and in it the token, at which the running sum passes u times the sum
+    static constexpr int kEach = (kSegments + kThreads - 1) / kThreads;
+    u64 mine = 0;
+    u64 own[kEach];
+#pragma unroll
+    for (int i = 0; i < kEach; ++i) {
+        const int at = tid * kEach + i;
+        own[i] = at < segments ? sh.segment[at] : 0;
+        mine += own[i];
+    }
+    const u64 total = block_sum(mine);
+    const double goal = (double)fminf(fmaxf(p.u[b], 0.f), 0.99999994f) * (double)total;  // below the total
+    u64 run = block_scan(mine);
+    if (tid == 0) sh.digit = 0;
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < kEach; ++i) {
+        const u64 next = run + own[i];
+        if ((double)run <= goal && (double)next > goal) {
+            sh.digit = tid * kEach + i;
+            sh.before = run;
+        }
+        run = next;
+    }
+    __syncthreads();
+    if (tid < 64) {
+        const int base = ((int)sh.digit * 64 + lane) * Vec<BF16>::kN;
+        const Vec<BF16> x = load_vec<BF16>(row, min(base, p.V), p.V);
+        u64 each[Vec<BF16>::kN], sum = 0;
+#pragma unroll
+        for (int j = 0; j < Vec<BF16>::kN; ++j) {
+            const float v = x[j];
+            each[j] = 0;
+            if (v != -INFINITY && pack(key_of(v), base + j) >= cut) {
+                const double w = weight(r, v, sh.roots);
+                if (w >= min_p) each[j] = whole(r, w);
+            }
+            sum += each[j];
+        }
+        u64 at = sum;
+#pragma unroll
+        for (int off = 1; off < 64; off <<= 1) {
+            const u64 o = __shfl_up(at, off, 64);
+            if (lane >= off) at += o;
+        }
+        at += sh.before - sum;
+#pragma unroll
+        for (int j = 0; j < Vec<BF16>::kN; ++j) {
+            if ((double)at <= goal && (double)(at + each[j]) > goal) sh.token = base + j;
+            at += each[j];
+        }
     }
     __syncthreads();
     if (tid == 0) {
-        // u < 1 in fp32 and whole numbers below 2^63: the sum passes u times itself, unless rounding of the product lifts it there
-        const int token = sh.token == 0x7fffffff ? first : sh.token;
+        const int token = min(sh.token, p.V - 1);  // the running sum passes a part of the total for some token; an index in any case
         p.token[b] = token;
-        if (p.logprob) p.logprob[b] = (float)log(weight(r, logit_at<BF16>(row, token)) / ((double)total / r.unit));
+        if (p.logprob) p.logprob[b] = (float)log(weight(r, logit_at<BF16>(row, token), sh.roots) / ((double)total / r.unit));
     }
+}
+
+template <bool BF16>
+int launch_as(const SampleParams &p, hipStream_t s)
+{
+    static std::once_flag once;
+    static hipError_t setup_rc = hipSuccess;
+    std::call_once(once, [&]() {
+        setup_rc = hipFuncSetAttribute(reinterpret_cast<const void *>(sample_kernel<BF16>), hipFuncAttributeMaxDynamicSharedMemorySize, (int)sizeof(Shared));
+    });
+    MOE_HIP_CHECK(setup_rc);
+    ProfScope ps("sample", s);
+    hipLaunchKernelGGL(sample_kernel<BF16>, dim3(p.B), dim3(kThreads), sizeof(Shared), s, p);
+    MOE_LAUNCH_CHECK("sample_kernel");
+    return MOE_OK;
 }
 
 }  // namespace
@@ -291,12 +608,10 @@ int launch_sample(const void *logits, int dtype, int64_t stride, int B, int V, c
 {
     int bits = 62;
     while ((1ll << (62 - bits)) < V) --bits;
+    bits = bits < 50 ? bits : 50;
     const SampleParams p = {logits, stride, B, V, bits, u, temperature, top_p, min_p, top_k, token, logprob};
     (void)ws;
-    if (dtype == MOE_DTYPE_BF16) hipLaunchKernelGGL(sample_kernel<true>, dim3(B), dim3(kThreads), 0, s, p);
-    else hipLaunchKernelGGL(sample_kernel<false>, dim3(B), dim3(kThreads), 0, s, p);
-    MOE_LAUNCH_CHECK("sample_kernel");
-    return MOE_OK;
+    return dtype == MOE_DTYPE_BF16 ? launch_as<true>(p, s) : launch_as<false>(p, s);
 }
 
 int64_t sample_workspace(int B, int V) { return 256 + 0 * (int64_t)B * V; }
