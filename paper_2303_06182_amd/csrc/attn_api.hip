@@ -12,6 +12,9 @@ int64_t sample_workspace(int B, int V);
 
 namespace {
 
+// Rows (new tokens times heads of a group) up to which a sequence is the decode kernel's, 16 at a time.
+constexpr int kFewRows = 32;
+
 bool bad_ptr(const void *p, const char *name, int align, bool nullable = false)
 {
     if (!p && nullable) return false;
@@ -159,7 +162,9 @@ int64_t moe_attn_workspace_bytes(const moe_attn_handle_t *h)
         set_error("handle is NULL");
         return MOE_ERR_INVALID_ARG;
     }
-    return attn_decode_workspace(h->cfg.head_dim, h->cfg.B_max, h->num_cus);
+    // partial results, of one kernel at a time, and where the sequences begin among the tiles
+    const int64_t decode = attn_decode_workspace(h->cfg.head_dim, h->num_cus), prefill = attn_prefill_workspace(h->cfg.head_dim, h->num_cus);
+    return (decode > prefill ? decode : prefill) + align_up((int64_t)(h->cfg.B_max + 1) * 8, 256);
 }
 
 int moe_kv_append(moe_attn_handle_t *h, const moe_kv_cache_t *cache, const void *q, int64_t q_stride, const void *k, int64_t k_stride,
@@ -225,7 +230,14 @@ int moe_attn_forward(moe_attn_handle_t *h, const moe_kv_cache_t *cache, const vo
     p.lse = lse;
     p.part = static_cast<float *>(workspace);
     p.seq_tiles = reinterpret_cast<int64_t *>(static_cast<uint8_t *>(workspace) + need - align_up((int64_t)(c.B_max + 1) * 8, 256));
-    return launch_attn_decode(c.dtype, c.head_dim, p, h->num_cus, (hipStream_t)stream);
+    p.few_rows = kFewRows;
+    const bool many = (int64_t)p.max_q * p.group > kFewRows;
+    // sequences of few rows: none where all sequences have max_q new tokens, and these are many
+    if (!many || (int64_t)p.max_q * B > T) {
+        const int failed = launch_attn_decode(c.dtype, c.head_dim, p, h->num_cus, (hipStream_t)stream);
+        if (failed != MOE_OK) return failed;
+    }
+    return many ? launch_attn_prefill(c.dtype, c.head_dim, p, h->num_cus, (hipStream_t)stream) : MOE_OK;
 }
 
 int64_t moe_sample_workspace_bytes(int32_t B, int32_t V)

@@ -14,15 +14,13 @@
 // Bound by HBM: 2 DH bytes a key, at 16 columns 32 MFMAs of 16 cycles per 16 KB and SIMD, far below.  Split: the tiles of all
 // (sequence, rows, head) units lie in one row and every block takes the same number of them, whatever the lengths are; a unit
 // that several blocks share leaves partial results that a second kernel joins.
-#include "attn_internal.h"
-#include "gemm_bf16_dev.h"
+#include "attn_dev.h"
 
 namespace moe355 {
 
 namespace {
 
 static constexpr int kThreads = 256, kWaves = 4;
-static constexpr float kLn2 = 0.69314718055994530942f;
 
 constexpr int tile_keys(int dh) { return dh <= 128 ? 64 : 32; }
 
@@ -39,7 +37,7 @@ __device__ __forceinline__ void seq_range(const AttnParams &p, const Seq &sq, in
 __device__ __forceinline__ int64_t seq_cost(const AttnParams &p, int b, int tile)
 {
     const Seq sq = load_seq(p, b);
-    if (sq.n == 0) return 0;
+    if (sq.n == 0 || sq.n * p.group > p.few_rows) return 0;
     int first, count;
     seq_range(p, sq, tile, first, count);
     return (int64_t)count * ceil_div(sq.n * p.group, 16) * p.n_kv_heads;
@@ -83,54 +81,6 @@ __device__ __forceinline__ int64_t tiles_per_block(int64_t total, int n_blocks)
 // A partial result: 16 rows of DH outputs (not divided by the sum), then the 16 maxima and the 16 sums
 template <int DH>
 constexpr int part_floats() { return 16 * DH + 32; }
-
-template <int NS>
-struct Pieces {
-    bf16x8 x[NS];
-};
-// eight fp32 numbers as NS bf16 pieces: rounded, the rest rounded, ..
-template <int NS>
-__device__ __forceinline__ Pieces<NS> split(const float (&v)[8])
-{
-    Pieces<NS> r;
-    float rest[8];
-#pragma unroll
-    for (int i = 0; i < 8; ++i) rest[i] = v[i];
-#pragma unroll
-    for (int n = 0; n < NS; ++n) {
-        uint32_t w[4];
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            w[i] = pack_bf16(rest[2 * i], rest[2 * i + 1]);
-            rest[2 * i] -= __uint_as_float(w[i] << 16);
-            rest[2 * i + 1] -= __uint_as_float(w[i] & 0xffff0000u);
-        }
-        const uint4 q = make_uint4(w[0], w[1], w[2], w[3]);
-        r.x[n] = __builtin_bit_cast(bf16x8, q);
-    }
-    return r;
-}
-
-__device__ __forceinline__ bf16x8 widen(uint32_t lo, uint32_t hi)
-{
-    uint4 w;
-    w.x = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, 1.f, false));
-    w.y = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, 1.f, true));
-    w.z = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, 1.f, false));
-    w.w = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, 1.f, true));
-    return __builtin_bit_cast(bf16x8, w);
-}
-
-// out[c] = byte c of r0, r1, r2, r3, for c = 0 .. 3
-__device__ __forceinline__ void transpose4(uint32_t r0, uint32_t r1, uint32_t r2, uint32_t r3, uint32_t (&out)[4])
-{
-    const uint32_t a = __builtin_amdgcn_perm(r1, r0, 0x05010400), b = __builtin_amdgcn_perm(r1, r0, 0x07030602);
-    const uint32_t c = __builtin_amdgcn_perm(r3, r2, 0x05010400), d = __builtin_amdgcn_perm(r3, r2, 0x07030602);
-    out[0] = __builtin_amdgcn_perm(c, a, 0x05040100);
-    out[1] = __builtin_amdgcn_perm(c, a, 0x07060302);
-    out[2] = __builtin_amdgcn_perm(d, b, 0x05040100);
-    out[3] = __builtin_amdgcn_perm(d, b, 0x07060302);
-}
 
 template <int DH>
 struct TileData {
@@ -414,7 +364,7 @@ __global__ __launch_bounds__(kThreads) void attn_join_kernel(AttnParams p)
     static constexpr int kTile = tile_keys(DH);
     const int b = blockIdx.y, unit = blockIdx.x, tid = threadIdx.x;
     const Seq sq = load_seq(p, b);
-    if (sq.n == 0 || unit >= ceil_div(sq.n * p.group, 16) * p.n_kv_heads) return;
+    if (sq.n == 0 || sq.n * p.group > p.few_rows || unit >= ceil_div(sq.n * p.group, 16) * p.n_kv_heads) return;
     int first, count;
     seq_range(p, sq, kTile, first, count);
     const int64_t per = tiles_per_block(p.seq_tiles[p.B], p.n_blocks);
@@ -464,7 +414,7 @@ int launch_as(const AttnParams &p, hipStream_t s)
         MOE_LAUNCH_CHECK("attn_decode_kernel");
     }
     ProfScope ps("attn_join", s);
-    const int units = ceil_div(p.max_q * p.group, 16) * p.n_kv_heads;
+    const int units = ceil_div((int)((int64_t)p.max_q * p.group < p.few_rows ? (int64_t)p.max_q * p.group : p.few_rows), 16) * p.n_kv_heads;
     hipLaunchKernelGGL((attn_join_kernel<DH, NS>), dim3(units, p.B), dim3(kThreads), 0, s, p);
     MOE_LAUNCH_CHECK("attn_join_kernel");
     return MOE_OK;
@@ -474,10 +424,10 @@ int decode_blocks(int num_cus) { return 2 * num_cus; }
 
 }  // namespace
 
-// partial results of two units a block, then the sequences' places among the tiles
-int64_t attn_decode_workspace(int head_dim, int B_max, int num_cus)
+// partial results of two units a block
+int64_t attn_decode_workspace(int head_dim, int num_cus)
 {
-    return align_up((int64_t)decode_blocks(num_cus) * 2 * (16 * head_dim + 32) * 4, 256) + align_up((int64_t)(B_max + 1) * 8, 256);
+    return align_up((int64_t)decode_blocks(num_cus) * 2 * (16 * head_dim + 32) * 4, 256);
 }
 
 int launch_attn_decode(int dtype, int head_dim, AttnParams p, int num_cus, hipStream_t s)

@@ -30,6 +30,7 @@ struct AttnParams {
     float *part;
     int64_t *seq_tiles;
     int n_blocks;
+    int few_rows;                          // sequences of up to so many rows (new tokens times group) are the decode kernel's
 };
 
 // A sequence's new tokens and length, clamped to what can exist, so that no index derived from them leaves its array.
@@ -56,6 +57,8 @@ struct AppendParams {
 
 int launch_kv_append(int dtype, int head_dim, const AppendParams &p, int num_cus, hipStream_t s);
 int launch_attn_decode(int dtype, int head_dim, AttnParams p, int num_cus, hipStream_t s);
-int64_t attn_decode_workspace(int head_dim, int B_max, int num_cus);
+int64_t attn_decode_workspace(int head_dim, int num_cus);
+int launch_attn_prefill(int dtype, int head_dim, const AttnParams &p, int num_cus, hipStream_t s);
+int64_t attn_prefill_workspace(int head_dim, int num_cus);
 
 }  // namespace moe355

@@ -1,0 +1,447 @@
+// Attention over a paged e4m3 cache for many query rows per key head (prefill, chunks of it, cross attention).
+//
+// A block owns 32 W query rows (new tokens x heads of a group) of a (sequence, key head), a wave 32 of them, and walks tiles of 64
+// keys with a running maximum and sum.  Keys and values are widened to bf16 once for the block on their way into LDS:
+//   K    [64 keys][DH], V^T [DH][64 keys], 16-byte chunks swizzled so that 16 lanes that read a fragment, and 16 that write, meet each
+//        bank once (V's writes: twice); two buffers, the next tile's bytes are in flight while this one is computed
+//   S^T = K Q^T and O^T = V^T P^T by 32x32x16 MFMAs; queries stay in registers.  A lane holds 4 keys in 8 of one query; a chunk of
+//        V^T holds just those keys in just that order, so the weights are the second product's operand where the first left them.
+// The maximum, the sum and the rescaling of a query are its lane's own; two lanes share a query.  Scales cost nothing: a key's scale is
+// part of the factor in front of the exponent, a value's of its offset (weights 2^(s - m + log2 v_scale)), taken out of the sum per 16
+// keys.  The output is rescaled only where the maximum has grown by more than 8 (a factor of 256 on the weights, which fp32 and bf16
+// both hold), for most tiles not at all.
+//
+// Bound by the matrix cores and the exponentials (a quarter of the rate of other instructions) in about equal parts: per 32 x 64 weights
+// and wave 32 MFMAs of 32 cycles, 32 exponentials of 16 and some 110 others of 4.  Two waves a SIMD overlap them.
+//
+// Blocks begin with the last rows, which see the most keys; a sequence's heads stay on one XCD and its L2.  Where there are too few
+// blocks for the chip, the keys are cut into parts, joined by a second kernel.
+#include "attn_dev.h"
+
+#include <mutex>
+
+namespace moe355 {
+
+namespace {
+
+static constexpr int kTile = 64;
+static constexpr float kLeast = 1.17549435e-38f;  // factors stay normal numbers: 0 times a masked score's infinity is none
+
+struct PrefillParams {
+    AttnParams a;
+    int row_tiles, splits;  // bounds for all sequences
+};
+
+struct GroupInfo {          // of 16 keys
+    float key_scale;        // times scale * log2(e)
+    float value_log2;       // log2 of the values' scale
+    float value_inverse;
+    int held;
+};
+
+template <int DH>
+struct Buffer {
+    uint16_t k[kTile * DH];
+    uint16_t v[DH * kTile];
+    GroupInfo info[4];
+};
+
+template <int DH>
+__device__ __forceinline__ int k_at(int row, int chunk)  // element of a 16-byte chunk of K
+{
+    return row * DH + (DH == 64 ? chunk ^ ((row >> 1) & 7) : chunk ^ (row & 15)) * 8;
+}
+__device__ __forceinline__ int v_at(int dim, int chunk)
+{
+    return dim * kTile + (chunk ^ ((dim >> 1) & 7) ^ ((dim >> 4) & 1)) * 8;
+}
+
+// The tiles of keys that rows [row0, row0 + rows) of a sequence see: first, count.
+__device__ __forceinline__ void tile_range(const AttnParams &p, const Seq &sq, int row0, int rows, int &first, int &count)
+{
+    const int tok0 = row0 / p.group, tok1 = min((row0 + rows - 1) / p.group, sq.n - 1);
+    const int pos0 = sq.kv - sq.n + tok0, pos1 = sq.kv - sq.n + tok1;
+    const int end = p.causal ? min(sq.kv, max(pos1 + 1, 0)) : sq.kv;
+    const int begin = p.window > 0 ? min(max(0, pos0 - p.window + 1), end) : 0;
+    first = begin / kTile;
+    count = ceil_div(end, kTile) - first;
+}
+
+// A partial result: the rows' outputs (not divided by the sum), maxima, sums
+template <int DH, int W>
+constexpr int64_t part_floats() { return (int64_t)32 * W * (DH + 2); }
+
+template <int DH, int NS, int W>
+__global__ __launch_bounds__(64 * W, W == 8 ? 2 : 1) void attn_prefill_kernel(PrefillParams pp)
+{
+    static constexpr int kThreads = 64 * W, kRows = 32 * W, kRole = kThreads / 2;
+    static constexpr int kKItems = (4 * DH + kRole - 1) / kRole;  // 16 bytes of a key each
+    static constexpr int kVItems = (2 * DH + kRole - 1) / kRole;  // 4 dimensions of 8 values each
+    static constexpr int kWords = kKItems * 4 > kVItems * 8 ? kKItems * 4 : kVItems * 8;
+    static constexpr int kSteps = DH / 16, kCols = DH / 32;
+    extern __shared__ __align__(16) uint8_t lds[];
+    Buffer<DH> *buffer = reinterpret_cast<Buffer<DH> *>(lds);
+    const AttnParams &p = pp.a;
+    const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int l31 = lane & 31, half = lane >> 5;
+
+    const int per_tile = p.B * p.n_kv_heads * pp.splits;
+    const int rt = pp.row_tiles - 1 - (int)blockIdx.x / per_tile;
+    const int rest = (int)blockIdx.x % per_tile;
+    const int part = rest % pp.splits, h = rest / pp.splits % p.n_kv_heads, b = rest / pp.splits / p.n_kv_heads;
+    const Seq sq = load_seq(p, b);
+    if (sq.n * p.group <= p.few_rows || rt * kRows >= sq.n * p.group) return;
+    int first, count;
+    tile_range(p, sq, rt * kRows, kRows, first, count);
+    if (pp.splits > 1) {
+        const int each = ceil_div(count, pp.splits);
+        first += part * each;
+        count = min(each, max(0, count - part * each));
+    }
+    const int32_t *table = p.page_table + (int64_t)b * p.max_pages;
+
+    const int r = rt * kRows + w * 32 + l31;
+    const int tok = r / p.group, head = h * p.group + (r - tok * p.group);
+    const bool live = tok < sq.n;
+    const int pos = sq.kv - sq.n + tok;
+    const int key_end = !live ? 0 : p.causal ? min(pos + 1, sq.kv) : sq.kv;
+    const int key_begin = p.window > 0 ? max(0, pos - p.window + 1) : 0;
+    // over the wave's rows: keys that all see, and that any sees
+    int all_begin = live ? key_begin : 0, all_end = live ? key_end : 0x7fffffff;
+    int any_begin = live ? key_begin : 0x7fffffff, any_end = key_end;
+#pragma unroll
+    for (int off = 16; off >= 1; off >>= 1) {
+        all_begin = max(all_begin, __shfl_xor(all_begin, off, 64));
+        all_end = min(all_end, __shfl_xor(all_end, off, 64));
+        any_begin = min(any_begin, __shfl_xor(any_begin, off, 64));
+        any_end = max(any_end, __shfl_xor(any_end, off, 64));
+    }
+    all_begin = __builtin_amdgcn_readfirstlane(all_begin);
+    all_end = min(__builtin_amdgcn_readfirstlane(all_end), sq.kv);
+    any_begin = __builtin_amdgcn_readfirstlane(any_begin);
+    any_end = __builtin_amdgcn_readfirstlane(any_end);
+
+    // queries; a negative scale is theirs, so that the factor in front of the exponent is positive
+    const bool negative = p.scale_log2e < 0.f;
+    const float scale = fmaxf(fabsf(p.scale_log2e), 1e-30f);
+    Pieces<NS> q[kSteps];
+#pragma unroll
+    for (int s = 0; s < kSteps; ++s) {
+        const int64_t at = (int64_t)(sq.first + tok) * p.q_stride + (int64_t)head * DH + 16 * s + 8 * half;
+        if (NS == 1) {
+            uint4 x = make_uint4(0, 0, 0, 0);
+            if (live) x = *reinterpret_cast<const uint4 *>(static_cast<const uint16_t *>(p.q) + at);
+            if (negative) x = make_uint4(x.x ^ 0x80008000u, x.y ^ 0x80008000u, x.z ^ 0x80008000u, x.w ^ 0x80008000u);
+            q[s].x[0] = __builtin_bit_cast(bf16x8, x);
+        } else {
+            float x[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+            if (live) {
+                const float4 lo = *reinterpret_cast<const float4 *>(static_cast<const float *>(p.q) + at);
+                const float4 hi = *reinterpret_cast<const float4 *>(static_cast<const float *>(p.q) + at + 4);
+                x[0] = lo.x, x[1] = lo.y, x[2] = lo.z, x[3] = lo.w, x[4] = hi.x, x[5] = hi.y, x[6] = hi.z, x[7] = hi.w;
+            }
+            if (negative)
+#pragma unroll
+                for (int i = 0; i < 8; ++i) x[i] = -x[i];
+            q[s] = split<NS>(x);
+        }
+    }
+
+    // staging: the first half of the waves brings keys, the other values
+    const bool brings_k = w < W / 2;
+    const int role = brings_k ? tid : tid - kRole;
+    const int page_mask = (1 << p.page_shift) - 1;
+    uint32_t words[kWords];
+    int page[kKItems > kVItems ? kKItems : kVItems], info_page = -1;
+    const auto page_of = [&](int key) { return key < sq.kv ? table[key >> p.page_shift] : -1; };
+    const auto look_up = [&](int key0) {  // the pages of a tile, a tile ahead of its bytes
+        if (brings_k) {
+#pragma unroll
+            for (int i = 0; i < kKItems; ++i) page[i] = page_of(key0 + min((i * kRole + role) / (DH / 16), kTile - 1));
+        } else {
+#pragma unroll
+            for (int i = 0; i < kVItems; ++i) page[i] = page_of(key0 + 16 * (min((i * kRole + role) / (DH / 4), 7) >> 1));
+        }
+        if (tid < 4) info_page = page_of(key0 + 16 * tid);
+    };
+    float info_k = 1.f, info_v = 1.f;
+    bool info_held = false;
+    const auto load = [&](int key0) {
+        if (brings_k) {
+#pragma unroll
+            for (int i = 0; i < kKItems; ++i) {
+                const int item = i * kRole + role, row = item / (DH / 16), c = item - row * (DH / 16);
+                const bool there = row < kTile && key0 + row < sq.kv && page[i] >= 0 && page[i] < p.num_pages;
+                uint4 x = make_uint4(0, 0, 0, 0);
+                if (there)
+                    x = *reinterpret_cast<const uint4 *>(
+                        p.k + ((((int64_t)page[i] * p.n_kv_heads + h) << p.page_shift) + ((key0 + row) & page_mask)) * DH + 16 * c);
+                words[4 * i] = x.x, words[4 * i + 1] = x.y, words[4 * i + 2] = x.z, words[4 * i + 3] = x.w;
+            }
+        } else {
+#pragma unroll
+            for (int i = 0; i < kVItems; ++i) {
+                const int item = i * kRole + role, c = item / (DH / 4), quad = item - c * (DH / 4);
+                const int row0 = 16 * (c >> 1) + 4 * (c & 1);
+                const bool held = c < 8 && page[i] >= 0 && page[i] < p.num_pages;
+                const uint8_t *src = p.v + ((((int64_t)(held ? page[i] : 0) * p.n_kv_heads + h) << p.page_shift) + ((key0 + row0) & page_mask)) * DH + 4 * quad;
+#pragma unroll
+                for (int j = 0; j < 8; ++j) {
+                    const int row = (j & 3) + 8 * (j >> 2);
+                    words[8 * i + j] = held && key0 + row0 + row < sq.kv ? *reinterpret_cast<const uint32_t *>(src + row * DH) : 0u;
+                }
+            }
+        }
+        if (tid < 4) {
+            info_held = info_page >= 0 && info_page < p.num_pages;
+            const int64_t unit = (int64_t)(info_held ? info_page : 0) * p.n_kv_heads + h;
+            info_k = info_held ? p.k_scale[unit] : 1.f;
+            info_v = info_held ? p.v_scale[unit] : 1.f;
+        }
+    };
+    const auto store = [&](Buffer<DH> &to) {
+        if (brings_k) {
+#pragma unroll
+            for (int i = 0; i < kKItems; ++i) {
+                const int item = i * kRole + role, row = item / (DH / 16), c = item - row * (DH / 16);
+                if (row >= kTile) continue;
+                *reinterpret_cast<bf16x8 *>(to.k + k_at<DH>(row, 2 * c)) = widen(words[4 * i], words[4 * i + 1]);
+                *reinterpret_cast<bf16x8 *>(to.k + k_at<DH>(row, 2 * c + 1)) = widen(words[4 * i + 2], words[4 * i + 3]);
+            }
+        } else {
+#pragma unroll
+            for (int i = 0; i < kVItems; ++i) {
+                const int item = i * kRole + role, c = item / (DH / 4), quad = item - c * (DH / 4);
+                if (c >= 8) continue;
+                uint32_t lo[4], hi[4];
+                transpose4(words[8 * i], words[8 * i + 1], words[8 * i + 2], words[8 * i + 3], lo);
+                transpose4(words[8 * i + 4], words[8 * i + 5], words[8 * i + 6], words[8 * i + 7], hi);
+#pragma unroll
+                for (int y = 0; y < 4; ++y) *reinterpret_cast<bf16x8 *>(to.v + v_at(4 * quad + y, c)) = widen(lo[y], hi[y]);
+            }
+        }
+        if (tid < 4) to.info[tid] = {fmaxf(info_k * scale, kLeast), log2f(fmaxf(info_v, kLeast)), 1.f / fmaxf(info_v, kLeast), info_held};
+    };
+
+    f32x16 o[kCols];
+#pragma unroll
+    for (int c = 0; c < kCols; ++c)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) o[c][i] = 0.f;
+    float m = -INFINITY, l = 0.f;
+
+    if (count > 0) {
+        look_up(first * kTile);
+        load(first * kTile);
+        look_up((first + 1) * kTile);
+        store(buffer[0]);
+        __syncthreads();
+    }
+    for (int t = 0; t < count; ++t) {
+        const int key0 = (first + t) * kTile;
+        if (t + 1 < count) {
+            load(key0 + kTile);
+            look_up(key0 + 2 * kTile);
+        }
+        const Buffer<DH> &buf = buffer[t & 1];
+        if (key0 < any_end && key0 + kTile > any_begin) {
+            f32x16 s[2];
+#pragma unroll
+            for (int n = 0; n < 2; ++n)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) s[n][i] = 0.f;
+#pragma unroll
+            for (int x = 0; x < kSteps; ++x)
+#pragma unroll
+                for (int n = 0; n < 2; ++n) {
+                    const bf16x8 key = *reinterpret_cast<const bf16x8 *>(buf.k + k_at<DH>(32 * n + l31, 2 * x + half));
+#pragma unroll
+                    for (int i = 0; i < NS; ++i) s[n] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(key, q[x].x[i], s[n], 0, 0, 0);
+                }
+            GroupInfo info[4];
+            bool whole = key0 >= all_begin && key0 + kTile <= all_end;
+#pragma unroll
+            for (int g = 0; g < 4; ++g) {
+                info[g] = buf.info[g];
+                whole = whole && __builtin_amdgcn_readfirstlane(info[g].held);
+            }
+            if (!whole) {
+#pragma unroll
+                for (int n = 0; n < 2; ++n)
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) {
+                        const int key = key0 + 32 * n + 8 * (i >> 2) + 4 * half + (i & 3);
+                        s[n][i] = info[2 * n + (i >> 3)].held && key >= key_begin && key < key_end ? s[n][i] : -INFINITY;
+                    }
+            }
+            float top = -INFINITY;
+#pragma unroll
+            for (int g = 0; g < 4; ++g) {
+                float most = s[g >> 1][8 * (g & 1)];
+#pragma unroll
+                for (int i = 1; i < 8; ++i) most = fmaxf(most, s[g >> 1][8 * (g & 1) + i]);
+                top = fmaxf(top, most * info[g].key_scale);
+            }
+            top = fmaxf(top, __shfl_xor(top, 32, 64));
+            if (__any(top > m + 8.f)) {  // m is -infinity until a row has seen a key
+                const float m_new = fmaxf(m, top);
+                const float alpha = m_new == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m - m_new);
+                m = m_new;
+                l *= alpha;
+#pragma unroll
+                for (int c = 0; c < kCols; ++c)
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) o[c][i] *= alpha;
+            }
+            const float base = m == -INFINITY ? 0.f : m;
+#pragma unroll
+            for (int g = 0; g < 4; ++g) {
+                const float offset = info[g].value_log2 - base;
+                float weight[8], sum = 0.f;
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    weight[i] = __builtin_amdgcn_exp2f(fmaf(s[g >> 1][8 * (g & 1) + i], info[g].key_scale, offset));
+                    sum += weight[i];
+                }
+                l = fmaf(sum, info[g].value_inverse, l);
+                const Pieces<NS> wp = split<NS>(weight);
+#pragma unroll
+                for (int c = 0; c < kCols; ++c) {
+                    const bf16x8 value = *reinterpret_cast<const bf16x8 *>(buf.v + v_at(32 * c + l31, 2 * g + half));
+#pragma unroll
+                    for (int i = 0; i < NS; ++i) o[c] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(value, wp.x[i], o[c], 0, 0, 0);
+                }
+            }
+        }
+        if (t + 1 < count) store(buffer[(t + 1) & 1]);
+        __syncthreads();
+    }
+    l += __shfl_xor(l, 32, 64);
+    // o[c][i] of a lane is dimension 32 c + 8 (i / 4) + 4 half + i % 4 of its query
+    if (pp.splits > 1) {
+        const int64_t slot = ((int64_t)rt * p.B * p.n_kv_heads + (int64_t)b * p.n_kv_heads + h) * pp.splits + part;
+        float *to = p.part + slot * part_floats<DH, W>();
+        const int row = w * 32 + l31;
+#pragma unroll
+        for (int c = 0; c < kCols; ++c)
+#pragma unroll
+            for (int i = 0; i < 16; i += 4)
+                *reinterpret_cast<float4 *>(to + (int64_t)row * DH + 32 * c + 2 * i + 4 * half) = make_float4(o[c][i], o[c][i + 1], o[c][i + 2], o[c][i + 3]);
+        if (half == 0) {
+            to[(int64_t)kRows * DH + row] = m;
+            to[(int64_t)kRows * DH + kRows + row] = l;
+        }
+        return;
+    }
+    if (!live) return;
+    const int64_t at = (int64_t)(sq.first + tok) * p.n_heads + head;
+    const float inv = l > 0.f ? 1.f / l : 0.f;
+#pragma unroll
+    for (int c = 0; c < kCols; ++c)
+#pragma unroll
+        for (int i = 0; i < 16; i += 4) {
+            const int64_t dim = at * DH + 32 * c + 2 * i + 4 * half;
+            if (NS == 1)
+                *reinterpret_cast<uint2 *>(static_cast<uint16_t *>(p.out) + dim) =
+                    make_uint2(pack_bf16(o[c][i] * inv, o[c][i + 1] * inv), pack_bf16(o[c][i + 2] * inv, o[c][i + 3] * inv));
+            else
+                *reinterpret_cast<float4 *>(static_cast<float *>(p.out) + dim) = make_float4(o[c][i] * inv, o[c][i + 1] * inv, o[c][i + 2] * inv, o[c][i + 3] * inv);
+        }
+    if (half == 0 && p.lse) p.lse[at] = l > 0.f ? m * kLn2 + logf(l) : -INFINITY;
+}
+
+// Joins the parts of the keys: a block per 16 rows of a unit.
+template <int DH, int NS, int W>
+__global__ __launch_bounds__(256) void attn_prefill_join_kernel(PrefillParams pp)
+{
+    static constexpr int kRows = 32 * W, kPieces = kRows / 16;
+    const AttnParams &p = pp.a;
+    const int piece = blockIdx.x % kPieces, unit = blockIdx.x / kPieces;
+    const int h = unit % p.n_kv_heads, b = unit / p.n_kv_heads % p.B, rt = unit / p.n_kv_heads / p.B;
+    const Seq sq = load_seq(p, b);
+    if (sq.n * p.group <= p.few_rows) return;
+    for (int e = threadIdx.x * 4; e < 16 * DH; e += 256 * 4) {
+        const int row = piece * 16 + e / DH, dim = e % DH, r = rt * kRows + row, tok = r / p.group;
+        if (tok >= sq.n) continue;
+        float top = -INFINITY, l = 0.f;
+        float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
+        for (int k = 0; k < pp.splits; ++k) {
+            const float *part = p.part + ((int64_t)unit * pp.splits + k) * part_floats<DH, W>();
+            const float pm = part[(int64_t)kRows * DH + row], pl = part[(int64_t)kRows * DH + kRows + row];
+            const float4 x = *reinterpret_cast<const float4 *>(part + (int64_t)row * DH + dim);
+            const float m_new = fmaxf(top, pm), base = m_new == -INFINITY ? 0.f : m_new;
+            const float keep = __builtin_amdgcn_exp2f(top - base), add = __builtin_amdgcn_exp2f(pm - base);
+            top = m_new;
+            l = l * keep + pl * add;
+            sum.x = sum.x * keep + x.x * add;
+            sum.y = sum.y * keep + x.y * add;
+            sum.z = sum.z * keep + x.z * add;
+            sum.w = sum.w * keep + x.w * add;
+        }
+        const int64_t at = (int64_t)(sq.first + tok) * p.n_heads + h * p.group + (r - tok * p.group);
+        const float inv = l > 0.f ? 1.f / l : 0.f;
+        if (NS == 1)
+            *reinterpret_cast<uint2 *>(static_cast<uint16_t *>(p.out) + at * DH + dim) =
+                make_uint2(pack_bf16(sum.x * inv, sum.y * inv), pack_bf16(sum.z * inv, sum.w * inv));
+        else
+            *reinterpret_cast<float4 *>(static_cast<float *>(p.out) + at * DH + dim) = make_float4(sum.x * inv, sum.y * inv, sum.z * inv, sum.w * inv);
+        if (dim == 0 && p.lse) p.lse[at] = l > 0.f ? top * kLn2 + logf(l) : -INFINITY;
+    }
+}
+
+// Parts of the keys: none where the units give every CU two blocks; else so many that they do.  (part buffers: 2 a CU)
+int splits_for(int64_t units, int num_cus) { return units >= 2 * num_cus ? 1 : (int)(2 * num_cus / units); }
+
+template <int DH, int NS, int W>
+int launch_as(PrefillParams pp, int num_cus, hipStream_t s)
+{
+    static constexpr size_t kLds = 2 * sizeof(Buffer<DH>);
+    static std::once_flag once;
+    static hipError_t setup_rc = hipSuccess;
+    std::call_once(once, [&]() {
+        setup_rc = hipFuncSetAttribute(reinterpret_cast<const void *>(attn_prefill_kernel<DH, NS, W>), hipFuncAttributeMaxDynamicSharedMemorySize, (int)kLds);
+    });
+    MOE_HIP_CHECK(setup_rc);
+    const AttnParams &p = pp.a;
+    pp.row_tiles = (int)(((int64_t)p.max_q * p.group + 32 * W - 1) / (32 * W));
+    const int64_t units = (int64_t)pp.row_tiles * p.B * p.n_kv_heads;
+    const int most = ceil_div(p.max_kv, kTile) > 0 ? ceil_div(p.max_kv, kTile) : 1;
+    pp.splits = splits_for(units, num_cus);
+    pp.splits = pp.splits < most ? pp.splits : most;
+    if (units * pp.splits >= 1ll << 31) {
+        set_error("moe_attn_forward: %lld blocks", (long long)units);
+        return MOE_ERR_INVALID_ARG;
+    }
+    {
+        ProfScope ps("attn_prefill", s);
+        hipLaunchKernelGGL((attn_prefill_kernel<DH, NS, W>), dim3((unsigned)(units * pp.splits)), dim3(64 * W), kLds, s, pp);
+        MOE_LAUNCH_CHECK("attn_prefill_kernel");
+    }
+    if (pp.splits > 1) {
+        ProfScope ps("attn_prefill_join", s);
+        hipLaunchKernelGGL((attn_prefill_join_kernel<DH, NS, W>), dim3((unsigned)(units * 2 * W)), dim3(256), 0, s, pp);
+        MOE_LAUNCH_CHECK("attn_prefill_join_kernel");
+    }
+    return MOE_OK;
+}
+
+}  // namespace
+
+int64_t attn_prefill_workspace(int head_dim, int num_cus)
+{
+    const int w = head_dim <= 128 ? 8 : 4;
+    return align_up((int64_t)2 * num_cus * 32 * w * (head_dim + 2) * 4, 256);
+}
+
+// p.part: attn_prefill_workspace() bytes
+int launch_attn_prefill(int dtype, int head_dim, const AttnParams &p, int num_cus, hipStream_t s)
+{
+    const PrefillParams pp = {p, 0, 1};
+    const bool bf = dtype == MOE_DTYPE_BF16;
+    // rows of 256 and two waves a SIMD; fp32 and 256 dimensions need the registers of both
+    if (head_dim == 64) return bf ? launch_as<64, 1, 8>(pp, num_cus, s) : launch_as<64, 3, 4>(pp, num_cus, s);
+    if (head_dim == 128) return bf ? launch_as<128, 1, 8>(pp, num_cus, s) : launch_as<128, 3, 4>(pp, num_cus, s);
+    return bf ? launch_as<256, 1, 4>(pp, num_cus, s) : launch_as<256, 3, 4>(pp, num_cus, s);
+}
+
+}  // namespace moe355
