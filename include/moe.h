@@ -406,7 +406,7 @@ typedef struct moe_kv_cache {
  * pages in the cache; 1 <= max_pages pages of a sequence with max_pages * page_size < 2^30; rot_dim rotated dimensions
  * of a head: 0 or a multiple of 16 up to head_dim. */
 #define MOE_ATTN_MAX_HEADS 256
-#define MOE_ATTN_MAX_B 4096
+#define MOE_ATTN_MAX_B 2048
 typedef struct moe_attn_config {
     int32_t B_max;
     int32_t T_max;

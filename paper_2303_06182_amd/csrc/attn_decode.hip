@@ -12,9 +12,14 @@
 // exactly, so nothing else is lost.
 //
 // Bound by HBM: 2 DH bytes a key, at 16 columns 32 MFMAs of 16 cycles per 16 KB and SIMD, far below.  Split: the tiles of all
-// (sequence, rows, head) units lie in one row and every block takes the same number of them, whatever the lengths are; a unit
-// that several blocks share leaves partial results that a second kernel joins.
+// (sequence, rows, head) units lie in one row; every block takes the same number of them, whatever the lengths are, and every wave
+// a quarter of the block's.  A wave works alone until its tiles are done: units that lie inside its part are written at once, the one
+// or two that do not are left in LDS, where the block joins them; what reaches past the block is joined by a second kernel.
+// (With the waves of a block on one unit at a time, joined after each, short sequences cost a block 8 us a unit: 32 sequences of up to
+// 1111 keys, 16 heads of 64, fp32 41 us.)
 #include "attn_dev.h"
+
+#include <mutex>
 
 namespace moe355 {
 
@@ -127,36 +132,70 @@ __device__ __forceinline__ void load_tile(const AttnParams &p, const int32_t *ta
     }
 }
 
-// DH: head dimension; NS: bf16 pieces of an fp32 number (1: bf16 queries and weights rounded once)
-template <int DH, int NS>
-__global__ __launch_bounds__(kThreads, 2) void attn_decode_kernel(AttnParams p)
+// What a wave (or a block, in memory) has of a unit that it shares: 16 rows of DH outputs (not divided by the sum), the 16 maxima, the 16
+// sums.  In LDS the rows are 4 floats further apart, so that the 16 lanes that write a dimension each meet other banks.
+struct Piece {
+    int64_t unit_begin;  // first tile of the unit, -1: nothing here
+    int b, unit, run, count;
+};
+template <int DH>
+struct Shared {
+    static constexpr int kRow = DH + 4;
+    Piece piece[kWaves][2];
+    float m[kWaves][2][16], l[kWaves][2][16];
+    int64_t wave_sum[kWaves];
+    float o[kWaves][2][16 * kRow];
+};
+
+// four outputs of a row, from dimension dim on
+template <int NS>
+__device__ __forceinline__ void store_out(const AttnParams &p, int64_t at, float4 x)
+{
+    if (NS == 1)
+        *reinterpret_cast<uint2 *>(static_cast<uint16_t *>(p.out) + at) = make_uint2(pack_bf16(x.x, x.y), pack_bf16(x.z, x.w));
+    else
+        *reinterpret_cast<float4 *>(static_cast<float *>(p.out) + at) = x;
+}
+
+// The unit `unit` of a sequence: its rows' tile and its key head; a row's output begins at element row_out() * DH, -1: there is no such row
+__device__ __forceinline__ int64_t row_out(const AttnParams &p, const Seq &sq, int unit, int row)
+{
+    const int rt = unit / p.n_kv_heads, h = unit - rt * p.n_kv_heads;
+    const int r = rt * 16 + row, tok = r / p.group;
+    return tok < sq.n ? (int64_t)(sq.first + tok) * p.n_heads + h * p.group + (r - tok * p.group) : -1;
+}
+
+// DH: head dimension; NS: bf16 pieces of an fp32 number (1: bf16 queries and weights rounded once); M: blocks a CU holds
+template <int DH, int NS, int M>
+__global__ __launch_bounds__(kThreads, M) void attn_decode_kernel(AttnParams p)
 {
     static constexpr int kTile = tile_keys(DH), kBlocks = kTile / 16, kChunks = DH / 64, kCols = DH / 16, kWords = DH / 64;
+    static constexpr int kRow = Shared<DH>::kRow;
     extern __shared__ __align__(16) uint8_t lds[];
-    float *merge = reinterpret_cast<float *>(lds);                                       // [waves][16][DH]
-    float *merge_m = merge + kWaves * 16 * DH, *merge_l = merge_m + kWaves * 16;           // [waves][16]
-    int64_t *wave_sum = reinterpret_cast<int64_t *>(merge_l + kWaves * 16);                // [waves]
-    int64_t *begin = wave_sum + kWaves;                                                    // [B + 1]
+    Shared<DH> &sh = *reinterpret_cast<Shared<DH> *>(lds);
+    int64_t *begin = reinterpret_cast<int64_t *>(lds + sizeof(Shared<DH>));  // [B + 1]
     const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int l15 = lane & 15, g = lane >> 4;
 
-    scan_sequences(p, kTile, begin, wave_sum);
+    if (tid < 2 * kWaves) sh.piece[tid >> 1][tid & 1].unit_begin = -1;
+    scan_sequences(p, kTile, begin, sh.wave_sum);
     const int64_t total = begin[p.B], per = tiles_per_block(total, p.n_blocks);
-    if (blockIdx.x == 0 && p.seq_tiles)  // for the kernel that joins
+    if (blockIdx.x == 0)  // for the kernel that joins
         for (int b = tid; b <= p.B; b += kThreads) p.seq_tiles[b] = begin[b];
     const int64_t t_begin = (int64_t)blockIdx.x * per, t_end = min(total, t_begin + per);
     if (t_begin >= t_end) return;
+    const int64_t w_begin = t_begin + w * (per / kWaves), w_end = min(t_end, w_begin + per / kWaves);
     int b = 0;
-    {   // the sequence that holds t_begin: the last one that begins at or before it
+    if (w_begin < w_end) {  // the sequence that holds w_begin: the last one that begins at or before it
         int lo = 0, hi = p.B;
         while (hi - lo > 1) {
             const int mid = (lo + hi) >> 1;
-            if (begin[mid] <= t_begin) lo = mid;
+            if (begin[mid] <= w_begin) lo = mid;
             else hi = mid;
         }
         b = lo;
     }
-    for (int64_t t = t_begin; t < t_end;) {
+    for (int64_t t = w_begin; t < w_end;) {
         while (begin[b + 1] <= t) ++b;
         const int bu = __builtin_amdgcn_readfirstlane(b);
         const Seq sq = load_seq(p, bu);
@@ -164,9 +203,12 @@ __global__ __launch_bounds__(kThreads, 2) void attn_decode_kernel(AttnParams p)
         seq_range(p, sq, kTile, first, count);
         const int local = (int)(t - begin[bu]);
         const int unit = __builtin_amdgcn_readfirstlane(local / count), tile0 = __builtin_amdgcn_readfirstlane(local - unit * count);
-        const int run = __builtin_amdgcn_readfirstlane((int)min(t_end - t, (int64_t)(count - tile0)));
+        const int run = __builtin_amdgcn_readfirstlane((int)min(w_end - t, (int64_t)(count - tile0)));
         const int rt = unit / p.n_kv_heads, h = unit - rt * p.n_kv_heads;
         const int32_t *table = p.page_table + (int64_t)bu * p.max_pages;
+
+        TileData<DH> d, next;
+        load_tile<DH>(p, table, sq.kv, h, (first + tile0) * kTile, lane, next);
 
         // this lane's query: row r of the sequence's n * group rows
         const int r = rt * 16 + l15;
@@ -210,14 +252,10 @@ __global__ __launch_bounds__(kThreads, 2) void attn_decode_kernel(AttnParams p)
         all_begin = __builtin_amdgcn_readfirstlane(all_begin);
         all_end = min(__builtin_amdgcn_readfirstlane(all_end), sq.kv);
 
-        TileData<DH> d, next;
-        int tile = tile0 + w;
-        const int tile_end = tile0 + run;
-        if (tile < tile_end) load_tile<DH>(p, table, sq.kv, h, (first + tile) * kTile, lane, next);
-        for (; tile < tile_end; tile += kWaves) {
+        for (int tile = tile0; tile < tile0 + run; ++tile) {
             d = next;
             const int key0 = (first + tile) * kTile;
-            if (tile + kWaves < tile_end) load_tile<DH>(p, table, sq.kv, h, key0 + kWaves * kTile, lane, next);
+            if (tile + 1 < tile0 + run) load_tile<DH>(p, table, sq.kv, h, key0 + kTile, lane, next);
             f32x4 s[kBlocks];
             bool whole = key0 >= all_begin && key0 + kTile <= all_end;
 #pragma unroll
@@ -298,145 +336,177 @@ __global__ __launch_bounds__(kThreads, 2) void attn_decode_kernel(AttnParams p)
         l += __shfl_xor(l, 16, 64);
         l += __shfl_xor(l, 32, 64);
 
-        // join the waves: o[c][i] of a lane is dimension kCols * (4 g + i) + c of query row l15
-        if (g == 0) {
-            merge_m[w * 16 + l15] = m;
-            merge_l[w * 16 + l15] = l;
+        // o[c][i] of a lane is dimension kCols * (4 g + i) + c of query row l15
+        if (run == count) {
+            const int64_t at = row_out(p, sq, unit, l15);
+            const float inv = l > 0.f ? 1.f / l : 0.f;
+            if (at >= 0) {
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+#pragma unroll
+                    for (int c = 0; c < kCols; c += 4)
+                        store_out<NS>(p, at * DH + kCols * (4 * g + i) + c, make_float4(o[c][i] * inv, o[c + 1][i] * inv, o[c + 2][i] * inv, o[c + 3][i] * inv));
+                if (g == 0 && p.lse) p.lse[at] = l > 0.f ? m * kLn2 + logf(l) : -INFINITY;
+            }
+        } else {
+            const int slot = t == w_begin ? 0 : 1;
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+#pragma unroll
+                for (int c = 0; c < kCols; c += 4)
+                    *reinterpret_cast<float4 *>(sh.o[w][slot] + l15 * kRow + kCols * (4 * g + i) + c) = make_float4(o[c][i], o[c + 1][i], o[c + 2][i], o[c + 3][i]);
+            if (g == 0) {
+                sh.m[w][slot][l15] = m;
+                sh.l[w][slot][l15] = l;
+            }
+            if (lane == 0) sh.piece[w][slot] = {begin[bu] + (int64_t)unit * count, bu, unit, run, count};
         }
-        __syncthreads();
-        float top = -INFINITY;
-#pragma unroll
-        for (int i = 0; i < kWaves; ++i) top = fmaxf(top, merge_m[i * 16 + l15]);
-        const float mine = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - top);
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-#pragma unroll
-            for (int c = 0; c < kCols; c += 4)
-                *reinterpret_cast<float4 *>(merge + (w * 16 + l15) * DH + kCols * (4 * g + i) + c) =
-                    make_float4(o[c][i] * mine, o[c + 1][i] * mine, o[c + 2][i] * mine, o[c + 3][i] * mine);
-        __syncthreads();
-        const bool all = run == count;
-        float *part = nullptr;
-        if (!all) part = p.part + ((int64_t)blockIdx.x * 2 + (t == t_begin ? 0 : 1)) * part_floats<DH>();
+        t += run;
+    }
+    __syncthreads();
+    // the block's pieces, in the order of the tiles; those of one unit follow each other
+    for (int i = 0; i < 2 * kWaves;) {
+        const Piece piece = sh.piece[i >> 1][i & 1];
+        if (piece.unit_begin < 0) {
+            ++i;
+            continue;
+        }
+        int end = i + 1, run = piece.run;
+        for (; end < 2 * kWaves; ++end) {
+            const Piece &other = sh.piece[end >> 1][end & 1];
+            if (other.unit_begin >= 0 && other.unit_begin != piece.unit_begin) break;
+            if (other.unit_begin >= 0) run += other.run;
+        }
+        const Seq sq = load_seq(p, piece.b);
+        float *part = p.part + ((int64_t)blockIdx.x * 2 + (piece.unit_begin > t_begin ? 1 : 0)) * part_floats<DH>();
         for (int e = tid * 4; e < 16 * DH; e += kThreads * 4) {
             const int row = e / DH, dim = e - row * DH;
+            float top = -INFINITY, l = 0.f;
+            for (int k = i; k < end; ++k)
+                if (sh.piece[k >> 1][k & 1].unit_begin >= 0) top = fmaxf(top, sh.m[k >> 1][k & 1][row]);
             float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll
-            for (int i = 0; i < kWaves; ++i) {
-                const float4 x = *reinterpret_cast<const float4 *>(merge + (i * 16 + row) * DH + dim);
-                sum.x += x.x, sum.y += x.y, sum.z += x.z, sum.w += x.w;
+            for (int k = i; k < end; ++k) {
+                if (sh.piece[k >> 1][k & 1].unit_begin < 0) continue;
+                const float mk = sh.m[k >> 1][k & 1][row], scale = mk == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(mk - top);
+                const float4 x = *reinterpret_cast<const float4 *>(sh.o[k >> 1][k & 1] + row * kRow + dim);
+                l = fmaf(sh.l[k >> 1][k & 1][row], scale, l);
+                sum.x = fmaf(x.x, scale, sum.x), sum.y = fmaf(x.y, scale, sum.y), sum.z = fmaf(x.z, scale, sum.z), sum.w = fmaf(x.w, scale, sum.w);
             }
-            float row_top = -INFINITY, row_l = 0.f;
-#pragma unroll
-            for (int i = 0; i < kWaves; ++i) row_top = fmaxf(row_top, merge_m[i * 16 + row]);
-#pragma unroll
-            for (int i = 0; i < kWaves; ++i)
-                row_l += merge_m[i * 16 + row] == -INFINITY ? 0.f : merge_l[i * 16 + row] * __builtin_amdgcn_exp2f(merge_m[i * 16 + row] - row_top);
-            if (!all) {
+            if (run < piece.count) {
                 *reinterpret_cast<float4 *>(part + e) = sum;
                 if (dim == 0) {
-                    part[16 * DH + row] = row_top;
-                    part[16 * DH + 16 + row] = row_l;
+                    part[16 * DH + row] = top;
+                    part[16 * DH + 16 + row] = l;
                 }
                 continue;
             }
-            const int rr = rt * 16 + row, token = rr / p.group;
-            if (token >= sq.n) continue;
-            const int64_t at = (int64_t)(sq.first + token) * p.n_heads + h * p.group + (rr - token * p.group);
-            const float inv = row_l > 0.f ? 1.f / row_l : 0.f;
-            if (NS == 1)
-                *reinterpret_cast<uint2 *>(static_cast<uint16_t *>(p.out) + at * DH + dim) =
-                    make_uint2(pack_bf16(sum.x * inv, sum.y * inv), pack_bf16(sum.z * inv, sum.w * inv));
-            else
-                *reinterpret_cast<float4 *>(static_cast<float *>(p.out) + at * DH + dim) =
-                    make_float4(sum.x * inv, sum.y * inv, sum.z * inv, sum.w * inv);
-            if (dim == 0 && p.lse) p.lse[at] = row_l > 0.f ? row_top * kLn2 + logf(row_l) : -INFINITY;
+            const int64_t at = row_out(p, sq, piece.unit, row);
+            if (at < 0) continue;
+            const float inv = l > 0.f ? 1.f / l : 0.f;
+            store_out<NS>(p, at * DH + dim, make_float4(sum.x * inv, sum.y * inv, sum.z * inv, sum.w * inv));
+            if (dim == 0 && p.lse) p.lse[at] = l > 0.f ? top * kLn2 + logf(l) : -INFINITY;
         }
-        __syncthreads();
-        t += run;
+        i = end;
     }
 }
 
-// Joins the partial results of the units that more than one block worked on.  A block per unit (x: unit of a sequence, y: sequence).
+// Joins the partial results of the units that more than one block worked on.  A block per unit (x: row of a unit of a sequence, y: sequence)
+// and row; DH / 4 threads hold the row, the block's other threads take other partial results.  (A block a unit, one partial result after
+// the other: two sequences of 131072 keys, two heads, 128 results a unit: 49 us.)
 template <int DH, int NS>
 __global__ __launch_bounds__(kThreads) void attn_join_kernel(AttnParams p)
 {
-    static constexpr int kTile = tile_keys(DH);
-    const int b = blockIdx.y, unit = blockIdx.x, tid = threadIdx.x;
+    static constexpr int kTile = tile_keys(DH), kLanes = DH / 4, kGroups = kThreads / kLanes;
+    __shared__ float4 sums[kGroups][kLanes];
+    __shared__ float tops[kGroups], ls[kGroups];
+    const int b = blockIdx.y, unit = blockIdx.x >> 4, row = blockIdx.x & 15;
     const Seq sq = load_seq(p, b);
     if (sq.n == 0 || sq.n * p.group > p.few_rows || unit >= ceil_div(sq.n * p.group, 16) * p.n_kv_heads) return;
+    const int64_t at = row_out(p, sq, unit, row);
+    if (at < 0) return;
     int first, count;
     seq_range(p, sq, kTile, first, count);
     const int64_t per = tiles_per_block(p.seq_tiles[p.B], p.n_blocks);
     const int64_t t0 = p.seq_tiles[b] + (int64_t)unit * count, t1 = t0 + count;
     const int64_t b0 = t0 / per, b1 = (t1 - 1) / per;
     if (b0 == b1) return;
-    const int rt = unit / p.n_kv_heads, h = unit - rt * p.n_kv_heads;
-    for (int e = tid * 4; e < 16 * DH; e += kThreads * 4) {
-        const int row = e / DH, dim = e - row * DH;
-        const int rr = rt * 16 + row, token = rr / p.group;
-        if (token >= sq.n) continue;
-        float top = -INFINITY, l = 0.f;
-        float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
-        for (int64_t k = b0; k <= b1; ++k) {
-            const float *part = p.part + (2 * k + (t0 > k * per ? 1 : 0)) * part_floats<DH>();
-            const float pm = part[16 * DH + row], pl = part[16 * DH + 16 + row];
-            const float4 x = *reinterpret_cast<const float4 *>(part + e);
-            const float m_new = fmaxf(top, pm), base = m_new == -INFINITY ? 0.f : m_new;
-            const float keep = __builtin_amdgcn_exp2f(top - base), add = __builtin_amdgcn_exp2f(pm - base);
-            top = m_new;
-            l = l * keep + pl * add;
-            sum.x = sum.x * keep + x.x * add;
-            sum.y = sum.y * keep + x.y * add;
-            sum.z = sum.z * keep + x.z * add;
-            sum.w = sum.w * keep + x.w * add;
-        }
-        const int64_t at = (int64_t)(sq.first + token) * p.n_heads + h * p.group + (rr - token * p.group);
-        const float inv = l > 0.f ? 1.f / l : 0.f;
-        if (NS == 1)
-            *reinterpret_cast<uint2 *>(static_cast<uint16_t *>(p.out) + at * DH + dim) =
-                make_uint2(pack_bf16(sum.x * inv, sum.y * inv), pack_bf16(sum.z * inv, sum.w * inv));
-        else
-            *reinterpret_cast<float4 *>(static_cast<float *>(p.out) + at * DH + dim) = make_float4(sum.x * inv, sum.y * inv, sum.z * inv, sum.w * inv);
-        if (dim == 0 && p.lse) p.lse[at] = l > 0.f ? top * kLn2 + logf(l) : -INFINITY;
+    const int x = threadIdx.x % kLanes, group = threadIdx.x / kLanes;
+    float top = -INFINITY, l = 0.f;
+    float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
+    const auto add = [&](float pm, float pl, float4 v) {
+        const float m_new = fmaxf(top, pm), base = m_new == -INFINITY ? 0.f : m_new;
+        const float keep = __builtin_amdgcn_exp2f(top - base), more = __builtin_amdgcn_exp2f(pm - base);
+        top = m_new;
+        l = l * keep + pl * more;
+        sum.x = sum.x * keep + v.x * more;
+        sum.y = sum.y * keep + v.y * more;
+        sum.z = sum.z * keep + v.z * more;
+        sum.w = sum.w * keep + v.w * more;
+    };
+#pragma unroll 4
+    for (int64_t k = b0 + group; k <= b1; k += kGroups) {
+        const float *part = p.part + (2 * k + (t0 > k * per ? 1 : 0)) * part_floats<DH>();
+        add(part[16 * DH + row], part[16 * DH + 16 + row], *reinterpret_cast<const float4 *>(part + row * DH + 4 * x));
     }
+    if (x == 0) {
+        tops[group] = top;
+        ls[group] = l;
+    }
+    sums[group][x] = sum;
+    __syncthreads();
+    if (group > 0) return;
+#pragma unroll
+    for (int k = 1; k < kGroups; ++k) add(tops[k], ls[k], sums[k][x]);
+    const float inv = l > 0.f ? 1.f / l : 0.f;
+    store_out<NS>(p, at * DH + 4 * x, make_float4(sum.x * inv, sum.y * inv, sum.z * inv, sum.w * inv));
+    if (x == 0 && p.lse) p.lse[at] = l > 0.f ? top * kLn2 + logf(l) : -INFINITY;
 }
 
+// Blocks a CU: two; one where a wave needs the registers of two (fp32 over 128 dimensions, 256 dimensions)
 template <int DH, int NS>
-int launch_as(const AttnParams &p, hipStream_t s)
+constexpr int blocks_per_cu() { return DH == 256 || (DH == 128 && NS == 3) ? 1 : 2; }
+
+template <int DH, int NS>
+int launch_as(AttnParams p, int num_cus, hipStream_t s)
 {
-    const size_t lds = (size_t)(kWaves * 16 * DH + 2 * kWaves * 16) * 4 + (kWaves + p.B + 1) * 8;
-    if (lds > 64 * 1024)
-        MOE_HIP_CHECK(hipFuncSetAttribute(reinterpret_cast<const void *>(attn_decode_kernel<DH, NS>), hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds));
+    static constexpr int M = blocks_per_cu<DH, NS>();
+    p.n_blocks = M * num_cus;
+    static constexpr size_t kMost = sizeof(Shared<DH>) + (MOE_ATTN_MAX_B + 1) * 8;
+    static_assert(kMost <= 160 * 1024, "the sequences' places have to fit the LDS beside the pieces");
+    const size_t lds = sizeof(Shared<DH>) + (p.B + 1) * 8;
+    static std::once_flag once;
+    static hipError_t setup_rc = hipSuccess;
+    std::call_once(once, [&]() {
+        setup_rc = hipFuncSetAttribute(reinterpret_cast<const void *>(attn_decode_kernel<DH, NS, M>), hipFuncAttributeMaxDynamicSharedMemorySize, (int)kMost);
+    });
+    MOE_HIP_CHECK(setup_rc);
     {
         ProfScope ps("attn_decode", s);
-        hipLaunchKernelGGL((attn_decode_kernel<DH, NS>), dim3(p.n_blocks), dim3(kThreads), lds, s, p);
+        hipLaunchKernelGGL((attn_decode_kernel<DH, NS, M>), dim3(p.n_blocks), dim3(kThreads), lds, s, p);
         MOE_LAUNCH_CHECK("attn_decode_kernel");
     }
     ProfScope ps("attn_join", s);
-    const int units = ceil_div((int)((int64_t)p.max_q * p.group < p.few_rows ? (int64_t)p.max_q * p.group : p.few_rows), 16) * p.n_kv_heads;
-    hipLaunchKernelGGL((attn_join_kernel<DH, NS>), dim3(units, p.B), dim3(kThreads), 0, s, p);
+    const int64_t rows = (int64_t)p.max_q * p.group < p.few_rows ? (int64_t)p.max_q * p.group : p.few_rows;
+    const int units = ceil_div((int)rows, 16) * p.n_kv_heads;
+    hipLaunchKernelGGL((attn_join_kernel<DH, NS>), dim3(units * 16, p.B), dim3(kThreads), 0, s, p);
     MOE_LAUNCH_CHECK("attn_join_kernel");
     return MOE_OK;
 }
-
-int decode_blocks(int num_cus) { return 2 * num_cus; }
 
 }  // namespace
 
 // partial results of two units a block
 int64_t attn_decode_workspace(int head_dim, int num_cus)
 {
-    return align_up((int64_t)decode_blocks(num_cus) * 2 * (16 * head_dim + 32) * 4, 256);
+    return align_up((int64_t)2 * num_cus * 2 * (16 * head_dim + 32) * 4, 256);
 }
 
-int launch_attn_decode(int dtype, int head_dim, AttnParams p, int num_cus, hipStream_t s)
+int launch_attn_decode(int dtype, int head_dim, const AttnParams &p, int num_cus, hipStream_t s)
 {
-    p.n_blocks = decode_blocks(num_cus);
     const bool bf = dtype == MOE_DTYPE_BF16;
-    if (head_dim == 64) return bf ? launch_as<64, 1>(p, s) : launch_as<64, 3>(p, s);
-    if (head_dim == 128) return bf ? launch_as<128, 1>(p, s) : launch_as<128, 3>(p, s);
-    return bf ? launch_as<256, 1>(p, s) : launch_as<256, 3>(p, s);
+    if (head_dim == 64) return bf ? launch_as<64, 1>(p, num_cus, s) : launch_as<64, 3>(p, num_cus, s);
+    if (head_dim == 128) return bf ? launch_as<128, 1>(p, num_cus, s) : launch_as<128, 3>(p, num_cus, s);
+    return bf ? launch_as<256, 1>(p, num_cus, s) : launch_as<256, 3>(p, num_cus, s);
 }
 
 }  // namespace moe355
