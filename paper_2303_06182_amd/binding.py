@@ -205,6 +205,20 @@ def _stream() -> ctypes.c_void_p:
     return ctypes.c_void_p(torch.cuda.current_stream().cuda_stream)
 
 
+def _addr(t: Optional[torch.Tensor]) -> Optional[int]:
+    """_ptr for calls of a few microseconds: the address alone, which an argument declared as a pointer takes."""
+    if t is None:
+        return None
+    if not t.is_contiguous():
+        raise ValueError("tensor must be contiguous")
+    return t.data_ptr()
+
+
+def _stream_on(device: torch.device) -> int:
+    """The current stream of a device (index 0 where it has none), without making a stream object."""
+    return torch._C._cuda_getCurrentRawStream(device.index or 0)
+
+
 def moe_capacity(T: int, E: int, k: int, cf: float, convention: int = MOE_CAPACITY_SHARE) -> int:
     c = load_library().moe_capacity(T, E, k, cf, convention)
     if c < 0:
@@ -553,7 +567,9 @@ class KvCache:
         if k_scale.dtype != torch.float32 or v_scale.dtype != torch.float32:
             raise ValueError("scales must be float32")
         self.k, self.v, self.k_scale, self.v_scale = k, v, k_scale, v_scale
+        self.shape = tuple(k.shape)
         self.struct = MoeKvCache(_ptr(k), _ptr(v), _ptr(k_scale), _ptr(v_scale))
+        self.ref = ctypes.byref(self.struct)
 
 
 class PagedAttention:
@@ -589,26 +605,25 @@ class PagedAttention:
         return KvCache(k, v, ks, vs)
 
     def _rows(self, t: Optional[torch.Tensor], heads: int, name: str):
-        """(pointer, elements from token to token) of [T, heads, head_dim]."""
+        """(address, elements from token to token) of [T, heads, head_dim]."""
         if t is None:
             return None, 0
-        if t.dim() != 3 or t.shape[1] != heads or t.shape[2] != self.cfg.head_dim or t.dtype != self.torch_dtype:
-            raise ValueError("%s must be [T, %d, %d] of %s" % (name, heads, self.cfg.head_dim, self.torch_dtype))
-        if t.shape[0] and (t.stride(2) != 1 or (heads > 1 and t.stride(1) != self.cfg.head_dim)):
+        dim, shape, strides = self.cfg.head_dim, t.shape, t.stride()
+        if len(shape) != 3 or shape[1] != heads or shape[2] != dim or t.dtype != self.torch_dtype:
+            raise ValueError("%s must be [T, %d, %d] of %s" % (name, heads, dim, self.torch_dtype))
+        if shape[0] and (strides[2] != 1 or (heads > 1 and strides[1] != dim)):
             raise ValueError("%s: the heads of a token must lie together" % name)
-        stride = t.stride(0) if t.shape[0] > 1 else heads * self.cfg.head_dim
-        return ctypes.c_void_p(t.data_ptr()), stride
+        return t.data_ptr(), strides[0] if shape[0] > 1 else heads * dim
 
     def _batch(self, cache: KvCache, q_offsets, kv_len, page_table):
         c = self.cfg
-        if tuple(cache.k.shape) != (c.num_pages, c.n_kv_heads, c.page_size, c.head_dim):
-            raise ValueError("the cache has shape %s, the handle another geometry" % (tuple(cache.k.shape),))
+        if cache.shape != (c.num_pages, c.n_kv_heads, c.page_size, c.head_dim):
+            raise ValueError("the cache has shape %s, the handle another geometry" % (cache.shape,))
         B = kv_len.shape[0]
-        if q_offsets.shape[0] != B + 1 or tuple(page_table.shape) != (B, c.max_pages):
+        if q_offsets.shape[0] != B + 1 or page_table.shape != (B, c.max_pages):
             raise ValueError("q_offsets must be [B + 1], kv_len [B] and page_table [B, max_pages]")
-        for t in (q_offsets, kv_len, page_table):
-            if t.dtype != torch.int32:
-                raise ValueError("q_offsets, kv_len and page_table must be int32")
+        if q_offsets.dtype != torch.int32 or kv_len.dtype != torch.int32 or page_table.dtype != torch.int32:
+            raise ValueError("q_offsets, kv_len and page_table must be int32")
         return B
 
     def moe_kv_append(self, cache: KvCache, q, k, v, inv_freq, q_offsets, kv_len, page_table, max_q: int, q_out=None):
@@ -621,8 +636,8 @@ class PagedAttention:
         if q is not None and q_out is None:
             q_out = torch.empty((T, c.n_heads, c.head_dim), dtype=self.torch_dtype, device=self.device)
         (qp, qs), (kp, ks), (vp, vs) = self._rows(q, c.n_heads, "q"), self._rows(k, c.n_kv_heads, "k"), self._rows(v, c.n_kv_heads, "v")
-        _check(self.lib.moe_kv_append(self.h, ctypes.byref(cache.struct), qp, qs, kp, ks, vp, vs, _ptr(inv_freq), _ptr(q_offsets), _ptr(kv_len),
-                                      _ptr(page_table), B, T, max_q, _ptr(q_out), _stream()))
+        _check(self.lib.moe_kv_append(self.h, cache.ref, qp, qs, kp, ks, vp, vs, _addr(inv_freq), _addr(q_offsets), _addr(kv_len),
+                                      _addr(page_table), B, T, max_q, _addr(q_out), _stream_on(self.device)))
         return q_out
 
     def moe_attn_forward(self, cache: KvCache, q, q_offsets, kv_len, page_table, max_q: int, max_kv: int, scale: Optional[float] = None,
@@ -634,9 +649,9 @@ class PagedAttention:
         if lse is None and want_lse:
             lse = torch.empty((T, c.n_heads), dtype=torch.float32, device=self.device)
         qp, qs = self._rows(q, c.n_heads, "q")
-        _check(self.lib.moe_attn_forward(self.h, ctypes.byref(cache.struct), qp, qs, _ptr(q_offsets), _ptr(kv_len), _ptr(page_table), B, T, max_q,
-                                         max_kv, c.head_dim ** -0.5 if scale is None else scale, int(causal), window, _ptr(out), _ptr(lse),
-                                         _ptr(self.workspace), self.workspace.numel(), _stream()))
+        _check(self.lib.moe_attn_forward(self.h, cache.ref, qp, qs, _addr(q_offsets), _addr(kv_len), _addr(page_table), B, T, max_q,
+                                         max_kv, c.head_dim ** -0.5 if scale is None else scale, int(causal), window, _addr(out), _addr(lse),
+                                         self.workspace.data_ptr(), self.workspace.numel(), _stream_on(self.device)))
         return out, lse
 
 
@@ -662,7 +677,7 @@ def moe_sample(logits, u, temperature=None, top_k=None, top_p=None, min_p=None, 
     logprob = new(torch.float32) if logprob is None else logprob
     if workspace is None:
         workspace = torch.empty(moe_sample_workspace_bytes(B, V), dtype=torch.uint8, device=logits.device)
-    _check(lib.moe_sample(ctypes.c_void_p(logits.data_ptr()), MOE_DTYPE_BF16 if logits.dtype == torch.bfloat16 else MOE_DTYPE_F32,
-                          logits.stride(0) if B > 1 else V, B, V, _ptr(u), _ptr(temperature), _ptr(top_k), _ptr(top_p), _ptr(min_p), _ptr(token),
-                          _ptr(logprob), _ptr(workspace), workspace.numel(), _stream()))
+    _check(lib.moe_sample(logits.data_ptr(), MOE_DTYPE_BF16 if logits.dtype == torch.bfloat16 else MOE_DTYPE_F32,
+                          logits.stride(0) if B > 1 else V, B, V, _addr(u), _addr(temperature), _addr(top_k), _addr(top_p), _addr(min_p), _addr(token),
+                          _addr(logprob), _addr(workspace), workspace.numel(), _stream_on(logits.device)))
     return token, logprob

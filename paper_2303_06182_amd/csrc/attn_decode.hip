@@ -414,12 +414,12 @@ __global__ __launch_bounds__(kThreads, M) void attn_decode_kernel(AttnParams p)
 // and row; DH / 4 threads hold the row, the block's other threads take other partial results.  (A block a unit, one partial result after
 // the other: two sequences of 131072 keys, two heads, 128 results a unit: 49 us.)
 template <int DH, int NS>
-__global__ __launch_bounds__(kThreads) void attn_join_kernel(AttnParams p)
+__global__ __launch_bounds__(kThreads) void attn_join_kernel(AttnParams p, int rows)
 {
     static constexpr int kTile = tile_keys(DH), kLanes = DH / 4, kGroups = kThreads / kLanes;
     __shared__ float4 sums[kGroups][kLanes];
     __shared__ float tops[kGroups], ls[kGroups];
-    const int b = blockIdx.y, unit = blockIdx.x >> 4, row = blockIdx.x & 15;
+    const int b = blockIdx.y, unit = blockIdx.x / rows, row = blockIdx.x - unit * rows;
     const Seq sq = load_seq(p, b);
     if (sq.n == 0 || sq.n * p.group > p.few_rows || unit >= ceil_div(sq.n * p.group, 16) * p.n_kv_heads) return;
     const int64_t at = row_out(p, sq, unit, row);
@@ -487,8 +487,8 @@ int launch_as(AttnParams p, int num_cus, hipStream_t s)
     }
     ProfScope ps("attn_join", s);
     const int64_t rows = (int64_t)p.max_q * p.group < p.few_rows ? (int64_t)p.max_q * p.group : p.few_rows;
-    const int units = ceil_div((int)rows, 16) * p.n_kv_heads;
-    hipLaunchKernelGGL((attn_join_kernel<DH, NS>), dim3(units * 16, p.B), dim3(kThreads), 0, s, p);
+    const int units = ceil_div((int)rows, 16) * p.n_kv_heads, unit_rows = rows < 16 ? (int)rows : 16;
+    hipLaunchKernelGGL((attn_join_kernel<DH, NS>), dim3(units * unit_rows, p.B), dim3(kThreads), 0, s, p, unit_rows);
     MOE_LAUNCH_CHECK("attn_join_kernel");
     return MOE_OK;
 }

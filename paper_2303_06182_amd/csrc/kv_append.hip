@@ -49,23 +49,27 @@ __device__ __forceinline__ void cos_sin(double angle, double &c, double &s)
     s = n >= 2 ? -b : b;
 }
 
+// eight elements as they lie in memory
 template <bool BF16>
-__device__ __forceinline__ void load8(const void *p, int64_t at, float (&v)[8])
+struct Raw {
+    uint4 q[BF16 ? 1 : 2];
+};
+template <bool BF16>
+__device__ __forceinline__ Raw<BF16> load8(const void *p, int64_t at)
 {
-    if (BF16) {
-        const uint4 r = *reinterpret_cast<const uint4 *>(static_cast<const uint16_t *>(p) + at);
-        const uint32_t w[4] = {r.x, r.y, r.z, r.w};
+    Raw<BF16> r;
+    const uint4 *src = reinterpret_cast<const uint4 *>(static_cast<const uint8_t *>(p) + at * (BF16 ? 2 : 4));
+    r.q[0] = src[0];
+    if (!BF16) r.q[BF16 ? 0 : 1] = src[1];
+    return r;
+}
+template <bool BF16>
+__device__ __forceinline__ void floats(const Raw<BF16> &r, float (&v)[8])
+{
+    const uint4 a = r.q[0], b = r.q[BF16 ? 0 : 1];
+    const uint32_t w[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            v[2 * i] = __uint_as_float(w[i] << 16);
-            v[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
-        }
-    } else {
-        const float4 a = *reinterpret_cast<const float4 *>(static_cast<const float *>(p) + at);
-        const float4 b = *reinterpret_cast<const float4 *>(static_cast<const float *>(p) + at + 4);
-        v[0] = a.x, v[1] = a.y, v[2] = a.z, v[3] = a.w;
-        v[4] = b.x, v[5] = b.y, v[6] = b.z, v[7] = b.w;
-    }
+    for (int i = 0; i < 8; ++i) v[i] = __uint_as_float(!BF16 ? w[i] : i & 1 ? w[i >> 1] & 0xffff0000u : w[i >> 1] << 16);
 }
 
 template <bool BF16>
@@ -161,10 +165,13 @@ __device__ __forceinline__ void round_anew(uint8_t *page, int bytes, float ratio
     }
 }
 
+// Heads of queries a thread turns by the same angles: their loads are in flight together, the angles' 40 operations in 64 bits a pair shared.
+constexpr int kQHeads = 4;
+
 // NT threads, each with at most U items of a page's keys and values.  kv_units: blocks of the first kind per sequence,
 // q_units: of the second.
 template <int DH, bool BF16, int NT, int U>
-__global__ __launch_bounds__(NT) void kv_append_kernel(AppendParams p, int kv_units, int q_units, int q_heads)
+__global__ __launch_bounds__(NT) void kv_append_kernel(AppendParams p, int kv_units, int q_units)
 {
     static constexpr int kItems = DH / 16;
     const int units = kv_units + q_units;
@@ -172,21 +179,28 @@ __global__ __launch_bounds__(NT) void kv_append_kernel(AppendParams p, int kv_un
     const Seq sq = load_seq(p.a, b);
     const int begin = sq.kv - sq.n;  // position of the first new token
     const int tid = threadIdx.x;
-    if (unit >= kv_units) {  // queries: an item of a token, the same of q_heads heads
-        const int per_token = p.a.max_q * kItems;
-        const int blocks = ceil_div(per_token, NT);
-        const int group = (unit - kv_units) / blocks, at = ((unit - kv_units) - group * blocks) * NT + tid;
-        const int i = at / kItems, e = at - i * kItems;
-        if (i >= sq.n) return;
+    if (unit >= kv_units) {  // queries: an item of a token, the same of kQHeads heads
+        const int per_group = p.a.max_q * kItems, at = (unit - kv_units) * NT + tid;
+        const int group = at / per_group, i = (at - group * per_group) / kItems, e = (at - group * per_group) - i * kItems;
+        if (i >= sq.n || group * kQHeads >= p.a.n_heads) return;
         const Item it = item_of(e, p.rot_dim, p.interleaved);
+        const int64_t t = sq.first + i;
+        Raw<BF16> rx[kQHeads], ry[kQHeads];
+#pragma unroll
+        for (int k = 0; k < kQHeads; ++k) {
+            const int h = min(group * kQHeads + k, p.a.n_heads - 1);
+            rx[k] = load8<BF16>(p.a.q, t * p.a.q_stride + (int64_t)h * DH + it.a);
+            ry[k] = load8<BF16>(p.a.q, t * p.a.q_stride + (int64_t)h * DH + it.b);
+        }
         double c[8], s[8];
         if (it.turns) angles(p.inv_freq, e, begin + i, c, s);
-        const int64_t t = sq.first + i;
-        const int h1 = min((group + 1) * q_heads, p.a.n_heads);
-        for (int h = group * q_heads; h < h1; ++h) {
+#pragma unroll
+        for (int k = 0; k < kQHeads; ++k) {
+            const int h = group * kQHeads + k;
+            if (h >= p.a.n_heads) break;
             float x[8], y[8];
-            load8<BF16>(p.a.q, t * p.a.q_stride + (int64_t)h * DH + it.a, x);
-            load8<BF16>(p.a.q, t * p.a.q_stride + (int64_t)h * DH + it.b, y);
+            floats<BF16>(rx[k], x);
+            floats<BF16>(ry[k], y);
             if (it.turns) turn(x, y, c, s, p.interleaved);
             store8<BF16>(p.q_out, (t * p.a.n_heads + h) * DH + it.a, x);
             store8<BF16>(p.q_out, (t * p.a.n_heads + h) * DH + it.b, y);
@@ -198,28 +212,38 @@ __global__ __launch_bounds__(NT) void kv_append_kernel(AppendParams p, int kv_un
     const int slot = (max(begin, 0) >> p.a.page_shift) + m;
     const int lo = max(max(begin, 0), slot << p.a.page_shift), hi = min(sq.kv, (slot + 1) << p.a.page_shift);
     if (lo >= hi || slot >= p.a.max_pages) return;
+    const int r0 = lo - (slot << p.a.page_shift), rows = hi - lo, items = rows * kItems;
+    // the new rows, and beside them the page and its scales
+    Raw<BF16> rx[U], ry[U];
+    Item it[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+        const int id = min(tid + u * NT, 2 * items - 1);
+        const bool is_v = id >= items;
+        const int r = (is_v ? id - items : id) / kItems, e = (is_v ? id - items : id) - r * kItems;
+        it[u] = is_v ? Item{16 * e, 16 * e + 8, false} : item_of(e, p.rot_dim, p.interleaved);
+        const int64_t t = sq.first + (lo - begin) + r;
+        const void *src = is_v ? p.v_new : p.k_new;
+        const int64_t at = t * (is_v ? p.v_stride : p.k_stride) + (int64_t)h * DH;
+        rx[u] = load8<BF16>(src, at + it[u].a);
+        ry[u] = load8<BF16>(src, at + it[u].b);
+    }
     const int page = p.a.page_table[(int64_t)b * p.a.max_pages + slot];
     if (page < 0 || page >= p.a.num_pages) return;
-    const int r0 = lo - (slot << p.a.page_shift), rows = hi - lo, items = rows * kItems;
     const int64_t unit_at = (int64_t)page * p.a.n_kv_heads + h;
     const float old_k = p.a.k_scale[unit_at], old_v = p.a.v_scale[unit_at];
 
     float x[U][8], y[U][8];
-    Item it[U];
     float top_k = 0.f, top_v = 0.f;
 #pragma unroll
     for (int u = 0; u < U; ++u) {
         const int id = tid + u * NT;
-        const bool is_v = id >= items;
-        const int r = (is_v ? id - items : id) / kItems, e = (is_v ? id - items : id) - r * kItems;
-        it[u] = is_v ? Item{16 * e, 16 * e + 8, false} : item_of(e, p.rot_dim, p.interleaved);
         if (id >= 2 * items) continue;
-        const int64_t t = sq.first + (lo - begin) + r;
-        const void *src = is_v ? p.v_new : p.k_new;
-        const int64_t at = t * (is_v ? p.v_stride : p.k_stride) + (int64_t)h * DH;
-        load8<BF16>(src, at + it[u].a, x[u]);
-        load8<BF16>(src, at + it[u].b, y[u]);
+        const bool is_v = id >= items;
+        floats<BF16>(rx[u], x[u]);
+        floats<BF16>(ry[u], y[u]);
         if (it[u].turns) {
+            const int r = id / kItems, e = id - r * kItems;
             double c[8], s[8];
             angles(p.inv_freq, e, lo + r, c, s);
             turn(x[u], y[u], c, s, p.interleaved);
@@ -277,18 +301,14 @@ int launch_as(const AppendParams &p, int num_cus, hipStream_t s)
 {
     const int kv_pages = (p.a.max_q + (1 << p.a.page_shift) - 2) / (1 << p.a.page_shift) + 1;
     const int64_t kv_units = (int64_t)kv_pages * p.a.n_kv_heads;
-    // queries: as many heads a thread as leave two blocks for every CU
-    const int64_t q_blocks = p.a.q ? ceil_div(p.a.max_q * (DH / 16), NT) : 0;
-    int q_heads = p.a.n_heads;
-    while (q_heads > 1 && q_blocks * p.a.B * ceil_div(p.a.n_heads, q_heads) < 2 * num_cus) q_heads = (q_heads + 1) / 2;
-    const int64_t q_units = q_blocks * ceil_div(p.a.n_heads, q_heads);
+    const int64_t q_units = p.a.q ? ((int64_t)ceil_div(p.a.n_heads, kQHeads) * p.a.max_q * (DH / 16) + NT - 1) / NT : 0;
     const int64_t blocks = (kv_units + q_units) * p.a.B;
     if (blocks >= (1ll << 31)) {
         set_error("moe_kv_append: %lld blocks", (long long)blocks);
         return MOE_ERR_INVALID_ARG;
     }
     ProfScope ps("kv_append", s);
-    hipLaunchKernelGGL((kv_append_kernel<DH, BF16, NT, U>), dim3((unsigned)blocks), dim3(NT), 0, s, p, (int)kv_units, (int)q_units, q_heads);
+    hipLaunchKernelGGL((kv_append_kernel<DH, BF16, NT, U>), dim3((unsigned)blocks), dim3(NT), 0, s, p, (int)kv_units, (int)q_units);
     MOE_LAUNCH_CHECK("kv_append_kernel");
     return MOE_OK;
 }
@@ -298,9 +318,12 @@ int launch_sized(const AppendParams &p, int num_cus, hipStream_t s)
 {
     const int rows = p.a.max_q < (1 << p.a.page_shift) ? p.a.max_q : 1 << p.a.page_shift;
     const int items = 2 * rows * (DH / 16);  // of keys and values in a block
+    // a key's and a value's item a thread, so that a block's loads are all in flight at once and registers leave room for five waves a SIMD
     if (items <= 64) return launch_as<DH, BF16, 64, 1>(p, num_cus, s);
-    if (items <= 256) return launch_as<DH, BF16, 64, 4>(p, num_cus, s);
-    if (items <= 1024) return launch_as<DH, BF16, 256, 4>(p, num_cus, s);
+    if (items <= 128) return launch_as<DH, BF16, 64, 2>(p, num_cus, s);
+    if (items <= 512) return launch_as<DH, BF16, 256, 2>(p, num_cus, s);
+    if (items <= 1024) return launch_as<DH, BF16, 512, 2>(p, num_cus, s);
+    if (items <= 2048) return launch_as<DH, BF16, 1024, 2>(p, num_cus, s);
     return launch_as<DH, BF16, 1024, 4>(p, num_cus, s);
 }
 
