@@ -168,32 +168,70 @@ __device__ __forceinline__ void round_anew(uint8_t *page, int bytes, float ratio
 // Heads of queries a thread turns by the same angles: their loads are in flight together, the angles' 40 operations in 64 bits a pair shared.
 constexpr int kQHeads = 4;
 
-// NT threads, each with at most U items of a page's keys and values.  kv_units: blocks of the first kind per sequence,
-// q_units: of the second.
+// Pages that a sequence's new tokens touch, and the first of them.
+__device__ __forceinline__ int pages_of(const AttnParams &p, const Seq &sq, int &first)
+{
+    const int lo = max(sq.kv - sq.n, 0);
+    first = lo >> p.page_shift;
+    return sq.n > 0 && sq.kv > lo ? ((sq.kv - 1) >> p.page_shift) - first + 1 : 0;
+}
+
+// The sequence of the index-th touched page of all, and which of its pages that is: every wave adds up the sequences' pages, 64 at a
+// time.  -1: there are not so many.
+__device__ __forceinline__ int page_owner(const AttnParams &p, int index, int &m)
+{
+    const int lane = threadIdx.x & 63;
+    for (int base = 0; base < p.B; base += 64) {
+        int first, sum = 0;
+        if (base + lane < p.B) sum = pages_of(p, load_seq(p, base + lane), first);
+        const int mine = sum;
+#pragma unroll
+        for (int off = 1; off < 64; off <<= 1) {
+            const int o = __shfl_up(sum, off, 64);
+            if (lane >= off) sum += o;
+        }
+        const unsigned long long past = __ballot(sum > index);
+        if (past) {
+            const int owner = __ffsll(past) - 1;
+            m = index - __shfl(sum - mine, owner, 64);
+            return base + owner;
+        }
+        index -= __shfl(sum, 63, 64);
+    }
+    return -1;
+}
+
+// NT threads, each with at most U items of a page's keys and values.  kv_units: blocks of the first kind; pages: 0 where these are
+// counted over the pages that are touched, else pages of a sequence at most (a decoder step: one, and nothing has to be added up).
 template <int DH, bool BF16, int NT, int U>
-__global__ __launch_bounds__(NT) void kv_append_kernel(AppendParams p, int kv_units, int q_units)
+__global__ __launch_bounds__(NT) void kv_append_kernel(AppendParams p, int kv_units, int pages)
 {
     static constexpr int kItems = DH / 16;
-    const int units = kv_units + q_units;
-    const int b = blockIdx.x / units, unit = blockIdx.x - b * units;
-    const Seq sq = load_seq(p.a, b);
-    const int begin = sq.kv - sq.n;  // position of the first new token
+    const int unit = blockIdx.x;
     const int tid = threadIdx.x;
     if (unit >= kv_units) {  // queries: an item of a token, the same of kQHeads heads
-        const int per_group = p.a.max_q * kItems, at = (unit - kv_units) * NT + tid;
-        const int group = at / per_group, i = (at - group * per_group) / kItems, e = (at - group * per_group) - i * kItems;
-        if (i >= sq.n || group * kQHeads >= p.a.n_heads) return;
+        const int64_t at = (int64_t)(unit - kv_units) * NT + tid, per_group = (int64_t)p.a.T * kItems;
+        const int group = (int)(at / per_group), item = (int)(at - group * per_group), t = item / kItems, e = item - t * kItems;
+        if (group * kQHeads >= p.a.n_heads) return;
+        int lo = 0, hi = p.a.B;  // the last sequence that begins at or before t
+        while (hi - lo > 1) {
+            const int mid = (lo + hi) >> 1;
+            if (p.a.q_offsets[mid] <= t) lo = mid;
+            else hi = mid;
+        }
+        const Seq sq = load_seq(p.a, lo);
+        const int i = t - sq.first;
+        if (i < 0 || i >= sq.n) return;
         const Item it = item_of(e, p.rot_dim, p.interleaved);
-        const int64_t t = sq.first + i;
         Raw<BF16> rx[kQHeads], ry[kQHeads];
 #pragma unroll
         for (int k = 0; k < kQHeads; ++k) {
             const int h = min(group * kQHeads + k, p.a.n_heads - 1);
-            rx[k] = load8<BF16>(p.a.q, t * p.a.q_stride + (int64_t)h * DH + it.a);
-            ry[k] = load8<BF16>(p.a.q, t * p.a.q_stride + (int64_t)h * DH + it.b);
+            rx[k] = load8<BF16>(p.a.q, (int64_t)t * p.a.q_stride + (int64_t)h * DH + it.a);
+            ry[k] = load8<BF16>(p.a.q, (int64_t)t * p.a.q_stride + (int64_t)h * DH + it.b);
         }
         double c[8], s[8];
-        if (it.turns) angles(p.inv_freq, e, begin + i, c, s);
+        if (it.turns) angles(p.inv_freq, e, sq.kv - sq.n + i, c, s);
 #pragma unroll
         for (int k = 0; k < kQHeads; ++k) {
             const int h = group * kQHeads + k;
@@ -202,14 +240,22 @@ __global__ __launch_bounds__(NT) void kv_append_kernel(AppendParams p, int kv_un
             floats<BF16>(rx[k], x);
             floats<BF16>(ry[k], y);
             if (it.turns) turn(x, y, c, s, p.interleaved);
-            store8<BF16>(p.q_out, (t * p.a.n_heads + h) * DH + it.a, x);
-            store8<BF16>(p.q_out, (t * p.a.n_heads + h) * DH + it.b, y);
+            store8<BF16>(p.q_out, ((int64_t)t * p.a.n_heads + h) * DH + it.a, x);
+            store8<BF16>(p.q_out, ((int64_t)t * p.a.n_heads + h) * DH + it.b, y);
         }
         return;
     }
     const int page_size = 1 << p.a.page_shift;
-    const int m = unit / p.a.n_kv_heads, h = unit - m * p.a.n_kv_heads;
-    const int slot = (max(begin, 0) >> p.a.page_shift) + m;
+    const int index = unit / p.a.n_kv_heads, h = unit - index * p.a.n_kv_heads;
+    int m = 0, b = index;
+    if (!pages) b = page_owner(p.a, index, m);
+    else if (pages > 1) b = index / pages, m = index - b * pages;
+    if (b < 0) return;
+    const Seq sq = load_seq(p.a, b);
+    const int begin = sq.kv - sq.n;  // position of the first new token
+    int slot;
+    if (m >= pages_of(p.a, sq, slot)) return;
+    slot += m;
     const int lo = max(max(begin, 0), slot << p.a.page_shift), hi = min(sq.kv, (slot + 1) << p.a.page_shift);
     if (lo >= hi || slot >= p.a.max_pages) return;
     const int r0 = lo - (slot << p.a.page_shift), rows = hi - lo, items = rows * kItems;
@@ -299,16 +345,20 @@ __global__ __launch_bounds__(NT) void kv_append_kernel(AppendParams p, int kv_un
 template <int DH, bool BF16, int NT, int U>
 int launch_as(const AppendParams &p, int num_cus, hipStream_t s)
 {
-    const int kv_pages = (p.a.max_q + (1 << p.a.page_shift) - 2) / (1 << p.a.page_shift) + 1;
-    const int64_t kv_units = (int64_t)kv_pages * p.a.n_kv_heads;
-    const int64_t q_units = p.a.q ? ((int64_t)ceil_div(p.a.n_heads, kQHeads) * p.a.max_q * (DH / 16) + NT - 1) / NT : 0;
-    const int64_t blocks = (kv_units + q_units) * p.a.B;
+    // touched pages: at most (n - 2) / page_size + 2 of each sequence, and T / page_size + 2 B of all
+    const int page_size = 1 << p.a.page_shift;
+    const int each = (p.a.max_q + page_size - 2) / page_size + 1;
+    const int64_t all = (int64_t)p.a.T / page_size + 2 * p.a.B;
+    const bool counted = (int64_t)each * p.a.B > all;
+    const int64_t kv_units = (counted ? all : (int64_t)each * p.a.B) * p.a.n_kv_heads;
+    const int64_t q_units = p.a.q ? ((int64_t)ceil_div(p.a.n_heads, kQHeads) * p.a.T * (DH / 16) + NT - 1) / NT : 0;
+    const int64_t blocks = kv_units + q_units;
     if (blocks >= (1ll << 31)) {
         set_error("moe_kv_append: %lld blocks", (long long)blocks);
         return MOE_ERR_INVALID_ARG;
     }
     ProfScope ps("kv_append", s);
-    hipLaunchKernelGGL((kv_append_kernel<DH, BF16, NT, U>), dim3((unsigned)blocks), dim3(NT), 0, s, p, (int)kv_units, (int)q_units);
+    hipLaunchKernelGGL((kv_append_kernel<DH, BF16, NT, U>), dim3((unsigned)blocks), dim3(NT), 0, s, p, (int)kv_units, counted ? 0 : each);
     MOE_LAUNCH_CHECK("kv_append_kernel");
     return MOE_OK;
 }
