@@ -28,6 +28,8 @@ struct SampleParams {
     const int32_t *top_k;
     int32_t *token;
     float *logprob;
+    int chunks, chunk;   // blocks of a row and tokens of each; 1: sample_kernel alone
+    uint8_t *work;       // with more: a RowWork a row
 };
 
 static constexpr uint32_t kLowest = 0x007fffffu;  // key of -infinity
@@ -193,25 +195,24 @@ __device__ __forceinline__ u64 block_scan(u64 mine)
     return front + x - mine;
 }
 
-// f(v, index) for every token of the row (-infinity for places past its end); after each vector done(its number).  A thread has the next
-// two vectors in flight, and the work of four tokens at most is mixed by the compiler: with more of it in registers the 64-bit arithmetic
-// spills.  skip(largest logit of a vector): whether f need not see the vector; where few tokens matter, a branch a token would cost six times
-// as much as all else (a 128000-token row by one block: 30 us, a branch a vector 5).
+// f(v, index) for every token from `from` (a multiple of 64 vectors) to `to`, -infinity for places past it; after each vector done(its
+// number).  A thread has the next two vectors in flight, and the work of four tokens at most is mixed by the compiler: with more of it in
+// registers the 64-bit arithmetic spills.  skip(largest logit of a vector): whether f need not see the vector.
 template <bool BF16, typename S, typename F, typename G>
-__device__ __forceinline__ void over_row(const char *row, int V, S skip, F f, G done)
+__device__ __forceinline__ void over_row(const char *row, int from, int to, S skip, F f, G done)
 {
     static constexpr int kN = Vec<BF16>::kN, kFlight = 2;
-    const int vectors = (V + kN - 1) / kN;
+    const int vectors = (to + kN - 1) / kN, mine = from / kN + (int)threadIdx.x;
     Vec<BF16> x[kFlight];
 #pragma unroll
-    for (int u = 0; u < kFlight; ++u) x[u] = load_vec<BF16>(row, min((int)threadIdx.x + u * kThreads, vectors) * kN, V);
+    for (int u = 0; u < kFlight; ++u) x[u] = load_vec<BF16>(row, min(mine + u * kThreads, vectors) * kN, to);
 #pragma unroll 1
-    for (int base = 0; base < vectors; base += kFlight * kThreads) {  // the same count for all threads: done() may use the whole wave
+    for (int base = 0; from / kN + base < vectors; base += kFlight * kThreads) {  // the same count for all threads: done() may use the whole wave
 #pragma unroll
         for (int u = 0; u < kFlight; ++u) {
-            const int at = base + u * kThreads + threadIdx.x;
+            const int at = mine + base + u * kThreads;
             const Vec<BF16> now = x[u];
-            x[u] = load_vec<BF16>(row, min(at + kFlight * kThreads, vectors) * kN, V);
+            x[u] = load_vec<BF16>(row, min(at + kFlight * kThreads, vectors) * kN, to);
             float most = now.raw(0);
 #pragma unroll
             for (int j = 1; j < kN; ++j) most = fmaxf(most, now.raw(j));
@@ -240,7 +241,7 @@ __device__ __forceinline__ u64 walk(const char *row, int V, const Row &r, bool b
         __syncthreads();
         if (tid < 512) sh.candidate[tid] = 0;
         __syncthreads();
-        over_row<BF16>(row, V, [](float) { return false; }, [&](float v, int i) {
+        over_row<BF16>(row, 0, V, [](float) { return false; }, [&](float v, int i) {
             if (v == -INFINITY || step_of(r, v) != step) return;
             const u64 c = pack(key_of(v), i);
             if (c < cut || (shift < 56 && (c >> (shift + 8)) != prefix)) return;
@@ -306,24 +307,23 @@ __device__ __forceinline__ void sort_candidates(int n)
     __syncthreads();
 }
 
-// The step in which the running value of the histogram reaches the target, and the running value in front of it; kSteps where it
-// never does.  upto: how many tokens the steps up to it hold, by weight only about: a token of step i weighs 2^f exp(-(i + 1/2) / 32), two per
-// cent more or less.
-__device__ __forceinline__ int border_step(const Row &r, bool by_mass, double target, u64 &before, float &upto)
+static constexpr int kEach = kSteps / kThreads;  // steps a thread
+
+// The step in which the running value of the histogram reaches the target, which is top_k, or top_p of the whole; kSteps where it never does.
+// own: the thread's steps.  before: the running value in front of the step.  upto: how many tokens the steps up to it hold, by weight only
+// about: a token of step i weighs 2^f exp(-(i + 1/2) / 32), two per cent more or less.
+__device__ __forceinline__ int border_step(const Row &r, bool by_mass, const u64 (&own)[kEach], double &target, u64 &before, float &upto)
 {
-    static constexpr int kEach = kSteps / kThreads;
     Shared &sh = shared();
     const int at = threadIdx.x * kEach;
-    u64 own[kEach], mine = 0;
+    u64 mine = 0;
 #pragma unroll
-    for (int i = 0; i < kEach; ++i) {
-        own[i] = 0;
-#pragma unroll
-        for (int c = 0; c < kCopies; ++c) own[i] += sh.histogram[(at + i) * kCopies + c];
-        mine += own[i];
-    }
+    for (int i = 0; i < kEach; ++i) mine += own[i];
     u64 run = block_scan(mine);
     if (threadIdx.x == 0) sh.digit = kSteps;
+    if (threadIdx.x == kThreads - 1) sh.before = run + mine;
+    __syncthreads();
+    if (by_mass) target *= (double)sh.before;
     __syncthreads();
 #pragma unroll
     for (int i = 0; i < kEach; ++i) {
@@ -362,135 +362,314 @@ __device__ __forceinline__ u64 border_candidate(const Row &r, bool by_mass, int 
     return sh.candidate[last];
 }
 
-// A block a row.
+// A row's settings.
+struct Plan {
+    Row r;
+    int top_k;
+    double top_p, min_p;
+    bool none, only_first;   // nothing can be drawn; the first of the order alone stays
+    bool by_count, by_mass;  // top-k, top-p leave something out
+};
+__device__ __forceinline__ Plan plan_of(const SampleParams &p, int b, float largest)
+{
+    Plan q;
+    const float temperature = p.temperature ? p.temperature[b] : 1.f;
+    q.top_k = p.top_k ? p.top_k[b] : 0;
+    q.top_p = p.top_p ? p.top_p[b] : 1.f;
+    q.min_p = p.min_p ? p.min_p[b] : 0.f;
+    q.none = largest == -INFINITY;
+    q.only_first = !(temperature > 0.f) || q.min_p > 1.0 || q.top_k == 1 || !(q.top_p > 0.0);
+    q.by_count = q.top_k > 0 && q.top_k < p.V;
+    q.by_mass = q.top_p < 1.0;
+    q.r = {largest, fminf(32.f / temperature, 3e38f), largest < INFINITY ? (double)largest : 1e300, 1.44269504088896340736 / (double)temperature,
+           (double)(1ull << p.bits)};
+    return q;
+}
+
+// The largest logit of the tokens from .. to: four vectors of a thread in flight, an instruction a token.
 template <bool BF16>
+__device__ __forceinline__ float largest_of(const char *row, int from, int to)
+{
+    static constexpr int kN = Vec<BF16>::kN, kFlight = 4;
+    const int vectors = (to + kN - 1) / kN, tid = threadIdx.x;
+    float largest = -INFINITY;
+    for (int base = from / kN + tid; base < vectors; base += kThreads * kFlight) {
+        Vec<BF16> x[kFlight];
+#pragma unroll
+        for (int u = 0; u < kFlight; ++u) x[u] = load_vec<BF16>(row, min(base + u * kThreads, vectors) * kN, to);
+#pragma unroll
+        for (int u = 0; u < kFlight; ++u)
+#pragma unroll
+            for (int j = 0; j < kN; ++j) largest = fmaxf(largest, x[u].raw(j));  // of a number and a NaN the number
+    }
+#pragma unroll
+    for (int off = 32; off >= 1; off >>= 1) largest = fmaxf(largest, __shfl_xor(largest, off, 64));
+    float *wave_top = reinterpret_cast<float *>(shared().sum);
+    if ((tid & 63) == 0) wave_top[tid >> 6] = largest;
+    __syncthreads();
+#pragma unroll
+    for (int w = 0; w < kWaves; ++w) largest = fmaxf(largest, wave_top[w]);
+    __syncthreads();
+    return largest + 0.f;  // -0 is 0
+}
+
+// Adds the tokens from .. to that are not below the cut to a cleared histogram.
+template <bool BF16>
+__device__ __forceinline__ void fill_histogram(const char *row, int from, int to, const Row &r, bool by_mass, u64 cut)
+{
+    Shared &sh = shared();
+    __syncthreads();
+    for (int i = threadIdx.x; i < kSteps * kCopies; i += kThreads) sh.histogram[i] = 0;
+    __syncthreads();
+    u64 *const own = sh.histogram + (threadIdx.x & (kCopies - 1));
+    const auto below = [&](float most) { return !(most > -INFINITY) || (cut && most < logit_of((uint32_t)(cut >> 32))); };
+    if (by_mass)
+        over_row<BF16>(row, from, to, below, [&](float v, int i) {
+            u64 w = whole(r, weight(r, v, sh.roots));
+            w = pack(key_of(v), i) < cut ? 0 : w;
+            atomicAdd(own + step_of(r, v) * kCopies, w);
+        }, [](int) {});
+    else
+        // -infinity counts in the last step: where that makes it the border, it holds fewer candidates, and all stay
+        over_row<BF16>(row, from, to, below, [&](float v, int) { atomicAdd(own + step_of(r, v) * kCopies, 1ull); }, [](int) {});
+    __syncthreads();
+}
+
+// Of the tokens from .. to, those of step hi, or of all up to it, from the cut on become candidates (sh.n of them; it may be more than there is
+// room for).  sum_up: what is not a candidate and surely stays by weight is summed by segments of the row.
+template <bool BF16>
+__device__ __forceinline__ int gather(const char *row, int from, int to, const Plan &q, u64 cut, int hi, bool only_hi, bool sum_up, u64 *segment)
+{
+    Shared &sh = shared();
+    const Row &r = q.r;
+    __syncthreads();
+    if (threadIdx.x == 0) sh.n = 0;
+    __syncthreads();
+    u64 kept = 0;
+    const auto beyond = [&](float most) { return hi < kSteps - 1 && (r.largest - most) * r.steps >= (float)(hi + 1); };  // in a step after hi
+    over_row<BF16>(row, from, to, beyond, [&](float v, int i) {
+        const int s = step_of(r, v);
+        const u64 c = pack(key_of(v), i);
+        const bool in = v > -INFINITY && s <= hi && c >= cut;
+        if (in && (s == hi || !only_hi)) {
+            const uint32_t at = atomicAdd(&sh.n, 1u);
+            if (at < (uint32_t)kCandidates) sh.candidate[at] = c;
+        } else if (sum_up) {
+            const double w = weight(r, v, sh.roots);
+            kept += in && w >= q.min_p ? whole(r, w) : 0;
+        }
+    }, [&](int at) {
+        if (!sum_up) return;
+        u64 sum = kept;
+#pragma unroll
+        for (int off = 32; off >= 1; off >>= 1) sum += __shfl_xor(sum, off, 64);
+        if ((threadIdx.x & 63) == 0 && at * Vec<BF16>::kN < to) segment[at / 64] = sum;
+        kept = 0;
+    });
+    __syncthreads();
+    return (int)sh.n;
+}
+
+// What stays of the tokens from .. to, summed by segments of the row.
+template <bool BF16>
+__device__ __forceinline__ void sum_segments(const char *row, int from, int to, const Plan &q, u64 cut, u64 *segment)
+{
+    u64 kept = 0;
+    const auto below = [&](float most) { return !(most > -INFINITY) || (cut && most < logit_of((uint32_t)(cut >> 32))); };
+    over_row<BF16>(row, from, to, below, [&](float v, int i) {
+        if (pack(key_of(v), i) < cut) return;
+        const double w = weight(q.r, v, shared().roots);
+        kept += w >= q.min_p ? whole(q.r, w) : 0;
+    }, [&](int at) {
+        u64 sum = kept;
+#pragma unroll
+        for (int off = 32; off >= 1; off >>= 1) sum += __shfl_xor(sum, off, 64);
+        if ((threadIdx.x & 63) == 0 && at * Vec<BF16>::kN < to) segment[at / 64] = sum;
+        kept = 0;
+    });
+}
+
+// Where there are few rows, several blocks share one: three kernels fill a row's RowWork, a chunk of the row a block, before sample_kernel
+// goes on with what is left of it.  (One row of 128000 tokens: 75 us by one block, 42 of them the histogram.)
+static constexpr int kMaxChunks = 64;
+struct RowWork {
+    float largest[kMaxChunks];       // of every chunk
+    uint32_t n, pad[63];             // candidates
+    u64 histogram[kSteps];
+    u64 candidate[kCandidates];
+    u64 segment[kSegments];
+};
+
+__device__ __forceinline__ RowWork &work_of(const SampleParams &p, int b) { return reinterpret_cast<RowWork *>(p.work)[b]; }
+__device__ __forceinline__ float largest_of_row(const SampleParams &p, int b)
+{
+    float largest = -INFINITY;
+    for (int c = 0; c < p.chunks; ++c) largest = fmaxf(largest, work_of(p, b).largest[c]);
+    return largest;
+}
+template <bool BF16>
+__device__ __forceinline__ const char *row_of(const SampleParams &p, int b)
+{
+    return static_cast<const char *>(p.logits) + (int64_t)b * p.stride * (BF16 ? 2 : 4);
+}
+
+template <bool BF16>
+__global__ __launch_bounds__(kThreads) void sample_largest_kernel(SampleParams p)
+{
+    const int c = blockIdx.x, b = blockIdx.y, from = c * p.chunk;
+    RowWork &work = work_of(p, b);
+    for (int i = c * kThreads + threadIdx.x; i < kSteps; i += p.chunks * kThreads) work.histogram[i] = 0;
+    if (c == 0 && threadIdx.x == 0) work.n = 0;
+    const float largest = largest_of<BF16>(row_of<BF16>(p, b), from, min(p.V, from + p.chunk));
+    if (threadIdx.x == 0) work.largest[c] = largest;
+}
+
+template <bool BF16>
+__global__ __launch_bounds__(kThreads) void sample_histogram_kernel(SampleParams p)
+{
+    Shared &sh = shared();
+    const int c = blockIdx.x, b = blockIdx.y, tid = threadIdx.x, from = c * p.chunk, to = min(p.V, from + p.chunk);
+    RowWork &work = work_of(p, b);
+    const Plan q = plan_of(p, b, largest_of_row(p, b));
+    if (q.none || q.only_first) return;
+    if (tid < 32) sh.roots[tid] = kRoots[tid];
+    __syncthreads();
+    if (!q.by_count && !q.by_mass) {
+        sum_segments<BF16>(row_of<BF16>(p, b), from, to, q, 0, work.segment);
+        return;
+    }
+    fill_histogram<BF16>(row_of<BF16>(p, b), from, to, q.r, !q.by_count, 0);
+    for (int i = tid; i < kSteps; i += kThreads) {
+        u64 sum = 0;
+#pragma unroll
+        for (int k = 0; k < kCopies; ++k) sum += sh.histogram[i * kCopies + k];
+        if (sum) atomicAdd(&work.histogram[i], sum);
+    }
+}
+
+// The border step of a row's first filter, as all its blocks find it: from the same whole numbers.
+__device__ __forceinline__ int border_of_work(const RowWork &work, const Plan &q, double &target, u64 &before, bool &all)
+{
+    u64 own[kEach];
+#pragma unroll
+    for (int i = 0; i < kEach; ++i) own[i] = work.histogram[threadIdx.x * kEach + i];
+    float upto;
+    target = q.by_count ? (double)q.top_k : q.top_p;
+    const int s = border_step(q.r, !q.by_count, own, target, before, upto);
+    all = upto <= 0.95f * kCandidates;
+    return s;
+}
+
+template <bool BF16>
+__global__ __launch_bounds__(kThreads) void sample_gather_kernel(SampleParams p)
+{
+    Shared &sh = shared();
+    const int c = blockIdx.x, b = blockIdx.y, tid = threadIdx.x, from = c * p.chunk, to = min(p.V, from + p.chunk);
+    RowWork &work = work_of(p, b);
+    const Plan q = plan_of(p, b, largest_of_row(p, b));
+    if (q.none || q.only_first || (!q.by_count && !q.by_mass)) return;
+    if (tid < 32) sh.roots[tid] = kRoots[tid];
+    double target;
+    u64 before;
+    bool all;
+    const int s = border_of_work(work, q, target, before, all);
+    if (s == kSteps) return;
+    const int n = gather<BF16>(row_of<BF16>(p, b), from, to, q, 0, s, !all, !all && !q.by_count, work.segment);
+    if (tid == 0) sh.digit = atomicAdd(&work.n, (uint32_t)n);
+    __syncthreads();
+    const uint32_t first = sh.digit;
+    for (int i = tid; i < min(n, kCandidates); i += kThreads)
+        if (first + i < (uint32_t)kCandidates) work.candidate[first + i] = sh.candidate[i];
+}
+
+// A block a row.
+template <bool BF16, bool SHARED_ROW>
 __global__ __launch_bounds__(kThreads) void sample_kernel(SampleParams p)
 {
     Shared &sh = shared();
     const int b = blockIdx.x, tid = threadIdx.x, lane = tid & 63;
-    const char *row = static_cast<const char *>(p.logits) + (int64_t)b * p.stride * (BF16 ? 2 : 4);
-    const auto nothing = [](int) {};
-
+    const char *row = row_of<BF16>(p, b);
     if (tid < 32) sh.roots[tid] = kRoots[tid];
-    // the largest logit: four vectors of a thread in flight, an instruction a token
-    float largest = -INFINITY;
-    {
-        static constexpr int kN = Vec<BF16>::kN, kFlight = 4;
-        const int vectors = (p.V + kN - 1) / kN;
-        for (int base = tid; base < vectors; base += kThreads * kFlight) {
-            Vec<BF16> x[kFlight];
-#pragma unroll
-            for (int u = 0; u < kFlight; ++u) x[u] = load_vec<BF16>(row, min(base + u * kThreads, vectors) * kN, p.V);
-#pragma unroll
-            for (int u = 0; u < kFlight; ++u)
-#pragma unroll
-                for (int j = 0; j < kN; ++j) largest = fmaxf(largest, x[u].raw(j));  // of a number and a NaN the number
-        }
-    }
-#pragma unroll
-    for (int off = 32; off >= 1; off >>= 1) largest = fmaxf(largest, __shfl_xor(largest, off, 64));
-    float *wave_top = reinterpret_cast<float *>(sh.sum);
-    if (lane == 0) wave_top[tid >> 6] = largest;
     if (tid == 0) sh.token = 0x7fffffff;
     __syncthreads();
-#pragma unroll
-    for (int w = 0; w < kWaves; ++w) largest = fmaxf(largest, wave_top[w]);
-    largest += 0.f;
-    const float temperature = p.temperature ? p.temperature[b] : 1.f;
-    const bool greedy = !(temperature > 0.f), none = largest == -INFINITY;
-    const int top_k = p.top_k ? p.top_k[b] : 0;
-    const double top_p = p.top_p ? p.top_p[b] : 1.f, min_p = p.min_p ? p.min_p[b] : 0.f;
-    const bool only_first = greedy || min_p > 1.0 || top_k == 1 || !(top_p > 0.0);  // the first of the order alone stays
-    if (none || only_first) {
-        if (!none) {
+    const float largest = SHARED_ROW ? largest_of_row(p, b) : largest_of<BF16>(row, 0, p.V);
+    const Plan q = plan_of(p, b, largest);
+    const Row &r = q.r;
+    const double min_p = q.min_p;
+    if (q.none || q.only_first) {
+        if (!q.none) {
             int first = 0x7fffffff;
-            over_row<BF16>(row, p.V, [&](float most) { return most < largest; }, [&](float v, int i) { first = v == largest && i < first ? i : first; }, nothing);
+            over_row<BF16>(row, 0, p.V, [&](float most) { return most < largest; }, [&](float v, int i) { first = v == largest && i < first ? i : first; }, [](int) {});
             if (first != 0x7fffffff) atomicMin(&sh.token, first);
         }
         __syncthreads();
         if (tid == 0) {
-            p.token[b] = none ? -1 : sh.token;
-            if (p.logprob) p.logprob[b] = none ? -INFINITY : 0.f;
+            p.token[b] = q.none ? -1 : sh.token;
+            if (p.logprob) p.logprob[b] = q.none ? -INFINITY : 0.f;
         }
         return;
     }
-    const Row r = {largest, fminf(32.f / temperature, 3e38f), largest < INFINITY ? (double)largest : 1e300, 1.44269504088896340736 / (double)temperature, (double)(1ull << p.bits)};
     const int segments = ceil_div(p.V, 64 * Vec<BF16>::kN);
-    u64 cut = 0;        // tokens from this pair on stay
-    int n = 0;          // candidates
-    bool all = false;   // they are all that may stay
-    const auto below = [&](float most) { return !(most > -INFINITY) || (cut && most < logit_of((uint32_t)(cut >> 32))); };  // all below the cut
-    // The tokens of step hi, or of all up to it, from the cut on as candidates; their number may be more than there is room for.  What is not a
-    // candidate and surely stays by weight is summed by segments of the row on the way.
-    const auto gather = [&](int hi, bool only_hi, bool sum_up) {
-        __syncthreads();
-        if (tid == 0) sh.n = 0;
-        __syncthreads();
-        u64 kept = 0;
-        const auto beyond = [&](float most) { return hi < kSteps - 1 && (r.largest - most) * r.steps >= (float)(hi + 1); };  // in a step after hi
-        over_row<BF16>(row, p.V, beyond, [&](float v, int i) {
-            const int s = step_of(r, v);
-            const u64 c = pack(key_of(v), i);
-            const bool in = v > -INFINITY && s <= hi && c >= cut;
-            if (in && (s == hi || !only_hi)) {
-                const uint32_t at = atomicAdd(&sh.n, 1u);
-                if (at < (uint32_t)kCandidates) sh.candidate[at] = c;
-            } else if (sum_up) {
-                const double w = weight(r, v, sh.roots);
-                kept += in && w >= min_p ? whole(r, w) : 0;
-            }
-        }, [&](int at) {
-            if (!sum_up) return;
-            u64 sum = kept;
-#pragma unroll
-            for (int off = 32; off >= 1; off >>= 1) sum += __shfl_xor(sum, off, 64);
-            if (lane == 0 && at / 64 < segments) sh.segment[at / 64] = sum;
-            kept = 0;
-        });
-        __syncthreads();
-        return (int)sh.n;
-    };
+    u64 cut = 0;          // tokens from this pair on stay
+    int n = 0;            // candidates
+    bool all = false;     // they are all that may stay
+    bool summed = false;  // the segments hold what stays in front of the border step
     const auto weigh = [&](u64 c) { return weight(r, logit_of((uint32_t)(c >> 32)), sh.roots); };
 
-    bool summed = false;  // the segments hold what stays in front of the border step
     // first by count, then by weight; in one loop, so that there is one copy of what they share
 #pragma unroll 1
     for (int stage = 0; stage < 2; ++stage) {
         const bool by_mass = stage == 1;
-        if (by_mass ? !(top_p < 1.0) : !(top_k > 0 && top_k < p.V)) continue;
-        double target = (double)top_k;
-        u64 before = 0, mine = 0;
+        if (by_mass ? !q.by_mass : !q.by_count) continue;
+        double target = by_mass ? q.top_p : (double)q.top_k;
+        u64 before = 0;
         int s = 0;
         if (all) {  // by weight, of the candidates that top-k left
+            u64 mine = 0;
             for (int i = tid; i < n; i += kThreads) mine += sh.candidate[i] >= cut ? whole(r, weigh(sh.candidate[i])) : 0;
-            target = top_p * (double)block_sum(mine);
+            target = q.top_p * (double)block_sum(mine);
         } else {
-            __syncthreads();
-            for (int i = tid; i < kSteps * kCopies; i += kThreads) sh.histogram[i] = 0;
-            __syncthreads();
-            u64 *const own = sh.histogram + (lane & (kCopies - 1));
-            if (by_mass)
-                over_row<BF16>(row, p.V, below, [&](float v, int i) {
-                    u64 w = whole(r, weight(r, v, sh.roots));
-                    w = pack(key_of(v), i) < cut ? 0 : w;
-                    mine += w;
-                    atomicAdd(own + step_of(r, v) * kCopies, w);
-                }, nothing);
-            else
-                // -infinity counts in the last step: where that makes it the border, it holds fewer candidates, and all stay
-                over_row<BF16>(row, p.V, below, [&](float v, int) { atomicAdd(own + step_of(r, v) * kCopies, 1ull); }, nothing);
-            const u64 sum = block_sum(mine);
-            if (by_mass) target = top_p * (double)sum;
-            float upto;
-            s = border_step(r, by_mass, target, before, upto);
-            if (s == kSteps) continue;  // fewer tokens than top_k
-            all = upto <= 0.95f * kCandidates;
-            summed = !all && by_mass;
-            n = gather(s, !all, summed);
-            if (all && n > kCandidates) {  // the estimate was wrong
+            const bool done = SHARED_ROW && !(by_mass && q.by_count);  // the first filter: other blocks have gathered the candidates
+            if (done) {
+                s = border_of_work(work_of(p, b), q, target, before, all);
+            } else {
+                fill_histogram<BF16>(row, 0, p.V, r, by_mass, cut);
+                u64 own[kEach];
+#pragma unroll
+                for (int i = 0; i < kEach; ++i) {
+                    own[i] = 0;
+#pragma unroll
+                    for (int c = 0; c < kCopies; ++c) own[i] += sh.histogram[(tid * kEach + i) * kCopies + c];
+                }
+                float upto;
+                s = border_step(r, by_mass, own, target, before, upto);
+                all = upto <= 0.95f * kCandidates;
+            }
+            if (s == kSteps) {  // fewer tokens than top_k
                 all = false;
-                summed = by_mass;
-                n = gather(s, true, summed);
+                continue;
+            }
+            summed = !all && by_mass;
+            if (done) {
+                const RowWork &work = work_of(p, b);
+                n = (int)work.n;
+                for (int i = tid; i < min(n, kCandidates); i += kThreads) sh.candidate[i] = work.candidate[i];
+                __syncthreads();
+                if (summed)
+                    for (int i = tid; i < segments; i += kThreads) sh.segment[i] = work.segment[i];
+                __syncthreads();
+            }
+            if (!done || (all && n > kCandidates)) {
+                if (done) {  // the estimate was wrong
+                    all = false;
+                    summed = by_mass;
+                }
+                n = gather<BF16>(row, 0, p.V, q, cut, s, !all, summed, sh.segment);
+                if (all && n > kCandidates) {  // as above
+                    all = false;
+                    summed = by_mass;
+                    n = gather<BF16>(row, 0, p.V, q, cut, s, true, summed, sh.segment);
+                }
             }
             if (all) before = 0;
             if (n == 0) continue;
@@ -511,23 +690,14 @@ __global__ __launch_bounds__(kThreads) void sample_kernel(SampleParams p)
             const double w = weigh(c);
             if (c >= cut && w >= min_p) atomicAdd(&sh.segment[(int)~(uint32_t)c / (64 * Vec<BF16>::kN)], whole(r, w));
         }
+    } else if (SHARED_ROW && !q.by_count && !q.by_mass) {
+        for (int i = tid; i < segments; i += kThreads) sh.segment[i] = work_of(p, b).segment[i];
     } else {
-        u64 kept = 0;
-        over_row<BF16>(row, p.V, below, [&](float v, int i) {
-            if (v == -INFINITY || pack(key_of(v), i) < cut) return;
-            const double w = weight(r, v, sh.roots);
-            if (w >= min_p) kept += whole(r, w);
-        }, [&](int at) {
-            u64 sum = kept;
-#pragma unroll
-            for (int off = 32; off >= 1; off >>= 1) sum += __shfl_xor(sum, off, 64);
-            if (lane == 0 && at / 64 < segments) sh.segment[at / 64] = sum;
-            kept = 0;
-        });
+        sum_segments<BF16>(row, 0, p.V, q, cut, sh.segment);
     }
     __syncthreads();
     // the segment, and in it the token, at which the running sum passes u times the sum
-    static constexpr int kEach = (kSegments + kThreads - 1) / kThreads;
+    static_assert(kSegments == kSteps, "as many segments a thread as steps");
     u64 mine = 0;
     u64 own[kEach];
 #pragma unroll
@@ -586,19 +756,56 @@ __global__ __launch_bounds__(kThreads) void sample_kernel(SampleParams p)
     }
 }
 
+int set_lds(const void *kernel)
+{
+    MOE_HIP_CHECK(hipFuncSetAttribute(kernel, hipFuncAttributeMaxDynamicSharedMemorySize, (int)sizeof(Shared)));
+    return MOE_OK;
+}
+
 template <bool BF16>
 int launch_as(const SampleParams &p, hipStream_t s)
 {
     static std::once_flag once;
-    static hipError_t setup_rc = hipSuccess;
+    static int setup_rc = MOE_OK;
     std::call_once(once, [&]() {
-        setup_rc = hipFuncSetAttribute(reinterpret_cast<const void *>(sample_kernel<BF16>), hipFuncAttributeMaxDynamicSharedMemorySize, (int)sizeof(Shared));
+        for (const void *kernel : {reinterpret_cast<const void *>(sample_kernel<BF16, false>), reinterpret_cast<const void *>(sample_kernel<BF16, true>),
+                                   reinterpret_cast<const void *>(sample_largest_kernel<BF16>), reinterpret_cast<const void *>(sample_histogram_kernel<BF16>),
+                                   reinterpret_cast<const void *>(sample_gather_kernel<BF16>)})
+            if (setup_rc == MOE_OK) setup_rc = set_lds(kernel);
     });
-    MOE_HIP_CHECK(setup_rc);
+    if (setup_rc != MOE_OK) {
+        set_error("moe_sample: the device refuses %d bytes of LDS", (int)sizeof(Shared));
+        return setup_rc;
+    }
+    if (p.chunks > 1) {
+        const dim3 grid(p.chunks, p.B);
+        {
+            ProfScope ps("sample_largest", s);
+            hipLaunchKernelGGL(sample_largest_kernel<BF16>, grid, dim3(kThreads), sizeof(Shared), s, p);
+            MOE_LAUNCH_CHECK("sample_largest_kernel");
+        }
+        {
+            ProfScope ps("sample_histogram", s);
+            hipLaunchKernelGGL(sample_histogram_kernel<BF16>, grid, dim3(kThreads), sizeof(Shared), s, p);
+            MOE_LAUNCH_CHECK("sample_histogram_kernel");
+        }
+        ProfScope ps("sample_gather", s);
+        hipLaunchKernelGGL(sample_gather_kernel<BF16>, grid, dim3(kThreads), sizeof(Shared), s, p);
+        MOE_LAUNCH_CHECK("sample_gather_kernel");
+    }
     ProfScope ps("sample", s);
-    hipLaunchKernelGGL(sample_kernel<BF16>, dim3(p.B), dim3(kThreads), sizeof(Shared), s, p);
+    if (p.chunks > 1) hipLaunchKernelGGL((sample_kernel<BF16, true>), dim3(p.B), dim3(kThreads), sizeof(Shared), s, p);
+    else hipLaunchKernelGGL((sample_kernel<BF16, false>), dim3(p.B), dim3(kThreads), sizeof(Shared), s, p);
     MOE_LAUNCH_CHECK("sample_kernel");
     return MOE_OK;
+}
+
+// Blocks of a row: so many that the rows together give 512 (a CU holds one), of 8192 tokens and more, which is a row's fixed cost in each.
+int chunks_for(int B, int V)
+{
+    int chunks = 512 / (B > 0 ? B : 1);
+    if (chunks > V / 8192) chunks = V / 8192;
+    return chunks < 1 ? 1 : chunks > kMaxChunks ? kMaxChunks : chunks;
 }
 
 }  // namespace
@@ -609,11 +816,12 @@ int launch_sample(const void *logits, int dtype, int64_t stride, int B, int V, c
     int bits = 62;
     while ((1ll << (62 - bits)) < V) --bits;
     bits = bits < 50 ? bits : 50;
-    const SampleParams p = {logits, stride, B, V, bits, u, temperature, top_p, min_p, top_k, token, logprob};
-    (void)ws;
+    // chunks begin at whole vectors of all threads
+    const int chunk = (int)align_up(ceil_div(V, chunks_for(B, V)), 8192);
+    const SampleParams p = {logits, stride, B, V, bits, u, temperature, top_p, min_p, top_k, token, logprob, ceil_div(V, chunk), chunk, static_cast<uint8_t *>(ws)};
     return dtype == MOE_DTYPE_BF16 ? launch_as<true>(p, s) : launch_as<false>(p, s);
 }
 
-int64_t sample_workspace(int B, int V) { return 256 + 0 * (int64_t)B * V; }
+int64_t sample_workspace(int B, int V) { return 256 + (chunks_for(B, V) > 1 ? (int64_t)B * (int64_t)sizeof(RowWork) : 0); }
 
 }  // namespace moe355

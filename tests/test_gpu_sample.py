@@ -93,7 +93,7 @@ def test_infinities_and_nan():
         check(x, u, **kw)
 
 
-@pytest.mark.parametrize("B,V", [(1, 128000), (3, 1 << 19), (130, 9001)])
+@pytest.mark.parametrize("B,V", [(1, 128000), (3, 1 << 19), (130, 9001), (5, 50001), (40, 33000)])
 def test_sizes(B, V):
     x, rng = logits_of(B, V, torch.float32, B)
     u = rng.random(B).astype(np.float32)
