@@ -2,7 +2,7 @@
 //
 // All filters keep a beginning of one order (descending logit, ascending index), so a row's kept set is one threshold on the pair
 // (key: the logit's bits, made to order like the logit; index).  It is found without sorting the row: a histogram over 2048 steps of
-// 1/32 in (largest - logit) / temperature, of counts for top-k and of weights for top-p, says which step holds the border.  Where the
+// 1/64 in (largest - logit) / temperature, of counts for top-k and of weights for top-p, says which step holds the border.  Where the
 // tokens down to that step are few (kCandidates), they alone are sorted, and all that is left happens on them; where they are many, the
 // ones of the border step alone; where these are too many as well (a flat or a very wide row), a radix walk over the pairs settles
 // it, 8 bits a pass over the row.
@@ -10,6 +10,8 @@
 // Weights are exp in 64 bits, summed as whole numbers of 2^-f (f = 62 - ceil(log2 V), at most 50): sums of whole numbers do not depend on
 // their order, so atomic sums give one result, and an error of V 2^-(f+1) at most, under 1e-11 of the sum for the usual V.
 // The token at the border of a cumulative sum then is the one that sums in 64 bits choose.
+#include <stddef.h>
+
 #include <mutex>
 
 #include "moe_internal.h"
@@ -51,6 +53,13 @@ struct Vec {
         return BF16 ? __uint_as_float(j & 1 ? w[j >> 1] & 0xffff0000u : w[j >> 1] << 16) : __uint_as_float(w[j & 3]);
     }
     __device__ __forceinline__ float operator[](int j) const { return clean(raw(j)); }
+    __device__ __forceinline__ float largest() const
+    {
+        float most = raw(0);
+#pragma unroll
+        for (int j = 1; j < kN; ++j) most = fmaxf(most, raw(j));
+        return most;
+    }
 };
 template <bool BF16>
 __device__ __forceinline__ Vec<BF16> load_vec(const char *row, int i, int V)
@@ -135,16 +144,17 @@ static constexpr int kThreads = 1024, kWaves = kThreads / 64, kSteps = 2048, kCa
 static constexpr int kCopies = 4;
 
 struct Shared {
-    union {
-        u64 histogram[kSteps * kCopies];  // counts or weights; then
-        u64 segment[kSegments];           // the kept weights of every 64 vectors of the row
-    };
-    u64 candidate[kCandidates];
     u64 sum[kWaves];
     double roots[32];                     // kRoots: lanes ask for different ones
     uint32_t n, digit;
     u64 before;
     int token;
+    alignas(16) union {
+        u64 histogram[kSteps * kCopies];  // counts or weights; then
+        u64 segment[kSegments];           // the kept weights of every 64 vectors of the row
+        u64 list[kCandidates];            // or, in a kernel that has only them, candidates
+    };
+    u64 candidate[kCandidates];
 };
 
 // The block's LDS.  Every function is inlined and asks for it itself: behind a reference the compiler may not know that it is LDS and
@@ -195,11 +205,10 @@ __device__ __forceinline__ u64 block_scan(u64 mine)
     return front + x - mine;
 }
 
-// f(v, index) for every token from `from` (a multiple of 64 vectors) to `to`, -infinity for places past it; after each vector done(its
-// number).  A thread has the next two vectors in flight, and the work of four tokens at most is mixed by the compiler: with more of it in
-// registers the 64-bit arithmetic spills.  skip(largest logit of a vector): whether f need not see the vector.
-template <bool BF16, typename S, typename F, typename G>
-__device__ __forceinline__ void over_row(const char *row, int from, int to, S skip, F f, G done)
+// f(vector, its number) for the vectors of the tokens from `from` (a multiple of 64 vectors) to `to`, -infinity for places past it.  A thread
+// has the next two vectors in flight.  f is called by whole waves.
+template <bool BF16, typename F>
+__device__ __forceinline__ void over_vectors(const char *row, int from, int to, F f)
 {
     static constexpr int kN = Vec<BF16>::kN, kFlight = 2;
     const int vectors = (to + kN - 1) / kN, mine = from / kN + (int)threadIdx.x;
@@ -207,25 +216,33 @@ __device__ __forceinline__ void over_row(const char *row, int from, int to, S sk
 #pragma unroll
     for (int u = 0; u < kFlight; ++u) x[u] = load_vec<BF16>(row, min(mine + u * kThreads, vectors) * kN, to);
 #pragma unroll 1
-    for (int base = 0; from / kN + base < vectors; base += kFlight * kThreads) {  // the same count for all threads: done() may use the whole wave
+    for (int base = 0; from / kN + base < vectors; base += kFlight * kThreads) {
 #pragma unroll
         for (int u = 0; u < kFlight; ++u) {
             const int at = mine + base + u * kThreads;
             const Vec<BF16> now = x[u];
             x[u] = load_vec<BF16>(row, min(at + kFlight * kThreads, vectors) * kN, to);
-            float most = now.raw(0);
-#pragma unroll
-            for (int j = 1; j < kN; ++j) most = fmaxf(most, now.raw(j));
-            if (!skip(most)) {
-#pragma unroll
-                for (int j = 0; j < kN; ++j) {
-                    f(now[j], at * kN + j);
-                    if (j % 4 == 3) __builtin_amdgcn_sched_barrier(0);
-                }
-            }
-            done(at);
+            f(now, at);
         }
     }
+}
+
+// f(v, index) for every token; skip(largest logit of a vector): whether f need not see the vector; after each vector done(its number).  The work
+// of four tokens at most is mixed by the compiler: with more of it in registers the 64-bit arithmetic spills.
+template <bool BF16, typename S, typename F, typename G>
+__device__ __forceinline__ void over_row(const char *row, int from, int to, S skip, F f, G done)
+{
+    static constexpr int kN = Vec<BF16>::kN;
+    over_vectors<BF16>(row, from, to, [&](const Vec<BF16> &now, int at) {
+        if (!skip(now.largest())) {
+#pragma unroll
+            for (int j = 0; j < kN; ++j) {
+                f(now[j], at * kN + j);
+                if (j % 4 == 3) __builtin_amdgcn_sched_barrier(0);
+            }
+        }
+        done(at);
+    });
 }
 
 // The border of a step that holds too many tokens to sort, `before` in front of the step: walks the step's pairs from the cut on, 8 bits
@@ -311,7 +328,7 @@ static constexpr int kEach = kSteps / kThreads;  // steps a thread
 
 // The step in which the running value of the histogram reaches the target, which is top_k, or top_p of the whole; kSteps where it never does.
 // own: the thread's steps.  before: the running value in front of the step.  upto: how many tokens the steps up to it hold, by weight only
-// about: a token of step i weighs 2^f exp(-(i + 1/2) / 32), two per cent more or less.
+// about: a token of step i weighs 2^f exp(-(i + 1/2) / 64), a per cent more or less.
 __device__ __forceinline__ int border_step(const Row &r, bool by_mass, const u64 (&own)[kEach], double &target, u64 &before, float &upto)
 {
     Shared &sh = shared();
@@ -339,7 +356,7 @@ __device__ __forceinline__ int border_step(const Row &r, bool by_mass, const u64
     float tokens = 0.f;
 #pragma unroll
     for (int i = 0; i < kEach; ++i)
-        if (at + i <= s) tokens += by_mass ? (float)own[i] / (float)r.unit * __expf(fminf((float)(at + i) * 0.03125f + 0.015625f, 80.f)) : (float)own[i];
+        if (at + i <= s) tokens += by_mass ? (float)own[i] / (float)r.unit * __expf(fminf((float)(at + i) * 0.015625f + 0.0078125f, 80.f)) : (float)own[i];
     tokens = fminf(tokens, 1e9f);
     upto = (float)block_sum((u64)tokens);
     return s;
@@ -349,10 +366,11 @@ __device__ __forceinline__ int border_step(const Row &r, bool by_mass, const u64
 __device__ __forceinline__ u64 border_candidate(const Row &r, bool by_mass, int n, double target, u64 before)
 {
     Shared &sh = shared();
+    if (!by_mass) return sh.candidate[min(n, (int)((u64)target - before)) - 1];
     int last = 0;
     for (int base = 0; base < n; base += kThreads) {
         const int i = base + threadIdx.x;
-        const u64 mine = i >= n ? 0 : by_mass ? whole(r, weight(r, logit_of((uint32_t)(sh.candidate[i] >> 32)), sh.roots)) : 1;
+        const u64 mine = i >= n ? 0 : whole(r, weight(r, logit_of((uint32_t)(sh.candidate[i] >> 32)), sh.roots));
         const u64 at = before + block_scan(mine);
         const int stay = (int)block_sum(i < n && (double)at < target ? 1 : 0);
         if (stay > 0) last = base + stay - 1;
@@ -361,6 +379,10 @@ __device__ __forceinline__ u64 border_candidate(const Row &r, bool by_mass, int 
     }
     return sh.candidate[last];
 }
+
+// Whether the tokens up to the border step are few enough to sort.  By weight, what is not sorted costs little (it is summed while the border
+// step's tokens are gathered); by count it costs top-p a histogram of its own.  (512 candidates to sort: 5 us, 4096: 18.)
+__device__ __forceinline__ bool few(bool by_mass, float upto) { return upto <= (by_mass ? 512.f : 0.95f * kCandidates); }
 
 // A row's settings.
 struct Plan {
@@ -381,7 +403,7 @@ __device__ __forceinline__ Plan plan_of(const SampleParams &p, int b, float larg
     q.only_first = !(temperature > 0.f) || q.min_p > 1.0 || q.top_k == 1 || !(q.top_p > 0.0);
     q.by_count = q.top_k > 0 && q.top_k < p.V;
     q.by_mass = q.top_p < 1.0;
-    q.r = {largest, fminf(32.f / temperature, 3e38f), largest < INFINITY ? (double)largest : 1e300, 1.44269504088896340736 / (double)temperature,
+    q.r = {largest, fminf(64.f / temperature, 3e38f), largest < INFINITY ? (double)largest : 1e300, 1.44269504088896340736 / (double)temperature,
            (double)(1ull << p.bits)};
     return q;
 }
@@ -438,32 +460,49 @@ __device__ __forceinline__ void fill_histogram(const char *row, int from, int to
 // Of the tokens from .. to, those of step hi, or of all up to it, from the cut on become candidates (sh.n of them; it may be more than there is
 // room for).  sum_up: what is not a candidate and surely stays by weight is summed by segments of the row.
 template <bool BF16>
-__device__ __forceinline__ int gather(const char *row, int from, int to, const Plan &q, u64 cut, int hi, bool only_hi, bool sum_up, u64 *segment)
+__device__ __forceinline__ int gather(const char *row, int from, int to, const Plan &q, u64 cut, int hi, bool only_hi, bool sum_up, u64 *segment, u64 *list)
 {
+    static constexpr int kN = Vec<BF16>::kN;
     Shared &sh = shared();
     const Row &r = q.r;
     __syncthreads();
     if (threadIdx.x == 0) sh.n = 0;
     __syncthreads();
     u64 kept = 0;
-    const auto beyond = [&](float most) { return hi < kSteps - 1 && (r.largest - most) * r.steps >= (float)(hi + 1); };  // in a step after hi
-    over_row<BF16>(row, from, to, beyond, [&](float v, int i) {
-        const int s = step_of(r, v);
-        const u64 c = pack(key_of(v), i);
-        const bool in = v > -INFINITY && s <= hi && c >= cut;
-        if (in && (s == hi || !only_hi)) {
-            const uint32_t at = atomicAdd(&sh.n, 1u);
-            if (at < (uint32_t)kCandidates) sh.candidate[at] = c;
-        } else if (sum_up) {
-            const double w = weight(r, v, sh.roots);
-            kept += in && w >= q.min_p ? whole(r, w) : 0;
+    over_vectors<BF16>(row, from, to, [&](const Vec<BF16> &now, int at) {
+        // in a step after hi, as most are
+        const bool beyond = hi < kSteps - 1 && (r.largest - now.largest()) * r.steps >= (float)(hi + 1);
+        if (!beyond) {
+            u64 c[kN];
+            uint32_t picked = 0;
+#pragma unroll
+            for (int j = 0; j < kN; ++j) {
+                const float v = now[j];
+                const int s = step_of(r, v);
+                c[j] = pack(key_of(v), at * kN + j);
+                const bool in = v > -INFINITY && s <= hi && c[j] >= cut, pick = in && (s == hi || !only_hi);
+                picked |= pick ? 1u << j : 0u;
+                if (sum_up) {
+                    const double w = weight(r, v, sh.roots);
+                    kept += in && !pick && w >= q.min_p ? whole(r, w) : 0;
+                    if (j % 4 == 3) __builtin_amdgcn_sched_barrier(0);
+                }
+            }
+            if (picked) {  // one sum for the vector: its result is waited for
+                uint32_t place = atomicAdd(&sh.n, (uint32_t)__popc(picked));
+#pragma unroll
+                for (int j = 0; j < kN; ++j)
+                    if (picked >> j & 1) {
+                        if (place < (uint32_t)kCandidates) list[place] = c[j];
+                        ++place;
+                    }
+            }
         }
-    }, [&](int at) {
         if (!sum_up) return;
         u64 sum = kept;
 #pragma unroll
         for (int off = 32; off >= 1; off >>= 1) sum += __shfl_xor(sum, off, 64);
-        if ((threadIdx.x & 63) == 0 && at * Vec<BF16>::kN < to) segment[at / 64] = sum;
+        if ((threadIdx.x & 63) == 0 && at * kN < to) segment[at / 64] = sum;
         kept = 0;
     });
     __syncthreads();
@@ -525,7 +564,7 @@ __global__ __launch_bounds__(kThreads) void sample_largest_kernel(SampleParams p
 }
 
 template <bool BF16>
-__global__ __launch_bounds__(kThreads) void sample_histogram_kernel(SampleParams p)
+__global__ __launch_bounds__(kThreads, 8) void sample_histogram_kernel(SampleParams p)
 {
     Shared &sh = shared();
     const int c = blockIdx.x, b = blockIdx.y, tid = threadIdx.x, from = c * p.chunk, to = min(p.V, from + p.chunk);
@@ -556,12 +595,12 @@ __device__ __forceinline__ int border_of_work(const RowWork &work, const Plan &q
     float upto;
     target = q.by_count ? (double)q.top_k : q.top_p;
     const int s = border_step(q.r, !q.by_count, own, target, before, upto);
-    all = upto <= 0.95f * kCandidates;
+    all = few(!q.by_count, upto);
     return s;
 }
 
 template <bool BF16>
-__global__ __launch_bounds__(kThreads) void sample_gather_kernel(SampleParams p)
+__global__ __launch_bounds__(kThreads, 8) void sample_gather_kernel(SampleParams p)
 {
     Shared &sh = shared();
     const int c = blockIdx.x, b = blockIdx.y, tid = threadIdx.x, from = c * p.chunk, to = min(p.V, from + p.chunk);
@@ -574,12 +613,12 @@ __global__ __launch_bounds__(kThreads) void sample_gather_kernel(SampleParams p)
     bool all;
     const int s = border_of_work(work, q, target, before, all);
     if (s == kSteps) return;
-    const int n = gather<BF16>(row_of<BF16>(p, b), from, to, q, 0, s, !all, !all && !q.by_count, work.segment);
+    const int n = gather<BF16>(row_of<BF16>(p, b), from, to, q, 0, s, !all, !all && !q.by_count, work.segment, sh.list);
     if (tid == 0) sh.digit = atomicAdd(&work.n, (uint32_t)n);
     __syncthreads();
     const uint32_t first = sh.digit;
     for (int i = tid; i < min(n, kCandidates); i += kThreads)
-        if (first + i < (uint32_t)kCandidates) work.candidate[first + i] = sh.candidate[i];
+        if (first + i < (uint32_t)kCandidates) work.candidate[first + i] = sh.list[i];
 }
 
 // A block a row.
@@ -598,8 +637,13 @@ __global__ __launch_bounds__(kThreads) void sample_kernel(SampleParams p)
     const double min_p = q.min_p;
     if (q.none || q.only_first) {
         if (!q.none) {
-            int first = 0x7fffffff;
-            over_row<BF16>(row, 0, p.V, [&](float most) { return most < largest; }, [&](float v, int i) { first = v == largest && i < first ? i : first; }, [](int) {});
+            int first = 0x7fffffff, from = 0, to = p.V;
+            if (SHARED_ROW) {  // in the first chunk that has it
+                while (work_of(p, b).largest[from] != largest) ++from;
+                from *= p.chunk;
+                to = min(p.V, from + p.chunk);
+            }
+            over_row<BF16>(row, from, to, [&](float most) { return most < largest; }, [&](float v, int i) { first = v == largest && i < first ? i : first; }, [](int) {});
             if (first != 0x7fffffff) atomicMin(&sh.token, first);
         }
         __syncthreads();
@@ -643,7 +687,7 @@ __global__ __launch_bounds__(kThreads) void sample_kernel(SampleParams p)
                 }
                 float upto;
                 s = border_step(r, by_mass, own, target, before, upto);
-                all = upto <= 0.95f * kCandidates;
+                all = few(by_mass, upto);
             }
             if (s == kSteps) {  // fewer tokens than top_k
                 all = false;
@@ -664,11 +708,11 @@ __global__ __launch_bounds__(kThreads) void sample_kernel(SampleParams p)
                     all = false;
                     summed = by_mass;
                 }
-                n = gather<BF16>(row, 0, p.V, q, cut, s, !all, summed, sh.segment);
+                n = gather<BF16>(row, 0, p.V, q, cut, s, !all, summed, sh.segment, sh.candidate);
                 if (all && n > kCandidates) {  // as above
                     all = false;
                     summed = by_mass;
-                    n = gather<BF16>(row, 0, p.V, q, cut, s, true, summed, sh.segment);
+                    n = gather<BF16>(row, 0, p.V, q, cut, s, true, summed, sh.segment, sh.candidate);
                 }
             }
             if (all) before = 0;
@@ -756,6 +800,9 @@ __global__ __launch_bounds__(kThreads) void sample_kernel(SampleParams p)
     }
 }
 
+// LDS of the kernels that share a row: a histogram or a list, so that a CU holds two blocks.
+constexpr size_t kHistogramLds = offsetof(Shared, candidate), kListLds = offsetof(Shared, list) + kCandidates * 8;
+
 int set_lds(const void *kernel)
 {
     MOE_HIP_CHECK(hipFuncSetAttribute(kernel, hipFuncAttributeMaxDynamicSharedMemorySize, (int)sizeof(Shared)));
@@ -781,16 +828,16 @@ int launch_as(const SampleParams &p, hipStream_t s)
         const dim3 grid(p.chunks, p.B);
         {
             ProfScope ps("sample_largest", s);
-            hipLaunchKernelGGL(sample_largest_kernel<BF16>, grid, dim3(kThreads), sizeof(Shared), s, p);
+            hipLaunchKernelGGL(sample_largest_kernel<BF16>, grid, dim3(kThreads), offsetof(Shared, list), s, p);
             MOE_LAUNCH_CHECK("sample_largest_kernel");
         }
         {
             ProfScope ps("sample_histogram", s);
-            hipLaunchKernelGGL(sample_histogram_kernel<BF16>, grid, dim3(kThreads), sizeof(Shared), s, p);
+            hipLaunchKernelGGL(sample_histogram_kernel<BF16>, grid, dim3(kThreads), kHistogramLds, s, p);
             MOE_LAUNCH_CHECK("sample_histogram_kernel");
         }
         ProfScope ps("sample_gather", s);
-        hipLaunchKernelGGL(sample_gather_kernel<BF16>, grid, dim3(kThreads), sizeof(Shared), s, p);
+        hipLaunchKernelGGL(sample_gather_kernel<BF16>, grid, dim3(kThreads), kListLds, s, p);
         MOE_LAUNCH_CHECK("sample_gather_kernel");
     }
     ProfScope ps("sample", s);
@@ -800,10 +847,10 @@ int launch_as(const SampleParams &p, hipStream_t s)
     return MOE_OK;
 }
 
-// Blocks of a row: so many that the rows together give 512 (a CU holds one), of 8192 tokens and more, which is a row's fixed cost in each.
+// Blocks of a row: so many that the rows together give 1024 (a CU holds two), of 8192 tokens and more, which is a row's fixed cost in each.
 int chunks_for(int B, int V)
 {
-    int chunks = 512 / (B > 0 ? B : 1);
+    int chunks = 1024 / (B > 0 ? B : 1);
     if (chunks > V / 8192) chunks = V / 8192;
     return chunks < 1 ? 1 : chunks > kMaxChunks ? kMaxChunks : chunks;
 }
