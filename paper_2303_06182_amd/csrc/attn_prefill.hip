@@ -32,7 +32,7 @@ struct PrefillParams {
     int row_tiles, splits;  // bounds for all sequences
 };
 
-struct GroupInfo {          // of 16 keys
+struct alignas(16) GroupInfo {// of 16 keys
     float key_scale;        // times scale * log2(e)
     float value_log2;       // log2 of the values' scale
     float value_inverse;
@@ -40,10 +40,11 @@ struct GroupInfo {          // of 16 keys
 };
 
 template <int DH>
-struct Buffer {
+struct alignas(16) Buffer {
     uint16_t k[kTile * DH];
     uint16_t v[DH * kTile];
     GroupInfo info[4];
+    int held;               // all of them
 };
 
 template <int DH>
@@ -220,6 +221,10 @@ __global__ __launch_bounds__(64 * W, W == 8 ? 2 : 1) void attn_prefill_kernel(Pr
                 for (int y = 0; y < 4; ++y) *reinterpret_cast<bf16x8 *>(to.v + v_at(4 * quad + y, c)) = widen(lo[y], hi[y]);
             }
         }
+        if (w == 0) {
+            const bool all = __all(tid >= 4 || info_held);
+            if (tid == 0) to.held = all;
+        }
         if (tid < 4) to.info[tid] = {fmaxf(info_k * scale, kLeast), log2f(fmaxf(info_v, kLeast)), 1.f / fmaxf(info_v, kLeast), info_held};
     };
 
@@ -245,26 +250,40 @@ __global__ __launch_bounds__(64 * W, W == 8 ? 2 : 1) void attn_prefill_kernel(Pr
         }
         const Buffer<DH> &buf = buffer[t & 1];
         if (key0 < any_end && key0 + kTile > any_begin) {
+            // Fragments are asked for kAhead steps before their MFMAs, and the order is kept by scheduling barriers: left to itself the
+            // compiler asks for two and waits for them (prefill of 8192 tokens 355 us, matrix pipes busy 30 %).
+            static constexpr int kAhead = kSteps < 4 ? kSteps : 4;
             f32x16 s[2];
 #pragma unroll
             for (int n = 0; n < 2; ++n)
 #pragma unroll
                 for (int i = 0; i < 16; ++i) s[n][i] = 0.f;
+            bf16x8 key[kAhead][2], value[2][kCols];
 #pragma unroll
-            for (int x = 0; x < kSteps; ++x)
+            for (int x = 0; x < kAhead; ++x)
 #pragma unroll
-                for (int n = 0; n < 2; ++n) {
-                    const bf16x8 key = *reinterpret_cast<const bf16x8 *>(buf.k + k_at<DH>(32 * n + l31, 2 * x + half));
-#pragma unroll
-                    for (int i = 0; i < NS; ++i) s[n] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(key, q[x].x[i], s[n], 0, 0, 0);
-                }
+                for (int n = 0; n < 2; ++n) key[x][n] = *reinterpret_cast<const bf16x8 *>(buf.k + k_at<DH>(32 * n + l31, 2 * x + half));
+            const int held = buf.held;
             GroupInfo info[4];
-            bool whole = key0 >= all_begin && key0 + kTile <= all_end;
 #pragma unroll
-            for (int g = 0; g < 4; ++g) {
-                info[g] = buf.info[g];
-                whole = whole && __builtin_amdgcn_readfirstlane(info[g].held);
+            for (int g = 0; g < 4; ++g) info[g] = buf.info[g];
+            __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+            for (int x = 0; x < kSteps; ++x) {
+                bf16x8 now[2] = {key[x % kAhead][0], key[x % kAhead][1]};
+#pragma unroll
+                for (int n = 0; n < 2; ++n)
+#pragma unroll
+                    for (int i = 0; i < NS; ++i) s[n] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(now[n], q[x].x[i], s[n], 0, 0, 0);
+                if (x + kAhead < kSteps)
+#pragma unroll
+                    for (int n = 0; n < 2; ++n) key[x % kAhead][n] = *reinterpret_cast<const bf16x8 *>(buf.k + k_at<DH>(32 * n + l31, 2 * (x + kAhead) + half));
+                __builtin_amdgcn_sched_barrier(0);
             }
+#pragma unroll
+            for (int c = 0; c < kCols; ++c) value[0][c] = *reinterpret_cast<const bf16x8 *>(buf.v + v_at(32 * c + l31, half));
+            __builtin_amdgcn_sched_barrier(0);
+            const bool whole = key0 >= all_begin && key0 + kTile <= all_end && __builtin_amdgcn_readfirstlane(held);
             if (!whole) {
 #pragma unroll
                 for (int n = 0; n < 2; ++n)
@@ -296,6 +315,10 @@ __global__ __launch_bounds__(64 * W, W == 8 ? 2 : 1) void attn_prefill_kernel(Pr
             const float base = m == -INFINITY ? 0.f : m;
 #pragma unroll
             for (int g = 0; g < 4; ++g) {
+                if (g < 3)
+#pragma unroll
+                    for (int c = 0; c < kCols; ++c) value[(g + 1) & 1][c] = *reinterpret_cast<const bf16x8 *>(buf.v + v_at(32 * c + l31, 2 * (g + 1) + half));
+                __builtin_amdgcn_sched_barrier(0);
                 const float offset = info[g].value_log2 - base;
                 float weight[8], sum = 0.f;
 #pragma unroll
@@ -306,11 +329,10 @@ __global__ __launch_bounds__(64 * W, W == 8 ? 2 : 1) void attn_prefill_kernel(Pr
                 l = fmaf(sum, info[g].value_inverse, l);
                 const Pieces<NS> wp = split<NS>(weight);
 #pragma unroll
-                for (int c = 0; c < kCols; ++c) {
-                    const bf16x8 value = *reinterpret_cast<const bf16x8 *>(buf.v + v_at(32 * c + l31, 2 * g + half));
+                for (int c = 0; c < kCols; ++c)
 #pragma unroll
-                    for (int i = 0; i < NS; ++i) o[c] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(value, wp.x[i], o[c], 0, 0, 0);
-                }
+                    for (int i = 0; i < NS; ++i) o[c] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(value[g & 1][c], wp.x[i], o[c], 0, 0, 0);
+                __builtin_amdgcn_sched_barrier(0);
             }
         }
         if (t + 1 < count) store(buffer[(t + 1) & 1]);
