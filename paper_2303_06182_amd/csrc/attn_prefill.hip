@@ -154,42 +154,59 @@ __global__ __launch_bounds__(64 * W, W == 8 ? 2 : 1) void attn_prefill_kernel(Pr
     const int page_mask = (1 << p.page_shift) - 1;
     uint32_t words[kWords];
     int page[kKItems > kVItems ? kKItems : kVItems], info_page = -1;
+    // Where this thread's bytes lie in a page, without the page: in tiles that are there as a whole, nearly all of them, the loads then take an
+    // address and offsets that are part of the instruction.  (With a predicate and an address of its own for each: 348 us where this takes 300.)
+    int in_tile[kKItems > kVItems ? kKItems : kVItems];
+#pragma unroll
+    for (int i = 0; i < (kKItems > kVItems ? kKItems : kVItems); ++i) {
+        const int item = i * kRole + role;
+        in_tile[i] = brings_k ? min(item / (DH / 16), kTile - 1) : 16 * (min(item / (DH / 4), 7) >> 1) + 4 * (item / (DH / 4) & 1);
+    }
     const auto page_of = [&](int key) { return key < sq.kv ? table[key >> p.page_shift] : -1; };
     const auto look_up = [&](int key0) {  // the pages of a tile, a tile ahead of its bytes
         if (brings_k) {
 #pragma unroll
-            for (int i = 0; i < kKItems; ++i) page[i] = page_of(key0 + min((i * kRole + role) / (DH / 16), kTile - 1));
+            for (int i = 0; i < kKItems; ++i) page[i] = page_of(key0 + in_tile[i]);
         } else {
 #pragma unroll
-            for (int i = 0; i < kVItems; ++i) page[i] = page_of(key0 + 16 * (min((i * kRole + role) / (DH / 4), 7) >> 1));
+            for (int i = 0; i < kVItems; ++i) page[i] = page_of(key0 + in_tile[i]);
         }
         if (tid < 4) info_page = page_of(key0 + 16 * tid);
     };
     float info_k = 1.f, info_v = 1.f;
     bool info_held = false;
     const auto load = [&](int key0) {
+        bool there = key0 + kTile <= sq.kv;
+#pragma unroll
+        for (int i = 0; i < (kKItems > kVItems ? kKItems : kVItems); ++i)
+            if (i < (brings_k ? kKItems : kVItems)) there = there && (uint32_t)page[i] < (uint32_t)p.num_pages;
+        const bool whole = __all(there);
         if (brings_k) {
 #pragma unroll
             for (int i = 0; i < kKItems; ++i) {
-                const int item = i * kRole + role, row = item / (DH / 16), c = item - row * (DH / 16);
-                const bool there = row < kTile && key0 + row < sq.kv && page[i] >= 0 && page[i] < p.num_pages;
-                uint4 x = make_uint4(0, 0, 0, 0);
-                if (there)
-                    x = *reinterpret_cast<const uint4 *>(
-                        p.k + ((((int64_t)page[i] * p.n_kv_heads + h) << p.page_shift) + ((key0 + row) & page_mask)) * DH + 16 * c);
+                const int item = i * kRole + role, row = in_tile[i], c = item % (DH / 16);
+                const bool held = whole || (key0 + row < sq.kv && (uint32_t)page[i] < (uint32_t)p.num_pages);
+                const uint8_t *src = p.k + ((((int64_t)(held ? page[i] : 0) * p.n_kv_heads + h) << p.page_shift) + ((key0 + row) & page_mask)) * DH + 16 * c;
+                uint4 x;
+                if (whole) x = *reinterpret_cast<const uint4 *>(src);
+                else x = held ? *reinterpret_cast<const uint4 *>(src) : make_uint4(0, 0, 0, 0);
                 words[4 * i] = x.x, words[4 * i + 1] = x.y, words[4 * i + 2] = x.z, words[4 * i + 3] = x.w;
             }
         } else {
 #pragma unroll
             for (int i = 0; i < kVItems; ++i) {
-                const int item = i * kRole + role, c = item / (DH / 4), quad = item - c * (DH / 4);
-                const int row0 = 16 * (c >> 1) + 4 * (c & 1);
-                const bool held = c < 8 && page[i] >= 0 && page[i] < p.num_pages;
+                const int quad = (i * kRole + role) % (DH / 4), row0 = in_tile[i];
+                const bool held = whole || (uint32_t)page[i] < (uint32_t)p.num_pages;
                 const uint8_t *src = p.v + ((((int64_t)(held ? page[i] : 0) * p.n_kv_heads + h) << p.page_shift) + ((key0 + row0) & page_mask)) * DH + 4 * quad;
+                if (whole) {
 #pragma unroll
-                for (int j = 0; j < 8; ++j) {
-                    const int row = (j & 3) + 8 * (j >> 2);
-                    words[8 * i + j] = held && key0 + row0 + row < sq.kv ? *reinterpret_cast<const uint32_t *>(src + row * DH) : 0u;
+                    for (int j = 0; j < 8; ++j) words[8 * i + j] = *reinterpret_cast<const uint32_t *>(src + ((j & 3) + 8 * (j >> 2)) * DH);
+                } else {
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) {
+                        const int row = (j & 3) + 8 * (j >> 2);
+                        words[8 * i + j] = held && key0 + row0 + row < sq.kv ? *reinterpret_cast<const uint32_t *>(src + row * DH) : 0u;
+                    }
                 }
             }
         }
