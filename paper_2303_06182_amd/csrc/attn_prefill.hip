@@ -242,7 +242,7 @@ __global__ __launch_bounds__(64 * W, W == 8 ? 2 : 1) void attn_prefill_kernel(Pr
             const bool all = __all(tid >= 4 || info_held);
             if (tid == 0) to.held = all;
         }
-        if (tid < 4) to.info[tid] = {fmaxf(info_k * scale, kLeast), log2f(fmaxf(info_v, kLeast)), 1.f / fmaxf(info_v, kLeast), info_held};
+        if (tid < 4) to.info[tid] = {fmaxf(info_k * scale, kLeast), __builtin_amdgcn_logf(fmaxf(info_v, kLeast)), __builtin_amdgcn_rcpf(fmaxf(info_v, kLeast)), info_held};
     };
 
     f32x16 o[kCols];
@@ -284,6 +284,7 @@ __global__ __launch_bounds__(64 * W, W == 8 ? 2 : 1) void attn_prefill_kernel(Pr
             GroupInfo info[4];
 #pragma unroll
             for (int g = 0; g < 4; ++g) info[g] = buf.info[g];
+            __builtin_amdgcn_s_setprio(1);  // the wave that has products goes before the one that has exponentials (1 %)
             __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
             for (int x = 0; x < kSteps; ++x) {
@@ -300,6 +301,7 @@ __global__ __launch_bounds__(64 * W, W == 8 ? 2 : 1) void attn_prefill_kernel(Pr
 #pragma unroll
             for (int c = 0; c < kCols; ++c) value[0][c] = *reinterpret_cast<const bf16x8 *>(buf.v + v_at(32 * c + l31, half));
             __builtin_amdgcn_sched_barrier(0);
+            __builtin_amdgcn_s_setprio(0);
             const bool whole = key0 >= all_begin && key0 + kTile <= all_end && __builtin_amdgcn_readfirstlane(held);
             if (!whole) {
 #pragma unroll
