@@ -73,13 +73,14 @@ template <int DH, int W>
 constexpr int64_t part_floats() { return (int64_t)32 * W * (DH + 2); }
 
 template <int DH, int NS, int W>
-__global__ __launch_bounds__(64 * W, W == 8 ? 2 : 1) void attn_prefill_kernel(PrefillParams pp)
+__global__ __launch_bounds__(64 * W, NS == 1 && DH <= 128 ? 2 : 1) void attn_prefill_kernel(PrefillParams pp)
 {
     static constexpr int kThreads = 64 * W, kRows = 32 * W, kRole = kThreads / 2;
     static constexpr int kKItems = (4 * DH + kRole - 1) / kRole;  // 16 bytes of a key each
     static constexpr int kVItems = (2 * DH + kRole - 1) / kRole;  // 4 dimensions of 8 values each
     static constexpr int kWords = kKItems * 4 > kVItems * 8 ? kKItems * 4 : kVItems * 8;
     static constexpr int kSteps = DH / 16, kCols = DH / 32;
+    static constexpr int kValues = DH <= 128 ? 2 : 1;  // fragments of the values in registers: of this 16 keys and the next, where they fit
     extern __shared__ __align__(16) uint8_t lds[];
     Buffer<DH> *buffer = reinterpret_cast<Buffer<DH> *>(lds);
     const AttnParams &p = pp.a;
@@ -275,7 +276,7 @@ __global__ __launch_bounds__(64 * W, W == 8 ? 2 : 1) void attn_prefill_kernel(Pr
             for (int n = 0; n < 2; ++n)
 #pragma unroll
                 for (int i = 0; i < 16; ++i) s[n][i] = 0.f;
-            bf16x8 key[kAhead][2], value[2][kCols];
+            bf16x8 key[kAhead][2], value[kValues][kCols];
 #pragma unroll
             for (int x = 0; x < kAhead; ++x)
 #pragma unroll
@@ -298,8 +299,9 @@ __global__ __launch_bounds__(64 * W, W == 8 ? 2 : 1) void attn_prefill_kernel(Pr
                     for (int n = 0; n < 2; ++n) key[x % kAhead][n] = *reinterpret_cast<const bf16x8 *>(buf.k + k_at<DH>(32 * n + l31, 2 * (x + kAhead) + half));
                 __builtin_amdgcn_sched_barrier(0);
             }
+            if (kValues == 2)
 #pragma unroll
-            for (int c = 0; c < kCols; ++c) value[0][c] = *reinterpret_cast<const bf16x8 *>(buf.v + v_at(32 * c + l31, half));
+                for (int c = 0; c < kCols; ++c) value[0][c] = *reinterpret_cast<const bf16x8 *>(buf.v + v_at(32 * c + l31, half));
             __builtin_amdgcn_sched_barrier(0);
             __builtin_amdgcn_s_setprio(0);
             const bool whole = key0 >= all_begin && key0 + kTile <= all_end && __builtin_amdgcn_readfirstlane(held);
@@ -334,9 +336,10 @@ __global__ __launch_bounds__(64 * W, W == 8 ? 2 : 1) void attn_prefill_kernel(Pr
             const float base = m == -INFINITY ? 0.f : m;
 #pragma unroll
             for (int g = 0; g < 4; ++g) {
-                if (g < 3)
+                const int ask = g + kValues - 1;
+                if (ask < 4)
 #pragma unroll
-                    for (int c = 0; c < kCols; ++c) value[(g + 1) & 1][c] = *reinterpret_cast<const bf16x8 *>(buf.v + v_at(32 * c + l31, 2 * (g + 1) + half));
+                    for (int c = 0; c < kCols; ++c) value[ask % kValues][c] = *reinterpret_cast<const bf16x8 *>(buf.v + v_at(32 * c + l31, 2 * ask + half));
                 __builtin_amdgcn_sched_barrier(0);
                 const float offset = info[g].value_log2 - base;
                 float weight[8], sum = 0.f;
@@ -350,7 +353,7 @@ __global__ __launch_bounds__(64 * W, W == 8 ? 2 : 1) void attn_prefill_kernel(Pr
 #pragma unroll
                 for (int c = 0; c < kCols; ++c)
 #pragma unroll
-                    for (int i = 0; i < NS; ++i) o[c] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(value[g & 1][c], wp.x[i], o[c], 0, 0, 0);
+                    for (int i = 0; i < NS; ++i) o[c] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(value[g % kValues][c], wp.x[i], o[c], 0, 0, 0);
                 __builtin_amdgcn_sched_barrier(0);
             }
         }
@@ -430,8 +433,16 @@ __global__ __launch_bounds__(256) void attn_prefill_join_kernel(PrefillParams pp
     }
 }
 
-// Parts of the keys: none where the units give every CU two blocks; else so many that they do.  (part buffers: 2 a CU)
-int splits_for(int64_t units, int num_cus) { return units >= 2 * num_cus ? 1 : (int)(2 * num_cus / units); }
+// Parts of the keys: none where the units give every CU two blocks, else so many that they do, of four tiles at least (a part of 256 rows and 128
+// dimensions costs 133 KB written and read again, as much as two tiles).  units: blocks of the grid; filled: about how many of them have rows.
+// Part buffers: 4 a CU.
+int splits_for(int64_t units, int64_t filled, int tiles, int num_cus)
+{
+    int64_t n = filled >= 2 * num_cus ? 1 : 2 * num_cus / (filled > 0 ? filled : 1);
+    if (n > (tiles + 3) / 4) n = (tiles + 3) / 4;
+    if (n > 4 * num_cus / units) n = 4 * num_cus / units;
+    return n < 1 ? 1 : (int)n;
+}
 
 template <int DH, int NS, int W>
 int launch_as(PrefillParams pp, int num_cus, hipStream_t s)
@@ -446,9 +457,8 @@ int launch_as(PrefillParams pp, int num_cus, hipStream_t s)
     const AttnParams &p = pp.a;
     pp.row_tiles = (int)(((int64_t)p.max_q * p.group + 32 * W - 1) / (32 * W));
     const int64_t units = (int64_t)pp.row_tiles * p.B * p.n_kv_heads;
-    const int most = ceil_div(p.max_kv, kTile) > 0 ? ceil_div(p.max_kv, kTile) : 1;
-    pp.splits = splits_for(units, num_cus);
-    pp.splits = pp.splits < most ? pp.splits : most;
+    const int64_t filled = ((int64_t)p.T * p.group / (32 * W) + p.B) * p.n_kv_heads;
+    pp.splits = splits_for(units, filled < units ? filled : units, ceil_div(p.max_kv, kTile), num_cus);
     if (units * pp.splits >= 1ll << 31) {
         set_error("moe_attn_forward: %lld blocks", (long long)units);
         return MOE_ERR_INVALID_ARG;
@@ -471,7 +481,7 @@ int launch_as(PrefillParams pp, int num_cus, hipStream_t s)
 int64_t attn_prefill_workspace(int head_dim, int num_cus)
 {
     const int w = head_dim <= 128 ? 8 : 4;
-    return align_up((int64_t)2 * num_cus * 32 * w * (head_dim + 2) * 4, 256);
+    return align_up((int64_t)4 * num_cus * 32 * w * (head_dim + 2) * 4, 256);
 }
 
 // p.part: attn_prefill_workspace() bytes
@@ -479,7 +489,11 @@ int launch_attn_prefill(int dtype, int head_dim, const AttnParams &p, int num_cu
 {
     const PrefillParams pp = {p, 0, 1};
     const bool bf = dtype == MOE_DTYPE_BF16;
-    // rows of 256 and two waves a SIMD; fp32 and 256 dimensions need the registers of both
+    // Rows of 256 and two waves a SIMD; fp32 and 256 dimensions need the registers of both.  Rows of 128 too where tiles of 256 would be fewer than
+    // the CUs: staging costs twice as much a row then (8192 tokens of 16 heads: 467 us, 313 with 256), but more CUs work.
+    const bool small = ((int64_t)p.T * p.group / 256 + p.B) * p.n_kv_heads < num_cus;
+    if (bf && small && head_dim == 64) return launch_as<64, 1, 4>(pp, num_cus, s);
+    if (bf && small && head_dim == 128) return launch_as<128, 1, 4>(pp, num_cus, s);
     if (head_dim == 64) return bf ? launch_as<64, 1, 8>(pp, num_cus, s) : launch_as<64, 3, 4>(pp, num_cus, s);
     if (head_dim == 128) return bf ? launch_as<128, 1, 8>(pp, num_cus, s) : launch_as<128, 3, 4>(pp, num_cus, s);
     return bf ? launch_as<256, 1, 4>(pp, num_cus, s) : launch_as<256, 3, 4>(pp, num_cus, s);
