@@ -197,7 +197,7 @@ int moe_kv_append(moe_attn_handle_t *h, const moe_kv_cache_t *cache, const void 
     p.rot_dim = c.rot_dim;
     p.interleaved = c.rot_interleaved;
     p.q_out = q_out;
-    return launch_kv_append(c.dtype, c.head_dim, p, h->num_cus, (hipStream_t)stream);
+    return launch_kv_append(c.dtype, c.head_dim, p, (hipStream_t)stream);
 }
 
 int moe_attn_forward(moe_attn_handle_t *h, const moe_kv_cache_t *cache, const void *q, int64_t q_stride, const int32_t *q_offsets,

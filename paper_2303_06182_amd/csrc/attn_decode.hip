@@ -480,12 +480,8 @@ int launch_as(AttnParams p, int num_cus, hipStream_t s)
         setup_rc = hipFuncSetAttribute(reinterpret_cast<const void *>(attn_decode_kernel<DH, NS, M>), hipFuncAttributeMaxDynamicSharedMemorySize, (int)kMost);
     });
     MOE_HIP_CHECK(setup_rc);
-    {
-        ProfScope ps("attn_decode", s);
-        hipLaunchKernelGGL((attn_decode_kernel<DH, NS, M>), dim3(p.n_blocks), dim3(kThreads), lds, s, p);
-        MOE_LAUNCH_CHECK("attn_decode_kernel");
-    }
-    ProfScope ps("attn_join", s);
+    hipLaunchKernelGGL((attn_decode_kernel<DH, NS, M>), dim3(p.n_blocks), dim3(kThreads), lds, s, p);
+    MOE_LAUNCH_CHECK("attn_decode_kernel");
     const int64_t rows = (int64_t)p.max_q * p.group < p.few_rows ? (int64_t)p.max_q * p.group : p.few_rows;
     const int units = ceil_div((int)rows, 16) * p.n_kv_heads, unit_rows = rows < 16 ? (int)rows : 16;
     hipLaunchKernelGGL((attn_join_kernel<DH, NS>), dim3(units * unit_rows, p.B), dim3(kThreads), 0, s, p, unit_rows);

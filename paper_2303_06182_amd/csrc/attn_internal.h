@@ -55,7 +55,7 @@ struct AppendParams {
     void *q_out;
 };
 
-int launch_kv_append(int dtype, int head_dim, const AppendParams &p, int num_cus, hipStream_t s);
+int launch_kv_append(int dtype, int head_dim, const AppendParams &p, hipStream_t s);
 int launch_attn_decode(int dtype, int head_dim, const AttnParams &p, int num_cus, hipStream_t s);
 int64_t attn_decode_workspace(int head_dim, int num_cus);
 int launch_attn_prefill(int dtype, int head_dim, const AttnParams &p, int num_cus, hipStream_t s);

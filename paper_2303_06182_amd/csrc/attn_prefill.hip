@@ -463,13 +463,9 @@ int launch_as(PrefillParams pp, int num_cus, hipStream_t s)
         set_error("moe_attn_forward: %lld blocks", (long long)units);
         return MOE_ERR_INVALID_ARG;
     }
-    {
-        ProfScope ps("attn_prefill", s);
-        hipLaunchKernelGGL((attn_prefill_kernel<DH, NS, W>), dim3((unsigned)(units * pp.splits)), dim3(64 * W), kLds, s, pp);
-        MOE_LAUNCH_CHECK("attn_prefill_kernel");
-    }
+    hipLaunchKernelGGL((attn_prefill_kernel<DH, NS, W>), dim3((unsigned)(units * pp.splits)), dim3(64 * W), kLds, s, pp);
+    MOE_LAUNCH_CHECK("attn_prefill_kernel");
     if (pp.splits > 1) {
-        ProfScope ps("attn_prefill_join", s);
         hipLaunchKernelGGL((attn_prefill_join_kernel<DH, NS, W>), dim3((unsigned)(units * 2 * W)), dim3(256), 0, s, pp);
         MOE_LAUNCH_CHECK("attn_prefill_join_kernel");
     }

@@ -15,8 +15,6 @@ namespace moe355 {
 
 namespace {
 
-typedef __attribute__((ext_vector_type(4))) float f32x4_t;
-
 // cos and sin of an angle in radians: the turns t = angle / (2 pi) less the nearest quarter, r in [-1/8, 1/8], then the Taylor
 // series of sin and cos at x = 2 pi r, |x| <= pi/4: the first terms left out are x^15 / 15! = 2e-14 and x^14 / 14! = 4e-13.
 // The product angle / (2 pi) is kept with its rounding error: alone it would be off by 1e-10 radians at angles of 1e6.
@@ -343,7 +341,7 @@ __global__ __launch_bounds__(NT) void kv_append_kernel(AppendParams p, int kv_un
 }
 
 template <int DH, bool BF16, int NT, int U>
-int launch_as(const AppendParams &p, int num_cus, hipStream_t s)
+int launch_as(const AppendParams &p, hipStream_t s)
 {
     // touched pages: at most (n - 2) / page_size + 2 of each sequence, and T / page_size + 2 B of all
     const int page_size = 1 << p.a.page_shift;
@@ -357,34 +355,33 @@ int launch_as(const AppendParams &p, int num_cus, hipStream_t s)
         set_error("moe_kv_append: %lld blocks", (long long)blocks);
         return MOE_ERR_INVALID_ARG;
     }
-    ProfScope ps("kv_append", s);
     hipLaunchKernelGGL((kv_append_kernel<DH, BF16, NT, U>), dim3((unsigned)blocks), dim3(NT), 0, s, p, (int)kv_units, counted ? 0 : each);
     MOE_LAUNCH_CHECK("kv_append_kernel");
     return MOE_OK;
 }
 
 template <int DH, bool BF16>
-int launch_sized(const AppendParams &p, int num_cus, hipStream_t s)
+int launch_sized(const AppendParams &p, hipStream_t s)
 {
     const int rows = p.a.max_q < (1 << p.a.page_shift) ? p.a.max_q : 1 << p.a.page_shift;
     const int items = 2 * rows * (DH / 16);  // of keys and values in a block
     // a key's and a value's item a thread, so that a block's loads are all in flight at once and registers leave room for five waves a SIMD
-    if (items <= 64) return launch_as<DH, BF16, 64, 1>(p, num_cus, s);
-    if (items <= 128) return launch_as<DH, BF16, 64, 2>(p, num_cus, s);
-    if (items <= 512) return launch_as<DH, BF16, 256, 2>(p, num_cus, s);
-    if (items <= 1024) return launch_as<DH, BF16, 512, 2>(p, num_cus, s);
-    if (items <= 2048) return launch_as<DH, BF16, 1024, 2>(p, num_cus, s);
-    return launch_as<DH, BF16, 1024, 4>(p, num_cus, s);
+    if (items <= 64) return launch_as<DH, BF16, 64, 1>(p, s);
+    if (items <= 128) return launch_as<DH, BF16, 64, 2>(p, s);
+    if (items <= 512) return launch_as<DH, BF16, 256, 2>(p, s);
+    if (items <= 1024) return launch_as<DH, BF16, 512, 2>(p, s);
+    if (items <= 2048) return launch_as<DH, BF16, 1024, 2>(p, s);
+    return launch_as<DH, BF16, 1024, 4>(p, s);
 }
 
 }  // namespace
 
-int launch_kv_append(int dtype, int head_dim, const AppendParams &p, int num_cus, hipStream_t s)
+int launch_kv_append(int dtype, int head_dim, const AppendParams &p, hipStream_t s)
 {
     const bool bf = dtype == MOE_DTYPE_BF16;
-    if (head_dim == 64) return bf ? launch_sized<64, true>(p, num_cus, s) : launch_sized<64, false>(p, num_cus, s);
-    if (head_dim == 128) return bf ? launch_sized<128, true>(p, num_cus, s) : launch_sized<128, false>(p, num_cus, s);
-    return bf ? launch_sized<256, true>(p, num_cus, s) : launch_sized<256, false>(p, num_cus, s);
+    if (head_dim == 64) return bf ? launch_sized<64, true>(p, s) : launch_sized<64, false>(p, s);
+    if (head_dim == 128) return bf ? launch_sized<128, true>(p, s) : launch_sized<128, false>(p, s);
+    return bf ? launch_sized<256, true>(p, s) : launch_sized<256, false>(p, s);
 }
 
 }  // namespace moe355

@@ -826,21 +826,13 @@ int launch_as(const SampleParams &p, hipStream_t s)
     }
     if (p.chunks > 1) {
         const dim3 grid(p.chunks, p.B);
-        {
-            ProfScope ps("sample_largest", s);
-            hipLaunchKernelGGL(sample_largest_kernel<BF16>, grid, dim3(kThreads), offsetof(Shared, list), s, p);
-            MOE_LAUNCH_CHECK("sample_largest_kernel");
-        }
-        {
-            ProfScope ps("sample_histogram", s);
-            hipLaunchKernelGGL(sample_histogram_kernel<BF16>, grid, dim3(kThreads), kHistogramLds, s, p);
-            MOE_LAUNCH_CHECK("sample_histogram_kernel");
-        }
-        ProfScope ps("sample_gather", s);
+        hipLaunchKernelGGL(sample_largest_kernel<BF16>, grid, dim3(kThreads), offsetof(Shared, list), s, p);
+        MOE_LAUNCH_CHECK("sample_largest_kernel");
+        hipLaunchKernelGGL(sample_histogram_kernel<BF16>, grid, dim3(kThreads), kHistogramLds, s, p);
+        MOE_LAUNCH_CHECK("sample_histogram_kernel");
         hipLaunchKernelGGL(sample_gather_kernel<BF16>, grid, dim3(kThreads), kListLds, s, p);
         MOE_LAUNCH_CHECK("sample_gather_kernel");
     }
-    ProfScope ps("sample", s);
     if (p.chunks > 1) hipLaunchKernelGGL((sample_kernel<BF16, true>), dim3(p.B), dim3(kThreads), sizeof(Shared), s, p);
     else hipLaunchKernelGGL((sample_kernel<BF16, false>), dim3(p.B), dim3(kThreads), sizeof(Shared), s, p);
     MOE_LAUNCH_CHECK("sample_kernel");

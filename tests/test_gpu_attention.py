@@ -170,6 +170,35 @@ def test_strided_queries_other_scale_and_no_lse(n):
     assert none is None and torch.equal(again, out)
 
 
+def test_sequences_around_few_rows_in_one_batch():
+    """Sequences of at most 32 rows (tokens times group) and of more are different kernels'; both in one call, each about its border."""
+    Batch([8, 9, 1, 0, 7, 40], [200, 9, 70, 5, 7, 333], 8, 2, 64, 32).fill().attend()
+    Batch([32, 33, 2], [40, 400, 90], 2, 2, 128, 16, "f32").fill().attend()
+
+
+@pytest.mark.parametrize("n", [1, 50])
+def test_pages_past_32_bits(n):
+    """A cache of more than 2^32 bytes: the same contents in its last pages give the same outputs, and appending lands there."""
+    b = Batch([n, 1], [n + 100, 300], 4, 2, 128, 64, rot=128).fill()
+    per_page = 2 * 64 * 128
+    pages = (1 << 32) // per_page + b.pages + 8
+    big = binding.PagedAttention(2, n + 1, 4, 2, 128, 64, pages, b.max_pages, "bf16", 128)
+    small, far = b.device_cache(), big.new_cache()
+    shift = pages - b.pages
+    for name in ("k", "v", "k_scale", "v_scale"):
+        getattr(far, name)[shift:].view(torch.uint8).copy_(getattr(small, name).view(torch.uint8))
+    offsets, kv, table = b.args()
+    there = torch.where(table >= 0, table + shift, table)
+    (q, _), (k, _), (v, _) = b.rows(4), b.rows(2), b.rows(2)
+    f = torch.from_numpy(b.inv_freq).to(DEV)
+    for att, cache, t in ((b.att, small, table), (big, far, there)):
+        cache.q = att.moe_kv_append(cache, q, k, v, f, offsets, kv, t, n)
+        cache.out, cache.lse = att.moe_attn_forward(cache, cache.q, offsets, kv, t, n, n + 300)
+    assert torch.equal(small.q, far.q) and torch.equal(small.out, far.out) and torch.equal(small.lse, far.lse)
+    for name in ("k", "v"):
+        assert torch.equal(getattr(far, name)[shift:].view(torch.uint8), getattr(small, name).view(torch.uint8))
+
+
 @pytest.mark.parametrize("n,kv", [(1, 900), (90, 400)])
 def test_large_scores_and_scales(n, kv):
     """Scores of some hundreds: all weight on single keys; scales far from one."""
