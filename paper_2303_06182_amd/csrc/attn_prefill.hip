@@ -6,10 +6,11 @@
 //        bank once (V's writes: twice); two buffers, the next tile's bytes are in flight while this one is computed
 //   S^T = K Q^T and O^T = V^T P^T by 32x32x16 MFMAs; queries stay in registers.  A lane holds 4 keys in 8 of one query; a chunk of
 //        V^T holds just those keys in just that order, so the weights are the second product's operand where the first left them.
-// The maximum, the sum and the rescaling of a query are its lane's own; two lanes share a query.  Scales cost nothing: a key's scale is
-// part of the factor in front of the exponent, a value's of its offset (weights 2^(s - m + log2 v_scale)), taken out of the sum per 16
-// keys.  The output is rescaled only where the maximum has grown by more than 8 (a factor of 256 on the weights, which fp32 and bf16
-// both hold), for most tiles not at all.
+// The maximum, the sum and the rescaling of a query are its lane's own; two lanes share a query.  The scales are powers of two, which the
+// conversion to bf16 multiplies by for nothing, and no later step knows of them.  (In the exponent instead, a key's as part of its factor and
+// a value's as its offset, they cost instructions per 16 keys, and the scale of a page of zeros, 2^-126, takes its weights out of fp32.)
+// Products below 2^-126 may be lost: what they weigh is less than that, too.  The output is rescaled only where the maximum has grown by more
+// than 8 (a factor of 256 on the weights, which fp32 and bf16 both hold), for most tiles not at all.
 //
 // Bound by the matrix cores and the exponentials (a quarter of the rate of other instructions) in about equal parts: per 32 x 64 weights
 // and wave 32 MFMAs of 32 cycles, 32 exponentials of 16 and some 110 others of 4.  Two waves a SIMD overlap them.
@@ -25,26 +26,18 @@ namespace moe355 {
 namespace {
 
 static constexpr int kTile = 64;
-static constexpr float kLeast = 1.17549435e-38f;  // factors stay normal numbers: 0 times a masked score's infinity is none
 
 struct PrefillParams {
     AttnParams a;
     int row_tiles, splits;  // bounds for all sequences
 };
 
-struct alignas(16) GroupInfo {// of 16 keys
-    float key_scale;        // times scale * log2(e)
-    float value_log2;       // log2 of the values' scale
-    float value_inverse;
-    int held;
-};
-
 template <int DH>
 struct alignas(16) Buffer {
     uint16_t k[kTile * DH];
     uint16_t v[DH * kTile];
-    GroupInfo info[4];
-    int held;               // all of them
+    int held[4];  // 16 keys each: the page table names a page for them
+    int whole;    // all of them
 };
 
 template <int DH>
@@ -125,7 +118,7 @@ __global__ __launch_bounds__(64 * W, NS == 1 && DH <= 128 ? 2 : 1) void attn_pre
 
     // queries; a negative scale is theirs, so that the factor in front of the exponent is positive
     const bool negative = p.scale_log2e < 0.f;
-    const float scale = fmaxf(fabsf(p.scale_log2e), 1e-30f);
+    const float scale = fmaxf(fabsf(p.scale_log2e), 1e-30f);  // not zero: times a masked score's infinity that is none
     Pieces<NS> q[kSteps];
 #pragma unroll
     for (int s = 0; s < kSteps; ++s) {
@@ -154,9 +147,10 @@ __global__ __launch_bounds__(64 * W, NS == 1 && DH <= 128 ? 2 : 1) void attn_pre
     const int role = brings_k ? tid : tid - kRole;
     const int page_mask = (1 << p.page_shift) - 1;
     uint32_t words[kWords];
-    int page[kKItems > kVItems ? kKItems : kVItems], info_page = -1;
+    float unit_scale[kKItems > kVItems ? kKItems : kVItems];
+    int page[kKItems > kVItems ? kKItems : kVItems], group_page = -1;
     // Where this thread's bytes lie in a page, without the page: in tiles that are there as a whole, nearly all of them, the loads then take an
-    // address and offsets that are part of the instruction.  (With a predicate and an address of its own for each: 348 us where this takes 300.)
+    // address and offsets that are part of the instruction.  (With a predicate and an address of its own for each: 348 us where this took 313.)
     int in_tile[kKItems > kVItems ? kKItems : kVItems];
 #pragma unroll
     for (int i = 0; i < (kKItems > kVItems ? kKItems : kVItems); ++i) {
@@ -172,10 +166,9 @@ __global__ __launch_bounds__(64 * W, NS == 1 && DH <= 128 ? 2 : 1) void attn_pre
 #pragma unroll
             for (int i = 0; i < kVItems; ++i) page[i] = page_of(key0 + in_tile[i]);
         }
-        if (tid < 4) info_page = page_of(key0 + 16 * tid);
+        if (tid < 4) group_page = page_of(key0 + 16 * tid);
     };
-    float info_k = 1.f, info_v = 1.f;
-    bool info_held = false;
+    bool group_held = false;
     const auto load = [&](int key0) {
         bool there = key0 + kTile <= sq.kv;
 #pragma unroll
@@ -187,7 +180,9 @@ __global__ __launch_bounds__(64 * W, NS == 1 && DH <= 128 ? 2 : 1) void attn_pre
             for (int i = 0; i < kKItems; ++i) {
                 const int item = i * kRole + role, row = in_tile[i], c = item % (DH / 16);
                 const bool held = whole || (key0 + row < sq.kv && (uint32_t)page[i] < (uint32_t)p.num_pages);
-                const uint8_t *src = p.k + ((((int64_t)(held ? page[i] : 0) * p.n_kv_heads + h) << p.page_shift) + ((key0 + row) & page_mask)) * DH + 16 * c;
+                const int64_t unit = (int64_t)(held ? page[i] : 0) * p.n_kv_heads + h;
+                const uint8_t *src = p.k + ((unit << p.page_shift) + ((key0 + row) & page_mask)) * DH + 16 * c;
+                unit_scale[i] = held ? p.k_scale[unit] : 1.f;
                 uint4 x;
                 if (whole) x = *reinterpret_cast<const uint4 *>(src);
                 else x = held ? *reinterpret_cast<const uint4 *>(src) : make_uint4(0, 0, 0, 0);
@@ -198,7 +193,9 @@ __global__ __launch_bounds__(64 * W, NS == 1 && DH <= 128 ? 2 : 1) void attn_pre
             for (int i = 0; i < kVItems; ++i) {
                 const int quad = (i * kRole + role) % (DH / 4), row0 = in_tile[i];
                 const bool held = whole || (uint32_t)page[i] < (uint32_t)p.num_pages;
-                const uint8_t *src = p.v + ((((int64_t)(held ? page[i] : 0) * p.n_kv_heads + h) << p.page_shift) + ((key0 + row0) & page_mask)) * DH + 4 * quad;
+                const int64_t unit = (int64_t)(held ? page[i] : 0) * p.n_kv_heads + h;
+                const uint8_t *src = p.v + ((unit << p.page_shift) + ((key0 + row0) & page_mask)) * DH + 4 * quad;
+                unit_scale[i] = held ? p.v_scale[unit] : 1.f;
                 if (whole) {
 #pragma unroll
                     for (int j = 0; j < 8; ++j) words[8 * i + j] = *reinterpret_cast<const uint32_t *>(src + ((j & 3) + 8 * (j >> 2)) * DH);
@@ -211,12 +208,7 @@ __global__ __launch_bounds__(64 * W, NS == 1 && DH <= 128 ? 2 : 1) void attn_pre
                 }
             }
         }
-        if (tid < 4) {
-            info_held = info_page >= 0 && info_page < p.num_pages;
-            const int64_t unit = (int64_t)(info_held ? info_page : 0) * p.n_kv_heads + h;
-            info_k = info_held ? p.k_scale[unit] : 1.f;
-            info_v = info_held ? p.v_scale[unit] : 1.f;
-        }
+        if (tid < 4) group_held = (uint32_t)group_page < (uint32_t)p.num_pages;
     };
     const auto store = [&](Buffer<DH> &to) {
         if (brings_k) {
@@ -224,8 +216,8 @@ __global__ __launch_bounds__(64 * W, NS == 1 && DH <= 128 ? 2 : 1) void attn_pre
             for (int i = 0; i < kKItems; ++i) {
                 const int item = i * kRole + role, row = item / (DH / 16), c = item - row * (DH / 16);
                 if (row >= kTile) continue;
-                *reinterpret_cast<bf16x8 *>(to.k + k_at<DH>(row, 2 * c)) = widen(words[4 * i], words[4 * i + 1]);
-                *reinterpret_cast<bf16x8 *>(to.k + k_at<DH>(row, 2 * c + 1)) = widen(words[4 * i + 2], words[4 * i + 3]);
+                *reinterpret_cast<bf16x8 *>(to.k + k_at<DH>(row, 2 * c)) = widen(words[4 * i], words[4 * i + 1], unit_scale[i]);
+                *reinterpret_cast<bf16x8 *>(to.k + k_at<DH>(row, 2 * c + 1)) = widen(words[4 * i + 2], words[4 * i + 3], unit_scale[i]);
             }
         } else {
 #pragma unroll
@@ -236,14 +228,14 @@ __global__ __launch_bounds__(64 * W, NS == 1 && DH <= 128 ? 2 : 1) void attn_pre
                 transpose4(words[8 * i], words[8 * i + 1], words[8 * i + 2], words[8 * i + 3], lo);
                 transpose4(words[8 * i + 4], words[8 * i + 5], words[8 * i + 6], words[8 * i + 7], hi);
 #pragma unroll
-                for (int y = 0; y < 4; ++y) *reinterpret_cast<bf16x8 *>(to.v + v_at(4 * quad + y, c)) = widen(lo[y], hi[y]);
+                for (int y = 0; y < 4; ++y) *reinterpret_cast<bf16x8 *>(to.v + v_at(4 * quad + y, c)) = widen(lo[y], hi[y], unit_scale[i]);
             }
         }
         if (w == 0) {
-            const bool all = __all(tid >= 4 || info_held);
-            if (tid == 0) to.held = all;
+            const bool all = __all(tid >= 4 || group_held);
+            if (tid == 0) to.whole = all;
+            if (tid < 4) to.held[tid] = group_held;
         }
-        if (tid < 4) to.info[tid] = {fmaxf(info_k * scale, kLeast), __builtin_amdgcn_logf(fmaxf(info_v, kLeast)), __builtin_amdgcn_rcpf(fmaxf(info_v, kLeast)), info_held};
     };
 
     f32x16 o[kCols];
@@ -281,10 +273,7 @@ __global__ __launch_bounds__(64 * W, NS == 1 && DH <= 128 ? 2 : 1) void attn_pre
             for (int x = 0; x < kAhead; ++x)
 #pragma unroll
                 for (int n = 0; n < 2; ++n) key[x][n] = *reinterpret_cast<const bf16x8 *>(buf.k + k_at<DH>(32 * n + l31, 2 * x + half));
-            const int held = buf.held;
-            GroupInfo info[4];
-#pragma unroll
-            for (int g = 0; g < 4; ++g) info[g] = buf.info[g];
+            const int all_held = buf.whole;
             __builtin_amdgcn_s_setprio(1);  // the wave that has products goes before the one that has exponentials (1 %)
             __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
@@ -304,25 +293,22 @@ __global__ __launch_bounds__(64 * W, NS == 1 && DH <= 128 ? 2 : 1) void attn_pre
                 for (int c = 0; c < kCols; ++c) value[0][c] = *reinterpret_cast<const bf16x8 *>(buf.v + v_at(32 * c + l31, half));
             __builtin_amdgcn_sched_barrier(0);
             __builtin_amdgcn_s_setprio(0);
-            const bool whole = key0 >= all_begin && key0 + kTile <= all_end && __builtin_amdgcn_readfirstlane(held);
+            const bool whole = key0 >= all_begin && key0 + kTile <= all_end && __builtin_amdgcn_readfirstlane(all_held);
             if (!whole) {
 #pragma unroll
                 for (int n = 0; n < 2; ++n)
 #pragma unroll
                     for (int i = 0; i < 16; ++i) {
                         const int key = key0 + 32 * n + 8 * (i >> 2) + 4 * half + (i & 3);
-                        s[n][i] = info[2 * n + (i >> 3)].held && key >= key_begin && key < key_end ? s[n][i] : -INFINITY;
+                        s[n][i] = buf.held[2 * n + (i >> 3)] && key >= key_begin && key < key_end ? s[n][i] : -INFINITY;
                     }
             }
             float top = -INFINITY;
 #pragma unroll
-            for (int g = 0; g < 4; ++g) {
-                float most = s[g >> 1][8 * (g & 1)];
+            for (int n = 0; n < 2; ++n)
 #pragma unroll
-                for (int i = 1; i < 8; ++i) most = fmaxf(most, s[g >> 1][8 * (g & 1) + i]);
-                top = fmaxf(top, most * info[g].key_scale);
-            }
-            top = fmaxf(top, __shfl_xor(top, 32, 64));
+                for (int i = 0; i < 16; ++i) top = fmaxf(top, s[n][i]);
+            top = fmaxf(top, __shfl_xor(top, 32, 64)) * scale;
             if (__any(top > m + 8.f)) {  // m is -infinity until a row has seen a key
                 const float m_new = fmaxf(m, top);
                 const float alpha = m_new == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m - m_new);
@@ -341,14 +327,12 @@ __global__ __launch_bounds__(64 * W, NS == 1 && DH <= 128 ? 2 : 1) void attn_pre
 #pragma unroll
                     for (int c = 0; c < kCols; ++c) value[ask % kValues][c] = *reinterpret_cast<const bf16x8 *>(buf.v + v_at(32 * c + l31, 2 * ask + half));
                 __builtin_amdgcn_sched_barrier(0);
-                const float offset = info[g].value_log2 - base;
-                float weight[8], sum = 0.f;
+                float weight[8];
 #pragma unroll
                 for (int i = 0; i < 8; ++i) {
-                    weight[i] = __builtin_amdgcn_exp2f(fmaf(s[g >> 1][8 * (g & 1) + i], info[g].key_scale, offset));
-                    sum += weight[i];
+                    weight[i] = __builtin_amdgcn_exp2f(fmaf(s[g >> 1][8 * (g & 1) + i], scale, -base));
+                    l += weight[i];
                 }
-                l = fmaf(sum, info[g].value_inverse, l);
                 const Pieces<NS> wp = split<NS>(weight);
 #pragma unroll
                 for (int c = 0; c < kCols; ++c)
@@ -486,7 +470,7 @@ int launch_attn_prefill(int dtype, int head_dim, const AttnParams &p, int num_cu
     const PrefillParams pp = {p, 0, 1};
     const bool bf = dtype == MOE_DTYPE_BF16;
     // Rows of 256 and two waves a SIMD; fp32 and 256 dimensions need the registers of both.  Rows of 128 too where tiles of 256 would be fewer than
-    // the CUs: staging costs twice as much a row then (8192 tokens of 16 heads: 467 us, 313 with 256), but more CUs work.
+    // the CUs: staging costs twice as much a row then (8192 tokens of 16 heads: 467 us, 313 with 256 at the time), but more CUs work.
     const bool small = ((int64_t)p.T * p.group / 256 + p.B) * p.n_kv_heads < num_cus;
     if (bf && small && head_dim == 64) return launch_as<64, 1, 4>(pp, num_cus, s);
     if (bf && small && head_dim == 128) return launch_as<128, 1, 4>(pp, num_cus, s);

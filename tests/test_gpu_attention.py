@@ -210,6 +210,24 @@ def test_large_scores_and_scales(n, kv):
     b.attend()
 
 
+@pytest.mark.parametrize("n", [1, 40])
+@pytest.mark.parametrize("page", [16, 64])
+def test_pages_of_zeros_and_tiny_values_keep_their_weight(n, page):
+    """A page whose values are all zero has the smallest scale; its keys take their share of the softmax all the same.  Pages whose scales
+    are far apart, in either direction."""
+    b = Batch([n, 1], [n + 200, 130], 4, 2, 64, page, rot=64).fill()
+    first, second = b.table[0][0], b.table[0][1]
+    b.cache["v"][first], b.cache["v_scale"][first] = 0, 2.0 ** -126
+    b.attend()
+    b.cache["v_scale"][first], b.cache["v_scale"][second] = 2.0 ** -126, 2.0 ** 100
+    b.attend()
+    b.cache["v"][first, :, :page // 2] = 0x30                              # 0.5 of 2^90
+    b.cache["v_scale"][first], b.cache["v_scale"][second] = 2.0 ** 90, 2.0 ** -100
+    b.attend()
+    b.cache["k"][first], b.cache["k_scale"][first] = 0, 2.0 ** -126
+    b.attend()
+
+
 @pytest.mark.parametrize("n", [1, 64])
 def test_parts_joined_by_lse_are_the_whole(n):
     """Two calls over halves of the keys, joined with their lse, against one over all of them (cross attention)."""
