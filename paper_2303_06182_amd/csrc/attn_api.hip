@@ -12,8 +12,12 @@ int64_t sample_workspace(int B, int V);
 
 namespace {
 
-// Rows (new tokens times heads of a group) up to which a sequence is the decode kernel's, 16 at a time.
-constexpr int kFewRows = 32;
+// Rows (new tokens times heads of a group) up to which a sequence is the decode kernel's, 16 at a time: it reads the cache once for each 16, the
+// prefill kernel once for 128 or 256, which it computes whether they are there or not.  64 sequences of 2048 keys, decode / prefill, us:
+//   4 key heads of 128, bf16   32 rows 51 / 88    48 rows 75 / 89     64 rows 80 / 89     128 rows 148 / 91
+//   16 key heads of 64, bf16   32 rows 94 / 168   48 rows 135 / 169   64 rows 182 / 170   128 rows 342 / 176
+//   16 key heads of 64, fp32   32 rows 145 / 175  48 rows 211 / 212   64 rows 279 / 213
+constexpr int kFewRows = 48;
 
 bool bad_ptr(const void *p, const char *name, int align, bool nullable = false)
 {

@@ -176,6 +176,11 @@ def test_sequences_around_few_rows_in_one_batch():
     Batch([32, 33, 2], [40, 400, 90], 2, 2, 128, 16, "f32").fill().attend()
 
 
+def test_sequences_around_48_rows_in_one_batch():
+    Batch([12, 13, 1, 0, 11, 40], [200, 13, 70, 5, 11, 333], 8, 2, 64, 32).fill().attend()
+    Batch([48, 49, 2], [60, 400, 90], 2, 2, 128, 16, "f32").fill().attend()
+
+
 @pytest.mark.parametrize("n", [1, 50])
 def test_pages_past_32_bits(n):
     """A cache of more than 2^32 bytes: the same contents in its last pages give the same outputs, and appending lands there."""
