@@ -11,12 +11,14 @@
 // fp32 queries and weights are three bf16 numbers each (8 bits of the mantissa a piece), one MFMA per piece: the bytes are bf16
 // exactly, so nothing else is lost.
 //
-// Bound by HBM: 2 DH bytes a key, at 16 columns 32 MFMAs of 16 cycles per 16 KB and SIMD, far below.  Split: the tiles of all
-// (sequence, rows, head) units lie in one row; every block takes the same number of them, whatever the lengths are, and every wave
+// Bound by HBM: 2 DH bytes a key, at 16 columns 32 MFMAs of 16 cycles per 16 KB and SIMD, far below; short calls by latency.  Split: where
+// the units (sequence, 16 rows, key head) are short, a block a unit and each wave an equal part of its tiles, joined in LDS.  Else the tiles of all
+// units lie in one row; every block takes the same number of them, whatever the lengths are, and every wave
 // a quarter of the block's.  A wave works alone until its tiles are done: units that lie inside its part are written at once, the one
 // or two that do not are left in LDS, where the block joins them; what reaches past the block is joined by a second kernel.
 // (With the waves of a block on one unit at a time, joined after each, short sequences cost a block 8 us a unit: 32 sequences of up to
 // 1111 keys, 16 heads of 64, fp32 41 us.)
+// Measured: 64 sequences of up to 16384 keys, 32 heads over 4 of 128, 116 MB: 31 us, 3.7 TB/s (a kernel that only sums reads 4.0), and 7 to join.
 #include "attn_dev.h"
 
 #include <mutex>
@@ -45,15 +47,16 @@ __device__ __forceinline__ int64_t seq_cost(const AttnParams &p, int b, int tile
     if (sq.n == 0 || sq.n * p.group > p.few_rows) return 0;
     int first, count;
     seq_range(p, sq, tile, first, count);
-    return (int64_t)(p.whole_units ? 1 : count) * ceil_div(sq.n * p.group, 16) * p.n_kv_heads;
+    return (int64_t)count * ceil_div(sq.n * p.group, 16) * p.n_kv_heads;
 }
 
 // Exclusive prefix of the sequences' tiles into begin[0 .. B] (LDS).  All threads.
+template <int W>
 __device__ void scan_sequences(const AttnParams &p, int tile, int64_t *begin, int64_t *wave_sum)
 {
     const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6;
     int64_t carry = 0;
-    for (int base = 0; base < p.B; base += kThreads) {
+    for (int base = 0; base < p.B; base += 64 * W) {
         const int b = base + tid;
         const int64_t mine = b < p.B ? seq_cost(p, b, tile) : 0;
         int64_t sum = mine;
@@ -65,7 +68,7 @@ __device__ void scan_sequences(const AttnParams &p, int tile, int64_t *begin, in
         if (lane == 63) wave_sum[w] = sum;
         __syncthreads();
         int64_t before = carry;
-        for (int i = 0; i < kWaves; ++i) {
+        for (int i = 0; i < W; ++i) {
             if (i < w) before += wave_sum[i];
             carry += wave_sum[i];
         }
@@ -138,13 +141,13 @@ struct Piece {
     int64_t unit_begin;  // first tile of the unit, -1: nothing here
     int b, unit, run, count;
 };
-template <int DH>
+template <int DH, int W>
 struct Shared {
     static constexpr int kRow = DH + 4;
-    Piece piece[kWaves][2];
-    float m[kWaves][2][16], l[kWaves][2][16];
-    int64_t wave_sum[kWaves];
-    float o[kWaves][2][16 * kRow];
+    Piece piece[W][2];
+    float m[W][2][16], l[W][2][16];
+    int64_t wave_sum[W];
+    float o[W][2][16 * kRow];
 };
 
 // four outputs of a row, from dimension dim on
@@ -165,29 +168,34 @@ __device__ __forceinline__ int64_t row_out(const AttnParams &p, const Seq &sq, i
     return tok < sq.n ? (int64_t)(sq.first + tok) * p.n_heads + h * p.group + (r - tok * p.group) : -1;
 }
 
-// DH: head dimension; NS: bf16 pieces of an fp32 number (1: bf16 queries and weights rounded once); M: blocks a CU holds
-template <int DH, int NS, int M>
-__global__ __launch_bounds__(kThreads, M) void attn_decode_kernel(AttnParams p)
+// DH: head dimension; NS: bf16 pieces of an fp32 number (1: bf16 queries and weights rounded once); M: blocks a CU holds; W: waves.
+// WHOLE: a block takes a whole unit
+template <int DH, int NS, int M, int W, bool WHOLE>
+__global__ __launch_bounds__(64 * W, M) void attn_decode_kernel(AttnParams p)
 {
     static constexpr int kTile = tile_keys(DH), kBlocks = kTile / 16, kChunks = DH / 64, kCols = DH / 16, kWords = DH / 64;
-    static constexpr int kRow = Shared<DH>::kRow;
+    static constexpr int kRow = Shared<DH, W>::kRow;
     extern __shared__ __align__(16) uint8_t lds[];
-    Shared<DH> &sh = *reinterpret_cast<Shared<DH> *>(lds);
-    int64_t *begin = reinterpret_cast<int64_t *>(lds + sizeof(Shared<DH>));  // [B + 1]
+    Shared<DH, W> &sh = *reinterpret_cast<Shared<DH, W> *>(lds);
+    int64_t *begin = reinterpret_cast<int64_t *>(lds + sizeof(Shared<DH, W>));  // [B + 1]
     const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int l15 = lane & 15, g = lane >> 4;
 
-    if (tid < 2 * kWaves) sh.piece[tid >> 1][tid & 1].unit_begin = -1;
-    scan_sequences(p, kTile, begin, sh.wave_sum);
-    // this block's part of the tiles, and this wave's of it; or (whole_units) this block's unit
-    const int64_t total = begin[p.B], per = p.whole_units ? 1 : tiles_per_block(total, p.n_blocks);
-    if (blockIdx.x == 0 && !p.whole_units)  // for the kernel that joins
-        for (int b = tid; b <= p.B; b += kThreads) p.seq_tiles[b] = begin[b];
-    const int64_t t_begin = (int64_t)blockIdx.x * per, t_end = min(total, t_begin + per);
-    if (t_begin >= t_end) return;
-    const int64_t w_begin = p.whole_units ? t_begin : t_begin + w * (per / kWaves), w_end = p.whole_units ? t_end : min(t_end, w_begin + per / kWaves);
-    int b = 0;
-    if (w_begin < w_end) {  // the sequence that holds w_begin: the last one that begins at or before it
+    if (tid < 2 * W) sh.piece[tid >> 1][tid & 1].unit_begin = -1;
+    // this block's unit, or its part of the tiles and this wave's of it
+    int64_t t_begin = 0, w_begin = 0, w_end = 1;
+    int b = WHOLE ? (int)blockIdx.x / p.units : 0;
+    if (!WHOLE) {
+        scan_sequences<W>(p, kTile, begin, sh.wave_sum);
+        const int64_t total = begin[p.B], per = tiles_per_block(total, p.n_blocks);
+        if (blockIdx.x == 0)  // for the kernel that joins
+            for (int i = tid; i <= p.B; i += 64 * W) p.seq_tiles[i] = begin[i];
+        t_begin = (int64_t)blockIdx.x * per;
+        const int64_t t_end = min(total, t_begin + per);
+        if (t_begin >= t_end) return;
+        w_begin = t_begin + w * (per / W), w_end = min(t_end, w_begin + per / W);
+    }
+    if (!WHOLE && w_begin < w_end) {  // the sequence that holds w_begin: the last one that begins at or before it
         int lo = 0, hi = p.B;
         while (hi - lo > 1) {
             const int mid = (lo + hi) >> 1;
@@ -197,20 +205,22 @@ __global__ __launch_bounds__(kThreads, M) void attn_decode_kernel(AttnParams p)
         b = lo;
     }
     for (int64_t t = w_begin; t < w_end;) {
-        while (begin[b + 1] <= t) ++b;
+        if (!WHOLE)
+            while (begin[b + 1] <= t) ++b;
         const int bu = __builtin_amdgcn_readfirstlane(b);
         const Seq sq = load_seq(p, bu);
         int first, count;
         seq_range(p, sq, kTile, first, count);
-        const int local = (int)(t - begin[bu]);
         int unit, tile0, run;
-        if (p.whole_units) {
-            const int each = ceil_div(count, kWaves);
-            unit = local;
+        if (WHOLE) {
+            const int each = ceil_div(count, W);
+            unit = (int)blockIdx.x % p.units;
+            if (sq.n * p.group > p.few_rows || unit >= ceil_div(sq.n * p.group, 16) * p.n_kv_heads) return;
             tile0 = w * each;
             run = min(each, count - tile0);
             if (run <= 0) break;
         } else {
+            const int local = (int)(t - begin[bu]);
             unit = local / count;
             tile0 = local - unit * count;
             run = (int)min(w_end - t, (int64_t)(count - tile0));
@@ -373,27 +383,56 @@ __global__ __launch_bounds__(kThreads, M) void attn_decode_kernel(AttnParams p)
                 sh.m[w][slot][l15] = m;
                 sh.l[w][slot][l15] = l;
             }
-            if (lane == 0) sh.piece[w][slot] = {p.whole_units ? t : begin[bu] + (int64_t)unit * count, bu, unit, run, count};
+            if (lane == 0) sh.piece[w][slot] = {WHOLE ? 0 : begin[bu] + (int64_t)unit * count, bu, unit, run, count};
         }
-        t += p.whole_units ? 1 : run;
+        t += WHOLE ? 1 : run;
     }
     __syncthreads();
+    if (WHOLE) {  // what the first waves have, all as much, of one unit
+        const Piece piece = sh.piece[0][0];
+        if (piece.unit_begin < 0) return;
+        const int waves = ceil_div(piece.count, piece.run);
+        const Seq sq = load_seq(p, piece.b);
+        for (int e = tid * 4; e < 16 * DH; e += 64 * W * 4) {
+            const int row = e / DH, dim = e - row * DH;
+            float m[W], l = 0.f, top = -INFINITY;
+            float4 x[W], sum = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+            for (int k = 0; k < W; ++k) {
+                m[k] = k < waves ? sh.m[k][0][row] : -INFINITY;
+                x[k] = *reinterpret_cast<const float4 *>(sh.o[k < waves ? k : 0][0] + row * kRow + dim);
+                top = fmaxf(top, m[k]);
+            }
+#pragma unroll
+            for (int k = 0; k < W; ++k) {
+                const float scale = m[k] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m[k] - top);
+                l = fmaf(sh.l[k < waves ? k : 0][0][row], scale, l);
+                sum.x = fmaf(x[k].x, scale, sum.x), sum.y = fmaf(x[k].y, scale, sum.y), sum.z = fmaf(x[k].z, scale, sum.z), sum.w = fmaf(x[k].w, scale, sum.w);
+            }
+            const int64_t at = row_out(p, sq, piece.unit, row);
+            if (at < 0) continue;
+            const float inv = l > 0.f ? 1.f / l : 0.f;
+            store_out<NS>(p, at * DH + dim, make_float4(sum.x * inv, sum.y * inv, sum.z * inv, sum.w * inv));
+            if (dim == 0 && p.lse) p.lse[at] = l > 0.f ? top * kLn2 + logf(l) : -INFINITY;
+        }
+        return;
+    }
     // the block's pieces, in the order of the tiles; those of one unit follow each other
-    for (int i = 0; i < 2 * kWaves;) {
+    for (int i = 0; i < 2 * W;) {
         const Piece piece = sh.piece[i >> 1][i & 1];
         if (piece.unit_begin < 0) {
             ++i;
             continue;
         }
         int end = i + 1, run = piece.run;
-        for (; end < 2 * kWaves; ++end) {
+        for (; end < 2 * W; ++end) {
             const Piece &other = sh.piece[end >> 1][end & 1];
             if (other.unit_begin >= 0 && other.unit_begin != piece.unit_begin) break;
             if (other.unit_begin >= 0) run += other.run;
         }
         const Seq sq = load_seq(p, piece.b);
         float *part = p.part + ((int64_t)blockIdx.x * 2 + (piece.unit_begin > t_begin ? 1 : 0)) * part_floats<DH>();
-        for (int e = tid * 4; e < 16 * DH; e += kThreads * 4) {
+        for (int e = tid * 4; e < 16 * DH; e += 64 * W * 4) {
             const int row = e / DH, dim = e - row * DH;
             float top = -INFINITY, l = 0.f;
             for (int k = i; k < end; ++k)
@@ -480,31 +519,47 @@ __global__ __launch_bounds__(kThreads) void attn_join_kernel(AttnParams p, int r
 template <int DH, int NS>
 constexpr int blocks_per_cu() { return DH == 256 || (DH == 128 && NS == 3) ? 1 : 2; }
 
-template <int DH, int NS>
-int launch_as(AttnParams p, int num_cus, hipStream_t s)
+template <int DH, int NS, int W, bool WHOLE>
+int launch_waves(const AttnParams &p, int64_t blocks, hipStream_t s)
 {
-    static constexpr int M = blocks_per_cu<DH, NS>();
-    p.n_blocks = M * num_cus;
-    static constexpr size_t kMost = sizeof(Shared<DH>) + (MOE_ATTN_MAX_B + 1) * 8;
+    static constexpr int M = W == kWaves ? blocks_per_cu<DH, NS>() : 1;  // waves of 256 registers in any case
+    static constexpr size_t kMost = sizeof(Shared<DH, W>) + (MOE_ATTN_MAX_B + 1) * 8;
     static_assert(kMost <= 160 * 1024, "the sequences' places have to fit the LDS beside the pieces");
-    const size_t lds = sizeof(Shared<DH>) + (p.B + 1) * 8;
+    const size_t lds = sizeof(Shared<DH, W>) + (WHOLE ? 0 : (p.B + 1) * 8);
     static std::once_flag once;
     static hipError_t setup_rc = hipSuccess;
     std::call_once(once, [&]() {
-        setup_rc = hipFuncSetAttribute(reinterpret_cast<const void *>(attn_decode_kernel<DH, NS, M>), hipFuncAttributeMaxDynamicSharedMemorySize, (int)kMost);
+        setup_rc = hipFuncSetAttribute(reinterpret_cast<const void *>(attn_decode_kernel<DH, NS, M, W, WHOLE>), hipFuncAttributeMaxDynamicSharedMemorySize, (int)kMost);
     });
     MOE_HIP_CHECK(setup_rc);
-    const int64_t rows = (int64_t)p.max_q * p.group < p.few_rows ? (int64_t)p.max_q * p.group : p.few_rows;
-    const int units = ceil_div((int)rows, 16) * p.n_kv_heads, unit_rows = rows < 16 ? (int)rows : 16;
-    // Where no unit has more than four tiles a wave, or eight and there are units for every CU, a block takes a whole unit and nothing is left to
-    // join.  (32 sequences of up to 1111 keys, 16 heads of 64, fp32: 20.8 us, in parts 23.3; one sequence of 900 keys: 13.0 and 14.5 in the kernels.)
-    const int tiles = ceil_div(p.max_kv, tile_keys(DH));
-    p.whole_units = tiles <= 4 * kWaves || (tiles <= 8 * kWaves && (int64_t)units * p.B >= num_cus);
-    const int64_t blocks = p.whole_units ? (int64_t)units * p.B : p.n_blocks;
-    hipLaunchKernelGGL((attn_decode_kernel<DH, NS, M>), dim3((unsigned)blocks), dim3(kThreads), lds, s, p);
+    hipLaunchKernelGGL((attn_decode_kernel<DH, NS, M, W, WHOLE>), dim3((unsigned)blocks), dim3(64 * W), lds, s, p);
     MOE_LAUNCH_CHECK("attn_decode_kernel");
-    if (p.whole_units) return MOE_OK;
-    hipLaunchKernelGGL((attn_join_kernel<DH, NS>), dim3(units * unit_rows, p.B), dim3(kThreads), 0, s, p, unit_rows);
+    return MOE_OK;
+}
+
+template <int DH, int NS>
+int launch_as(AttnParams p, int num_cus, hipStream_t s)
+{
+    p.n_blocks = blocks_per_cu<DH, NS>() * num_cus;
+    const int64_t rows = (int64_t)p.max_q * p.group < p.few_rows ? (int64_t)p.max_q * p.group : p.few_rows;
+    p.units = ceil_div((int)rows, 16) * p.n_kv_heads;
+    const int unit_rows = rows < 16 ? (int)rows : 16;
+    // Where no unit has more than four tiles a wave, or eight and there are units for every CU, a block takes a whole unit: it need not look for its
+    // part, and nothing is left to join.  Where there are not, and a CU has the registers, twice the waves take it.  us a call, whole / in parts / by
+    // eight waves:
+    //    1 x 1000 keys, 16 heads of 64     10.5 / 13.5 / 10.4       1 x 1000, 8 heads of 128    14.3 / 19.2 / 12.7
+    //    8 x 2000 keys, 16 heads of 64        - / 18.1 / 14.1       8 x 2000, 8 heads of 128       - / 19.4 / 19.6
+    //   64 x 2000 keys, 16 heads of 64     51.7 / 74.0 / 56.5     256 x 500, 16 heads of 64     55.6 / -    / 92.0
+    static constexpr bool kTwice = blocks_per_cu<DH, NS>() == 2;
+    const int tiles = ceil_div(p.max_kv, tile_keys(DH));
+    const bool every = (int64_t)p.units * p.B >= num_cus;
+    if (tiles <= 4 * kWaves || (tiles <= 8 * kWaves && (every || (kTwice && DH == 64)))) {
+        if (kTwice && !every && tiles > kWaves) return launch_waves<DH, NS, kTwice ? 2 * kWaves : kWaves, true>(p, (int64_t)p.units * p.B, s);
+        return launch_waves<DH, NS, kWaves, true>(p, (int64_t)p.units * p.B, s);
+    }
+    const int failed = launch_waves<DH, NS, kWaves, false>(p, p.n_blocks, s);
+    if (failed) return failed;
+    hipLaunchKernelGGL((attn_join_kernel<DH, NS>), dim3(p.units * unit_rows, p.B), dim3(kThreads), 0, s, p, unit_rows);
     MOE_LAUNCH_CHECK("attn_join_kernel");
     return MOE_OK;
 }

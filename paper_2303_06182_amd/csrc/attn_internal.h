@@ -30,7 +30,7 @@ struct AttnParams {
     float *part;
     int64_t *seq_tiles;
     int n_blocks;
-    int whole_units;                       // the decode kernel's blocks take whole units
+    int units;                             // of a sequence at most: pieces of 16 rows times key heads
     int few_rows;                          // sequences of up to so many rows (new tokens times group) are the decode kernel's
 };
 
