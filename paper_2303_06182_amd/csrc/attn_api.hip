@@ -14,10 +14,11 @@ namespace {
 
 // Rows (new tokens times heads of a group) up to which a sequence is the decode kernel's, 16 at a time: it reads the cache once for each 16, the
 // prefill kernel once for 128 or 256, which it computes whether they are there or not.  64 sequences of 2048 keys, decode / prefill, us:
-//   4 key heads of 128, bf16   32 rows 51 / 88    48 rows 75 / 89     64 rows 80 / 89     128 rows 148 / 91
-//   16 key heads of 64, bf16   32 rows 94 / 168   48 rows 135 / 169   64 rows 182 / 170   128 rows 342 / 176
-//   16 key heads of 64, fp32   32 rows 145 / 175  48 rows 211 / 212   64 rows 279 / 213
-constexpr int kFewRows = 48;
+//   4 key heads of 128, bf16   16 rows 33 / 88    48 rows 64 / 90     64 rows 69 / 90     96 rows 98 / 91
+//   16 key heads of 64, bf16   16 rows 58 / 168   48 rows 118 / 171   64 rows 156 / 171   96 rows 225 / 176
+//   4 key heads of 128, fp32   16 rows 39 / 167   48 rows 107 / 169   64 rows 139 / 170   96 rows 202 / 172
+//   16 key heads of 64, fp32   16 rows 68 / 171   48 rows 182 / 212   64 rows 238 / 213   96 rows 338 / 223
+constexpr int kFewRows = 64;
 
 bool bad_ptr(const void *p, const char *name, int align, bool nullable = false)
 {

@@ -181,6 +181,12 @@ def test_sequences_around_48_rows_in_one_batch():
     Batch([48, 49, 2], [60, 400, 90], 2, 2, 128, 16, "f32").fill().attend()
 
 
+def test_sequences_around_64_rows_in_one_batch():
+    Batch([16, 17, 1, 0, 15, 40], [200, 17, 70, 5, 15, 333], 8, 2, 64, 32).fill().attend()
+    Batch([64, 65, 2], [90, 400, 90], 2, 2, 128, 16, "f32").fill().attend()
+    Batch([16, 17], [3000, 2500], 4, 1, 256, 64).fill().attend()
+
+
 @pytest.mark.parametrize("n", [1, 50])
 def test_pages_past_32_bits(n):
     """A cache of more than 2^32 bytes: the same contents in its last pages give the same outputs, and appending lands there."""
