@@ -12,7 +12,9 @@
  * STATIC gating the paper replaces (Sec. 3.2, Sec. 5.1: fixed capacity per
  * expert, one-hot dispatch masks multiplied with the tokens, drops and zero
  * padding) is exported as a baseline for comparison.  Expert Buffering (Sec. 6:
- * expert parameters in host memory behind a small device cache) is at the end.
+ * expert parameters in host memory behind a small device cache), expert weights
+ * of 8 and 4 bits and the rest of a decoder step (a paged cache of keys and
+ * values, attention over it, sampling) are at the end.
  *
  * Conventions for every call
  *   - Plain C.  Returns MOE_OK (0) or a negative MOE_ERR_* code; after an error

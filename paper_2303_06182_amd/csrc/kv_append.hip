@@ -9,6 +9,9 @@
 // Angles are position * frequency in 64 bits: at position 10^5 an fp32 product is off by 4e-3 rad, more than bf16 keeps.  sin and
 // cos of the remainder too, by their series over an eighth of a turn (below), so the rotated key is the fp32 number nearest to
 // the exact one nearly always, and a page's scale does not depend on how the rotation was computed.
+//
+// Bound by HBM for many tokens, by latency for few.  Measured: 24 sequences, 6272 tokens, 16 heads of 128, half of them turned: 37 us for 128 MB,
+// 3.5 TB/s (a large copy: 4.8); 256 sequences of one token, 32 / 8 heads of 128: 7.9 us; one token: 4.8.
 #include "attn_internal.h"
 
 namespace moe355 {
