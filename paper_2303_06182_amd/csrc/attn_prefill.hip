@@ -62,6 +62,11 @@ __device__ __forceinline__ void tile_range(const AttnParams &p, const Seq &sq, i
     count = ceil_div(end, kTile) - first;
 }
 
+// Tiles between two barriers: while these are computed the next ones are stored.  With two, waves need not keep step so closely, and 8 waves' block
+// has the LDS for four buffers.
+template <int W>
+constexpr int kTogether = W == 8 ? 2 : 1;
+
 // A partial result: the rows' outputs (not divided by the sum), maxima, sums
 template <int DH, int W>
 constexpr int64_t part_floats() { return (int64_t)32 * W * (DH + 2); }
@@ -73,7 +78,7 @@ __global__ __launch_bounds__(64 * W, NS == 1 && DH <= 128 ? 2 : 1) void attn_pre
     static constexpr int kKItems = (4 * DH + kRole - 1) / kRole;  // 16 bytes of a key each
     static constexpr int kVItems = (2 * DH + kRole - 1) / kRole;  // 4 dimensions of 8 values each
     static constexpr int kWords = kKItems * 4 > kVItems * 8 ? kKItems * 4 : kVItems * 8;
-    static constexpr int kSteps = DH / 16, kCols = DH / 32;
+    static constexpr int kSteps = DH / 16, kCols = DH / 32, kNext = kTogether<W>;
     static constexpr int kValues = DH <= 128 ? 2 : 1;  // fragments of the values in registers: of this 16 keys and the next, where they fit
     extern __shared__ __align__(16) uint8_t lds[];
     Buffer<DH> *buffer = reinterpret_cast<Buffer<DH> *>(lds);
@@ -248,18 +253,21 @@ __global__ __launch_bounds__(64 * W, NS == 1 && DH <= 128 ? 2 : 1) void attn_pre
 
     if (count > 0) {
         look_up(first * kTile);
-        load(first * kTile);
-        look_up((first + 1) * kTile);
-        store(buffer[0]);
+#pragma unroll
+        for (int i = 0; i < kNext; ++i) {  // past the last tile: zeros, which nobody reads
+            load((first + i) * kTile);
+            look_up((first + i + 1) * kTile);
+            store(buffer[i]);
+        }
         __syncthreads();
     }
     for (int t = 0; t < count; ++t) {
         const int key0 = (first + t) * kTile;
-        if (t + 1 < count) {
-            load(key0 + kTile);
-            look_up(key0 + 2 * kTile);
+        if (t + kNext < count) {
+            load(key0 + kNext * kTile);
+            look_up(key0 + (kNext + 1) * kTile);
         }
-        const Buffer<DH> &buf = buffer[t & 1];
+        const Buffer<DH> &buf = buffer[t % (2 * kNext)];
         if (key0 < any_end && key0 + kTile > any_begin) {
             // Fragments are asked for kAhead steps before their MFMAs, and the order is kept by scheduling barriers: left to itself the
             // compiler asks for two and waits for them (prefill of 8192 tokens 355 us, matrix pipes busy 30 %).
@@ -342,8 +350,8 @@ __global__ __launch_bounds__(64 * W, NS == 1 && DH <= 128 ? 2 : 1) void attn_pre
                 __builtin_amdgcn_sched_barrier(0);
             }
         }
-        if (t + 1 < count) store(buffer[(t + 1) & 1]);
-        __syncthreads();
+        if (t + kNext < count) store(buffer[(t + kNext) % (2 * kNext)]);
+        if (t % kNext == kNext - 1) __syncthreads();
     }
     l += __shfl_xor(l, 32, 64);
     // o[c][i] of a lane is dimension 32 c + 8 (i / 4) + 4 half + i % 4 of its query
@@ -432,7 +440,7 @@ int splits_for(int64_t units, int64_t filled, int tiles, int num_cus)
 template <int DH, int NS, int W>
 int launch_as(PrefillParams pp, int num_cus, hipStream_t s)
 {
-    static constexpr size_t kLds = 2 * sizeof(Buffer<DH>);
+    static constexpr size_t kLds = 2 * kTogether<W> * sizeof(Buffer<DH>);
     static std::once_flag once;
     static hipError_t setup_rc = hipSuccess;
     std::call_once(once, [&]() {
