@@ -3,7 +3,7 @@
 // A block owns 32 W query rows (new tokens x heads of a group) of a (sequence, key head), a wave 32 of them, and walks tiles of 64
 // keys with a running maximum and sum.  Keys and values are widened to bf16 once for the block on their way into LDS:
 //   K    [64 keys][DH], V^T [DH][64 keys], 16-byte chunks swizzled so that 16 lanes that read a fragment, and 16 that write, meet each
-//        bank once (V's writes: twice); two buffers, the next tile's bytes are in flight while this one is computed
+//        bank once (V's writes: twice); two or four buffers, a later tile's bytes are in flight while this one is computed
 //   S^T = K Q^T and O^T = V^T P^T by 32x32x16 MFMAs; queries stay in registers.  A lane holds 4 keys in 8 of one query; a chunk of
 //        V^T holds just those keys in just that order, so the weights are the second product's operand where the first left them.
 // The maximum, the sum and the rescaling of a query are its lane's own; two lanes share a query.  The scales are powers of two, which the
@@ -14,7 +14,8 @@
 //
 // Bound by the matrix cores and the exponentials (a quarter of the rate of other instructions) in about equal parts: per 32 x 64 weights
 // and wave 32 MFMAs of 32 cycles, 32 exponentials of 16 and some 110 others of 4.  Two waves a SIMD overlap them.  Measured: 8192 tokens, 16
-// heads of 128, bf16, causal: 307 us, 896 TFLOP/s, matrix pipes busy 35 %.
+// heads of 128, bf16, causal: 294 us, 934 TFLOP/s; matrix pipes busy 37 %, vector issue 44 %, LDS reads about 40 %.  (Half of the waves held half a tile behind
+// the others by barriers, so that products meet exponentials: 327; other priorities of the waves: no difference.)
 //
 // Blocks begin with the last rows, which see the most keys; a sequence's heads stay on one XCD and its L2.  Where there are too few
 // blocks for the chip, the keys are cut into parts, joined by a second kernel.
@@ -63,7 +64,7 @@ __device__ __forceinline__ void tile_range(const AttnParams &p, const Seq &sq, i
 }
 
 // Tiles between two barriers: while these are computed the next ones are stored.  With two, waves need not keep step so closely, and 8 waves' block
-// has the LDS for four buffers.
+// has the LDS for four buffers (8192 tokens of 16 heads of 128: 294 us, with one 307).  A block of 4 shares its CU with another.
 template <int W>
 constexpr int kTogether = W == 8 ? 2 : 1;
 
