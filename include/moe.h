@@ -450,7 +450,8 @@ int64_t moe_attn_workspace_bytes(const moe_attn_handle_t *h);
  * values go into the cache: with need = the smallest power of two, at least 2^-126, that is no less than the largest
  * new element of the (page, head) over 448, its scale s becomes need where the first new row of the page is its row 0,
  * and max(s, need) else; where it grows, rows below the first new one are rounded to e4m3 anew, q <- e4m3(q * s_old / s).
- * New rows are e4m3(x / s), to nearest even.  A page may receive new tokens of one sequence only; rewriting positions
+ * New rows are e4m3(x / s), to nearest even.  New keys and values have to be finite: one that is not spoils what is
+ * computed from its page of its head, for queries that do not see it, too, and nothing else.  A page may receive new tokens of one sequence only; rewriting positions
  * (tokens that were rejected) is fine. */
 int moe_kv_append(moe_attn_handle_t *h, const moe_kv_cache_t *cache, const void *q, int64_t q_stride, const void *k,
                   int64_t k_stride, const void *v, int64_t v_stride, const double *inv_freq, const int32_t *q_offsets,
