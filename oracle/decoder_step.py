@@ -38,21 +38,24 @@ def rotate(x, pos, inv_freq, interleaved):
     return y
 
 
-def append(cache, q, k, v, inv_freq, interleaved, q_offsets, kv_len, page_table, page_size):
+def append(cache, q, k, v, inv_freq, interleaved, q_offsets, kv_len, page_table, page_size, max_q=None):
+    """max_q: a sequence's further new tokens are left out (their rows of the result are the queries as they came)."""
     q_out = None if q is None else np.array(q, dtype=np.float64)
     num_pages = cache["k"].shape[0]
     for b, kv in enumerate(kv_len):
         lo, hi = q_offsets[b], q_offsets[b + 1]
         begin = kv - (hi - lo)
+        n = hi - lo if max_q is None else min(hi - lo, max_q)
+        end = min(kv, begin + n)
         if q is not None:
-            for t in range(lo, hi):
+            for t in range(lo, lo + n):
                 q_out[t] = rotate(q[t], begin + t - lo, inv_freq, interleaved)
         first = max(begin, 0)
-        for slot in range(first // page_size, -(-kv // page_size) if hi > lo else 0):
+        for slot in range(first // page_size, -(-end // page_size) if n > 0 else 0):
             page = page_table[b][slot]
             if not 0 <= page < num_pages:
                 continue
-            rows = range(max(first, slot * page_size), min(kv, (slot + 1) * page_size))
+            rows = range(max(first, slot * page_size), min(end, (slot + 1) * page_size))
             if not len(rows):
                 continue
             r0 = rows[0] - slot * page_size
@@ -72,21 +75,23 @@ def append(cache, q, k, v, inv_freq, interleaved, q_offsets, kv_len, page_table,
     return q_out
 
 
-def attend(cache, q, q_offsets, kv_len, page_table, page_size, scale, causal=True, window=0):
+def attend(cache, q, q_offsets, kv_len, page_table, page_size, scale, causal=True, window=0, max_q=None, max_kv=None):
+    """max_q, max_kv: a sequence's further new tokens (rows of zeros here), and its further keys, are left out."""
     T, heads, dim = q.shape
     num_pages, kv_heads = cache["k"].shape[:2]
     out, absolute, lse = np.zeros((T, heads, dim)), np.zeros((T, heads, dim)), np.full((T, heads), -np.inf)
     spread = np.zeros((T, heads))                                          # largest sum of |q k| of a row, times scale
-    for b, kv in enumerate(kv_len):
+    for b, length in enumerate(kv_len):
         lo, hi = q_offsets[b], q_offsets[b + 1]
+        kv = length if max_kv is None else min(length, max_kv)
         slots = [page_table[b][s] for s in range(-(-kv // page_size))]
         held = np.array([0 <= slots[p // page_size] < num_pages for p in range(kv)], dtype=bool)
         at = [(slots[p // page_size], p % page_size) for p in range(kv)]
         for h in range(kv_heads):
             key, value = (np.array([VALUES[cache[n][pg, h, r]] * float(cache[n + "_scale"][pg, h]) if ok else np.zeros(dim)
                                     for (pg, r), ok in zip(at, held)]).reshape(kv, dim) for n in "kv")
-            for t in range(lo, hi):
-                pos, p = kv - (hi - lo) + t - lo, np.arange(kv)
+            for t in range(lo, hi if max_q is None else min(hi, lo + max_q)):
+                pos, p = length - (hi - lo) + t - lo, np.arange(kv)
                 sees = held.copy()
                 if causal:
                     sees &= p <= pos

@@ -237,10 +237,13 @@ int moe_attn_forward(moe_attn_handle_t *h, const moe_kv_cache_t *cache, const vo
     p.seq_tiles = reinterpret_cast<int64_t *>(static_cast<uint8_t *>(workspace) + need - align_up((int64_t)(c.B_max + 1) * 8, 256));
     p.few_rows = kFewRows;
     const bool many = (int64_t)p.max_q * p.group > kFewRows;
-    // sequences of few rows: none where all sequences have max_q new tokens, and these are many
+    // Sequences of few rows: none where all sequences have max_q new tokens, and these are many.  That is so where there are max_q a sequence, unless one
+    // has more; the prefill kernel then takes sequences of any number of rows, so that each is computed whatever the offsets say.
     if (!many || (int64_t)p.max_q * B > T) {
         const int failed = launch_attn_decode(c.dtype, c.head_dim, p, h->num_cus, (hipStream_t)stream);
         if (failed != MOE_OK) return failed;
+    } else {
+        p.few_rows = 0;
     }
     return many ? launch_attn_prefill(c.dtype, c.head_dim, p, h->num_cus, (hipStream_t)stream) : MOE_OK;
 }

@@ -417,3 +417,28 @@ def test_refusals():
             call()
     out, lse = b.att.moe_attn_forward(cache, q[:0], ints([0, 0, 0]), ints([20, 30]), batch[2], 1, 30)   # nothing to do
     assert out.shape[0] == 0 and lse.shape[0] == 0
+
+
+def bounded(b, max_q, max_kv, causal=True, window=0, unwritten=False):
+    """moe_attn_forward with bounds that may be less than the lengths: the tokens that are left out keep what the outputs held (NaN here), the others
+    are where they are.  unwritten: nobody wrote the rows of the tokens that are left out, nor those past the cache's bound."""
+    if unwritten:
+        for s, kv in enumerate(b.kv):
+            for p in range(max(0, kv - b.n[s] + min(b.n[s], max_q)), kv):
+                for name, byte in (("k", 0x7F), ("v", 0xFF)):
+                    b.cache[name][b.table[s][p // b.page], :, p % b.page] = byte
+    q, q64 = b.rows(b.heads, 1.5)
+    out, lse = torch.full_like(q, math.nan), torch.full((b.T, b.heads), math.nan, device=DEV)
+    scale = b.dim ** -0.5
+    b.att.moe_attn_forward(b.device_cache(), q, *b.args(), max_q, max_kv, scale=scale, causal=causal, window=window, out=out, lse=lse)
+    ref = od.attend(b.cache, q64, b.offsets, b.kv, b.table, b.page, np.float32(scale), causal, window, max_q, max_kv)
+    kept = np.array([t - lo < max_q for lo, hi in zip(b.offsets, b.offsets[1:]) for t in range(lo, hi)])
+    b.check(out[kept], lse[kept], [x[kept] for x in ref])
+    assert out[~kept].isnan().all() and lse[~kept].isnan().all()
+
+
+@pytest.mark.parametrize("n,kv,max_q", [([129, 1], [129, 90], 65), ([300, 5], [300, 40], 100), ([1, 259], [700, 300], 130)])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_every_sequence_is_computed_where_one_is_past_the_bound(n, kv, max_q, dtype):
+    """max_q times the sequences is no more than the tokens there are, and a sequence has few rows all the same."""
+    bounded(Batch(n, kv, 2, 2, 64, 16, dtype).fill(), max_q, max(kv), causal=False)
