@@ -435,9 +435,10 @@ int64_t moe_attn_workspace_bytes(const moe_attn_handle_t *h);
  * kv_len[b] tokens in the cache, the new ones among them: new token i is at position kv_len[b] - n_b + i.
  * page_table [B, max_pages]: position p is row p % page_size of page page_table[b][p / page_size]; entries past a
  * sequence's length are not read.  All three int32 on the device.  max_q (and max_kv) are bounds of n_b (of kv_len)
- * that the host knows; they size the launch, tokens past them are left out.  Lengths outside [0, max_pages * page_size]
- * and offsets outside [0, T] are clamped into the range, and a position whose table entry is outside [0, num_pages)
- * holds nothing: it is neither written nor attended to.
+ * that the host knows; they size the launch.  A sequence's new tokens (keys) past them are left out: their outputs, or
+ * their rows of the cache, are not written (they are not attended to), and the others keep their positions.  Lengths
+ * outside [0, max_pages * page_size] and offsets outside [0, T] are clamped into the range, and a position whose table
+ * entry is outside [0, num_pages) holds nothing: it is neither written nor attended to.
  * q [T, n_heads, head_dim], k and v [T, n_kv_heads, head_dim] elem: a token's heads lie together; from one token to
  * the next it is q_stride (k_stride, v_stride) elements, a multiple of 16 bytes, so q, k and v may be parts of one
  * projection's output.  Outputs are dense. */

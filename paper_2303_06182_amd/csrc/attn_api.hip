@@ -110,8 +110,8 @@ int check_batch(const moe_attn_handle_t *h, const moe_kv_cache_t *cache, const i
     p.num_pages = c.num_pages;
     p.max_pages = c.max_pages;
     p.max_q = max_q < T ? max_q : T;
-    const int32_t room = c.max_pages * c.page_size;
-    p.max_kv = max_kv < room ? max_kv : room;
+    p.room = c.max_pages * c.page_size;
+    p.max_kv = max_kv < p.room ? max_kv : p.room;
     return MOE_OK;
 }
 

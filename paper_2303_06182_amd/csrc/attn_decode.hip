@@ -36,7 +36,7 @@ constexpr int tile_keys(int dh) { return dh <= 128 ? 64 : 32; }
 __device__ __forceinline__ void seq_range(const AttnParams &p, const Seq &sq, int tile, int &first, int &count)
 {
     int lo = 0;
-    if (p.window > 0) lo = max(0, sq.kv - sq.n - p.window + 1);
+    if (p.window > 0) lo = max(0, sq.begin - p.window + 1);
     first = min(lo, sq.kv) / tile;
     count = max(1, ceil_div(sq.kv, tile) - first);
 }
@@ -238,7 +238,7 @@ __global__ __launch_bounds__(64 * W, M) void attn_decode_kernel(AttnParams p)
         const int r = rt * 16 + l15;
         const int tok = r / p.group, head = h * p.group + (r - tok * p.group);
         const bool live = tok < sq.n;
-        const int pos = sq.kv - sq.n + tok;
+        const int pos = sq.begin + tok;
         const int key_end = !live ? 0 : p.causal ? min(pos + 1, sq.kv) : sq.kv;
         const int key_begin = p.window > 0 ? max(0, pos - p.window + 1) : 0;
         Pieces<NS> q[kChunks][2];

@@ -18,7 +18,7 @@ struct AttnParams {
     const int32_t *q_offsets, *kv_len, *page_table;
     int B, T, n_heads, n_kv_heads, group;  // group: query heads of a key head
     int page_shift, num_pages, max_pages;
-    int max_q, max_kv;                     // clamped to what the handle can hold
+    int max_q, max_kv, room;               // clamped to what the handle can hold; room: the most keys of a sequence
     // attention
     const void *q;
     int64_t q_stride;
@@ -34,17 +34,22 @@ struct AttnParams {
     int few_rows;                          // sequences of up to so many rows (new tokens times group) are the decode kernel's
 };
 
-// A sequence's new tokens and length, clamped to what can exist, so that no index derived from them leaves its array.
+// A sequence's new tokens and keys, clamped to what can exist, so that no index derived from them leaves its array.  The bounds max_q and max_kv
+// say what is worked on, not where it is: positions come from the whole lengths.
 struct Seq {
-    int first, n, kv;
+    int first, n;  // new tokens that are worked on, and the first of them
+    int kv;        // keys in front of this one may be seen
+    int begin;     // position of the first new token; negative where there are more of them than the length says
 };
 __device__ __forceinline__ Seq load_seq(const AttnParams &p, int b)
 {
     int lo = p.q_offsets[b], hi = p.q_offsets[b + 1], kv = p.kv_len[b];
     lo = min(max(lo, 0), p.T);
     hi = min(max(hi, lo), p.T);
-    kv = min(max(kv, 0), p.max_kv);
-    return {lo, min(hi - lo, p.max_q), kv};
+    kv = min(max(kv, 0), p.room);
+    const int begin = kv - (hi - lo), n = min(hi - lo, p.max_q);
+    if (p.causal) kv = max(begin + n, 0);  // without the keys of new tokens past max_q, which may not have been written
+    return {lo, n, min(kv, p.max_kv), begin};
 }
 
 struct AppendParams {

@@ -56,7 +56,7 @@ __device__ __forceinline__ int v_at(int dim, int chunk)
 __device__ __forceinline__ void tile_range(const AttnParams &p, const Seq &sq, int row0, int rows, int &first, int &count)
 {
     const int tok0 = row0 / p.group, tok1 = min((row0 + rows - 1) / p.group, sq.n - 1);
-    const int pos0 = sq.kv - sq.n + tok0, pos1 = sq.kv - sq.n + tok1;
+    const int pos0 = sq.begin + tok0, pos1 = sq.begin + tok1;
     const int end = p.causal ? min(sq.kv, max(pos1 + 1, 0)) : sq.kv;
     const int begin = p.window > 0 ? min(max(0, pos0 - p.window + 1), end) : 0;
     first = begin / kTile;
@@ -105,7 +105,7 @@ __global__ __launch_bounds__(64 * W, NS == 1 && DH <= 128 ? 2 : 1) void attn_pre
     const int r = rt * kRows + w * 32 + l31;
     const int tok = r / p.group, head = h * p.group + (r - tok * p.group);
     const bool live = tok < sq.n;
-    const int pos = sq.kv - sq.n + tok;
+    const int pos = sq.begin + tok;
     const int key_end = !live ? 0 : p.causal ? min(pos + 1, sq.kv) : sq.kv;
     const int key_begin = p.window > 0 ? max(0, pos - p.window + 1) : 0;
     // over the wave's rows: keys that all see, and that any sees

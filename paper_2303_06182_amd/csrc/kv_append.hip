@@ -169,12 +169,22 @@ __device__ __forceinline__ void round_anew(uint8_t *page, int bytes, float ratio
 // Heads of queries a thread turns by the same angles: their loads are in flight together, the angles' 40 operations in 64 bits a pair shared.
 constexpr int kQHeads = 4;
 
+// A sequence's new tokens; its keys end with the last of them.
+__device__ __forceinline__ Seq load_new(const AttnParams &p, int b)
+{
+    int lo = p.q_offsets[b], hi = p.q_offsets[b + 1];
+    lo = min(max(lo, 0), p.T);
+    hi = min(max(hi, lo), p.T);
+    const int begin = min(max(p.kv_len[b], 0), p.room) - (hi - lo), n = min(hi - lo, p.max_q);
+    return {lo, n, begin + n, begin};
+}
+
 // Pages that a sequence's new tokens touch, and the first of them.
 __device__ __forceinline__ int pages_of(const AttnParams &p, const Seq &sq, int &first)
 {
-    const int lo = max(sq.kv - sq.n, 0);
+    const int lo = max(sq.begin, 0);
     first = lo >> p.page_shift;
-    return sq.n > 0 && sq.kv > lo ? ((sq.kv - 1) >> p.page_shift) - first + 1 : 0;
+    return sq.kv > lo ? ((sq.kv - 1) >> p.page_shift) - first + 1 : 0;
 }
 
 // The sequence of the index-th touched page of all, and which of its pages that is: every wave adds up the sequences' pages, 64 at a
@@ -184,7 +194,7 @@ __device__ __forceinline__ int page_owner(const AttnParams &p, int index, int &m
     const int lane = threadIdx.x & 63;
     for (int base = 0; base < p.B; base += 64) {
         int first, sum = 0;
-        if (base + lane < p.B) sum = pages_of(p, load_seq(p, base + lane), first);
+        if (base + lane < p.B) sum = pages_of(p, load_new(p, base + lane), first);
         const int mine = sum;
 #pragma unroll
         for (int off = 1; off < 64; off <<= 1) {
@@ -220,7 +230,7 @@ __global__ __launch_bounds__(NT) void kv_append_kernel(AppendParams p, int kv_un
             if (p.a.q_offsets[mid] <= t) lo = mid;
             else hi = mid;
         }
-        const Seq sq = load_seq(p.a, lo);
+        const Seq sq = load_new(p.a, lo);
         const int i = t - sq.first;
         if (i < 0 || i >= sq.n) return;
         const Item it = item_of(e, p.rot_dim, p.interleaved);
@@ -232,7 +242,7 @@ __global__ __launch_bounds__(NT) void kv_append_kernel(AppendParams p, int kv_un
             ry[k] = load8<BF16>(p.a.q, (int64_t)t * p.a.q_stride + (int64_t)h * DH + it.b);
         }
         double c[8], s[8];
-        if (it.turns) angles(p.inv_freq, e, sq.kv - sq.n + i, c, s);
+        if (it.turns) angles(p.inv_freq, e, sq.begin + i, c, s);
 #pragma unroll
         for (int k = 0; k < kQHeads; ++k) {
             const int h = group * kQHeads + k;
@@ -252,12 +262,11 @@ __global__ __launch_bounds__(NT) void kv_append_kernel(AppendParams p, int kv_un
     if (!pages) b = page_owner(p.a, index, m);
     else if (pages > 1) b = index / pages, m = index - b * pages;
     if (b < 0) return;
-    const Seq sq = load_seq(p.a, b);
-    const int begin = sq.kv - sq.n;  // position of the first new token
+    const Seq sq = load_new(p.a, b);
     int slot;
     if (m >= pages_of(p.a, sq, slot)) return;
     slot += m;
-    const int lo = max(max(begin, 0), slot << p.a.page_shift), hi = min(sq.kv, (slot + 1) << p.a.page_shift);
+    const int lo = max(max(sq.begin, 0), slot << p.a.page_shift), hi = min(sq.kv, (slot + 1) << p.a.page_shift);
     if (lo >= hi || slot >= p.a.max_pages) return;
     const int r0 = lo - (slot << p.a.page_shift), rows = hi - lo, items = rows * kItems;
     // the new rows, and beside them the page and its scales
@@ -269,7 +278,7 @@ __global__ __launch_bounds__(NT) void kv_append_kernel(AppendParams p, int kv_un
         const bool is_v = id >= items;
         const int r = (is_v ? id - items : id) / kItems, e = (is_v ? id - items : id) - r * kItems;
         it[u] = is_v ? Item{16 * e, 16 * e + 8, false} : item_of(e, p.rot_dim, p.interleaved);
-        const int64_t t = sq.first + (lo - begin) + r;
+        const int64_t t = sq.first + (lo - sq.begin) + r;
         const void *src = is_v ? p.v_new : p.k_new;
         const int64_t at = t * (is_v ? p.v_stride : p.k_stride) + (int64_t)h * DH;
         rx[u] = load8<BF16>(src, at + it[u].a);

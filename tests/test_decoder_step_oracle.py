@@ -83,3 +83,23 @@ def test_sampling_by_hand():
     assert [od.sample(ties, u, top_k=2)[0] for u in (0.0, 0.49, 0.51, 0.99)] == [1, 1, 2, 2]
     assert od.sample(np.array([-np.inf, np.nan]), 0.5) == (-1, -math.inf)
     assert od.sample(np.array([0.0, np.inf, np.inf]), 0.6)[0] == 2
+
+
+def test_bounds_leave_out_and_move_nothing():
+    """With max_q and max_kv: the rows that are kept are those of the whole call over the keys that are kept, and appending writes a part of what the
+    whole append writes."""
+    rng = np.random.default_rng(2)
+    table, f = [[5, 1, 3, -1]], 10000.0 ** (-np.arange(8) / 8)
+    k, v, q = rng.standard_normal((11, 2, 16)), rng.standard_normal((11, 2, 16)), rng.standard_normal((11, 4, 16))
+    whole, part = empty_cache(6, 2, 4, 16), empty_cache(6, 2, 4, 16)
+    turned = od.append(whole, q, k, v, f, False, [0, 11], [11], table, 4)
+    first = od.append(part, q, k, v, f, False, [0, 11], [11], table, 4, max_q=8)
+    assert np.array_equal(first[:8], turned[:8]) and np.array_equal(first[8:], q[8:])
+    for p, rows in ((5, 4), (1, 4), (3, 0)):
+        assert np.array_equal(part["k"][p, :, :rows], whole["k"][p, :, :rows]) and (part["k"][p, :, rows:] == 0x7F).all()
+    out, lse, *_ = od.attend(whole, turned, [0, 11], [11], table, 4, 0.25)
+    few, few_lse, *_ = od.attend(part, first, [0, 11], [11], table, 4, 0.25, max_q=8)
+    assert np.array_equal(few[:8], out[:8]) and not few[8:].any() and (few_lse[8:] == -np.inf).all()
+    short, *_ = od.attend(whole, turned, [0, 11], [11], table, 4, 0.25, max_kv=6)
+    cross, *_ = od.attend(whole, turned[6:], [0, 5], [6], table, 4, 0.25, causal=False)
+    assert np.array_equal(short[:6], out[:6]) and np.allclose(short[6:], cross, atol=1e-15)

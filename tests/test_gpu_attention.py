@@ -442,3 +442,52 @@ def bounded(b, max_q, max_kv, causal=True, window=0, unwritten=False):
 def test_every_sequence_is_computed_where_one_is_past_the_bound(n, kv, max_q, dtype):
     """max_q times the sequences is no more than the tokens there are, and a sequence has few rows all the same."""
     bounded(Batch(n, kv, 2, 2, 64, 16, dtype).fill(), max_q, max(kv), causal=False)
+
+
+@pytest.mark.parametrize("dtype,dim", [("bf16", 64), ("f32", 128)])
+@pytest.mark.parametrize("causal", [True, False])
+@pytest.mark.parametrize("window", [0, 20])
+def test_bounds_below_the_lengths(dtype, dim, causal, window):
+    """Tokens and keys past max_q and max_kv are left out; positions, masks and windows are those of the whole lengths."""
+    few = lambda: Batch([5, 1, 9, 0, 3], [60, 1, 300, 4, 2], 4, 2, dim, 16, dtype).fill()  # noqa: E731
+    many = lambda: Batch([130, 80, 1, 3], [200, 300, 90, 2], 4, 2, dim, 32, dtype).fill()  # noqa: E731
+    for make, bounds in ((few, [(3, 300), (1, 300), (9, 40), (4, 17), (9, 0)]), (many, [(100, 300), (33, 300), (130, 150), (70, 64)])):
+        for max_q, max_kv in bounds:
+            bounded(make(), max_q, max_kv, causal, window)
+
+
+@pytest.mark.parametrize("n", [6, 150])
+def test_bounds_below_the_lengths_of_long_sequences(n):
+    """As above where units are cut between blocks and joined, and where keys are cut into parts."""
+    for max_q, max_kv in ((n // 2, 9000 + n), (n, 5000), (n - 1, 8999)):
+        bounded(Batch([n, 1], [9000 + n, 3], 2, 1, 64, 64).fill(), max_q, max_kv)
+
+
+@pytest.mark.parametrize("n,max_q", [(5, 3), (200, 120)])
+def test_rows_of_tokens_that_are_left_out_may_be_unwritten(n, max_q):
+    """No causal query that is kept sees them, and what their bytes are (NaN) does not matter."""
+    bounded(Batch([n, 1], [n + 90, 40], 4, 2, 64, 16).fill(), max_q, n + 90, unwritten=True)
+
+
+@pytest.mark.parametrize("max_q", [1, 3, 17, 40])
+def test_append_with_a_bound_below_the_lengths(max_q):
+    """The first max_q new tokens of a sequence land where they belong, by the angles of their positions; nothing else is touched."""
+    for n, kv in (([5, 1, 9, 0, 3], [60, 1, 300, 4, 2]), ([60, 30, 1], [77, 30, 16])):
+        b = Batch(n, kv, 4, 2, 64, 16, "f32", rot=64).fill()
+        (q, q64), (k, k64), (v, v64) = b.rows(4), b.rows(2), b.rows(2)
+        dev, q_out = b.device_cache(), torch.full_like(q, math.nan)
+        b.att.moe_kv_append(dev, q, k, v, torch.from_numpy(b.inv_freq).to(DEV), *b.args(), max_q, q_out=q_out)
+        want = od.append(b.cache, q64, k64, v64, b.inv_freq, b.interleaved, b.offsets, b.kv, b.table, b.page, max_q)
+        for name in ("k", "v", "k_scale", "v_scale"):
+            assert np.array_equal(getattr(dev, name).cpu().numpy(), b.cache[name], equal_nan=name.endswith("scale")), name
+        kept = np.array([t - lo < max_q for lo, hi in zip(b.offsets, b.offsets[1:]) for t in range(lo, hi)])
+        got = q_out.double().cpu().numpy()
+        assert (np.abs(got[kept] - want[kept]) <= 2.0 ** -24 * np.abs(want[kept]) + 1e-11 * np.abs(q64).max()).all()
+        assert np.isnan(got[~kept]).all()
+
+
+@pytest.mark.parametrize("n,kv,max_q", [([129, 1], [129, 90], 65), ([300, 5], [300, 40], 100), ([1, 259], [700, 300], 130)])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_every_sequence_has_its_mask_where_one_is_past_the_bound(n, kv, max_q, dtype):
+    """As above, under the causal mask."""
+    bounded(Batch(n, kv, 2, 2, 64, 16, dtype).fill(), max_q, max(kv))
