@@ -230,7 +230,7 @@ int moe_attn_forward(moe_attn_handle_t *h, const moe_kv_cache_t *cache, const vo
     p.q_stride = q_stride;
     p.scale_log2e = scale * 1.44269504088896340736f;
     p.causal = causal;
-    p.window = window;
+    p.window = window < 1 << 30 ? window : 1 << 30;  // positions lie in (-2^24, 2^30): a difference of one and a window stays in 32 bits
     p.out = out;
     p.lse = lse;
     p.part = static_cast<float *>(workspace);

@@ -491,3 +491,14 @@ def test_append_with_a_bound_below_the_lengths(max_q):
 def test_every_sequence_has_its_mask_where_one_is_past_the_bound(n, kv, max_q, dtype):
     """As above, under the causal mask."""
     bounded(Batch(n, kv, 2, 2, 64, 16, dtype).fill(), max_q, max(kv))
+
+
+@pytest.mark.parametrize("n,kv", [(9, 4), (9, 40), (100, 97), (200, 130)])
+@pytest.mark.parametrize("causal", [True, False])
+@pytest.mark.parametrize("window", [2 ** 31 - 1, 2 ** 31 - 60, 2 ** 30])
+def test_windows_past_every_position_are_no_window(n, kv, causal, window):
+    """Also where the first positions are negative: nothing overflows."""
+    b = Batch([n, 1], [kv, 20], 2, 2, 64, 16).fill()
+    q, out, lse = b.attend(window=window, causal=causal)
+    plain, plain_lse = b.att.moe_attn_forward(b.device_cache(), q, *b.args(), n, max(kv, 20), causal=causal)
+    assert torch.equal(out, plain) and torch.equal(lse, plain_lse)
