@@ -478,7 +478,7 @@ int moe_attn_forward(moe_attn_handle_t *h, const moe_kv_cache_t *cache, const vo
  * ascending index; NaN counts as -infinity, and -infinity is never drawn.  With w = exp((logit - largest) / temperature):
  *   top_k > 0    the first top_k of the order stay;
  *   top_p < 1    of those, the shortest beginning whose w sum to at least top_p times the sum over all of those;
- *   min_p > 0    of those, the ones with w >= min_p;  the first of the order always stays;
+ *   min_p > 0    of those, the ones with w >= min_p (none where it is NaN);  the first of the order always stays;
  *   token        the first, in ascending index, at which the running sum of the remaining w exceeds u times their sum;
  *   temperature <= 0: the first of the order.
  * logprob [B] fp32 (may be NULL): the logarithm of the drawn token's share of the remaining w.  A row with nothing but

@@ -403,7 +403,7 @@ __device__ __forceinline__ Plan plan_of(const SampleParams &p, int b, float larg
     q.top_p = p.top_p ? p.top_p[b] : 1.f;
     q.min_p = p.min_p ? p.min_p[b] : 0.f;
     q.none = largest == -INFINITY;
-    q.only_first = !(temperature > 0.f) || q.min_p > 1.0 || q.top_k == 1 || !(q.top_p > 0.0);
+    q.only_first = !(temperature > 0.f) || !(q.min_p <= 1.0) || q.top_k == 1 || !(q.top_p > 0.0);  // NaN: no weight is at least that
     q.by_count = q.top_k > 0 && q.top_k < p.V;
     q.by_mass = q.top_p < 1.0;
     q.r = {largest, fminf(64.f / temperature, 3e38f), largest < INFINITY ? (double)largest : 1e300, 1.44269504088896340736 / (double)temperature,

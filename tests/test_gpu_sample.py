@@ -145,3 +145,15 @@ def test_same_result_every_time_and_in_a_graph():
         token, logprob = binding.moe_sample(x, u, top_p=top_p, workspace=workspace)
         torch.cuda.synchronize()
         assert torch.equal(got[0], token) and torch.equal(got[1], logprob)
+
+
+@pytest.mark.parametrize("V", [300, 30000])
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_min_p_that_is_no_number_leaves_the_first(V, dtype):
+    """No weight is at least NaN, and the first of the order always stays; alone, with the other filters, and on a row whose last tokens are masked."""
+    B = 4
+    x, rng = logits_of(B, V, dtype, 3)
+    x[:, V // 2:] = -math.inf
+    u = rng.random(B).astype(np.float32)
+    for kw in ({}, dict(top_k=[5] * B), dict(top_p=[0.9] * B), dict(temperature=[0.7] * B)):
+        check(x, u, min_p=[math.nan] * B, **kw)
