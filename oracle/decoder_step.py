@@ -119,7 +119,7 @@ def sample(row, u, temperature=1.0, top_k=0, top_p=1.0, min_p=0.0):
     if top_k > 0:
         order = order[:top_k]
     top = row[order[0]]
-    w = [1.0 if row[i] == top else math.exp((row[i] - top) / temperature) for i in order]
+    w = [1.0 if row[i] == top else 0.0 if top == math.inf else math.exp((row[i] - top) / temperature) for i in order]
     if top_p < 1:
         mass = np.cumsum(np.array(w, dtype=np.longdouble))
         n = 1

@@ -406,7 +406,9 @@ __device__ __forceinline__ Plan plan_of(const SampleParams &p, int b, float larg
     q.only_first = !(temperature > 0.f) || !(q.min_p <= 1.0) || q.top_k == 1 || !(q.top_p > 0.0);  // NaN: no weight is at least that
     q.by_count = q.top_k > 0 && q.top_k < p.V;
     q.by_mass = q.top_p < 1.0;
-    q.r = {largest, fminf(64.f / temperature, 3e38f), largest < INFINITY ? (double)largest : 1e300, 1.44269504088896340736 / (double)temperature,
+    // an infinite logit's share is the same at every temperature, an infinite one among them
+    const bool finite = largest < INFINITY;
+    q.r = {largest, fminf(64.f / temperature, 3e38f), finite ? (double)largest : 1e300, 1.44269504088896340736 / (finite ? (double)temperature : 1.0),
            (double)(1ull << p.bits)};
     return q;
 }

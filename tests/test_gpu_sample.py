@@ -157,3 +157,15 @@ def test_min_p_that_is_no_number_leaves_the_first(V, dtype):
     u = rng.random(B).astype(np.float32)
     for kw in ({}, dict(top_k=[5] * B), dict(top_p=[0.9] * B), dict(temperature=[0.7] * B)):
         check(x, u, min_p=[math.nan] * B, **kw)
+
+
+@pytest.mark.parametrize("V", [300, 30000])
+def test_infinite_logits_and_infinite_temperature(V):
+    """Where the largest logit is +infinity its tokens have w = 1 and the others none, at every temperature; with finite ones an infinite temperature
+    makes all of them equal."""
+    x = torch.full((4, V), -1.0, device=DEV)
+    x[0, 7], x[1, 40:60], x[2, ::2], x[3, 5] = math.inf, math.inf, -math.inf, 3.0
+    u = np.array([0.9, 0.3, 0.77, 0.5])
+    for t in (math.inf, 3e38, 1e30):
+        for kw in ({}, dict(min_p=[0.5] * 4), dict(top_k=[30] * 4), dict(top_p=[0.6] * 4)):
+            check(x, u, temperature=[t] * 4, **kw)
