@@ -536,9 +536,16 @@ __device__ __forceinline__ void sum_segments(const char *row, int from, int to, 
 // Where there are few rows, several blocks share one: three kernels fill a row's RowWork, a chunk of the row a block, before sample_kernel
 // goes on with what is left of it.  (One row of 128000 tokens: 75 us by one block, 42 of them the histogram.)
 static constexpr int kMaxChunks = 64;
+// The border step of the first filter.  What is gathered, and what is summed, goes by it, so it is settled once: two kernels need not round the same.
+struct Border {
+    double target;
+    u64 before;
+    int step, all;  // all: the tokens of all steps up to it are the candidates, not those of the step alone
+};
 struct RowWork {
     float largest[kMaxChunks];       // of every chunk
-    uint32_t n, pad[63];             // candidates
+    Border border;
+    uint32_t n, pad[57];             // candidates
     u64 histogram[kSteps];
     u64 candidate[kCandidates];
     u64 segment[kSegments];
@@ -591,19 +598,6 @@ __global__ __launch_bounds__(kThreads, 8) void sample_histogram_kernel(SamplePar
     }
 }
 
-// The border step of a row's first filter, as all its blocks find it: from the same whole numbers.
-__device__ __forceinline__ int border_of_work(const RowWork &work, const Plan &q, double &target, u64 &before, bool &all)
-{
-    u64 own[kEach];
-#pragma unroll
-    for (int i = 0; i < kEach; ++i) own[i] = work.histogram[threadIdx.x * kEach + i];
-    float upto;
-    target = q.by_count ? (double)q.top_k : q.top_p;
-    const int s = border_step(q.r, !q.by_count, own, target, before, upto);
-    all = few(!q.by_count, upto);
-    return s;
-}
-
 template <bool BF16>
 __global__ __launch_bounds__(kThreads, 8) void sample_gather_kernel(SampleParams p)
 {
@@ -613,10 +607,15 @@ __global__ __launch_bounds__(kThreads, 8) void sample_gather_kernel(SampleParams
     const Plan q = plan_of(p, b, largest_of_row(p, b));
     if (q.none || q.only_first || (!q.by_count && !q.by_mass)) return;
     if (tid < 32) sh.roots[tid] = kRoots[tid];
-    double target;
-    u64 before;
-    bool all;
-    const int s = border_of_work(work, q, target, before, all);
+    // every block of the row finds the same border, by the same instructions from the same whole numbers
+    u64 own[kEach], before;
+#pragma unroll
+    for (int i = 0; i < kEach; ++i) own[i] = work.histogram[tid * kEach + i];
+    float upto;
+    double target = q.by_count ? (double)q.top_k : q.top_p;
+    const int s = border_step(q.r, !q.by_count, own, target, before, upto);
+    const bool all = few(!q.by_count, upto);
+    if (c == 0 && tid == 0) work.border = {target, before, s, all};
     if (s == kSteps) return;
     const int n = gather<BF16>(row_of<BF16>(p, b), from, to, q, 0, s, !all, !all && !q.by_count, work.segment, sh.list);
     if (tid == 0) sh.digit = atomicAdd(&work.n, (uint32_t)n);
@@ -680,7 +679,11 @@ __global__ __launch_bounds__(kThreads) void sample_kernel(SampleParams p)
         } else {
             const bool done = SHARED_ROW && !(by_mass && q.by_count);  // the first filter: other blocks have gathered the candidates
             if (done) {
-                s = border_of_work(work_of(p, b), q, target, before, all);
+                const Border &border = work_of(p, b).border;
+                target = border.target;
+                before = border.before;
+                s = border.step;
+                all = border.all;
             } else {
                 fill_histogram<BF16>(row, 0, p.V, r, by_mass, cut);
                 u64 own[kEach];

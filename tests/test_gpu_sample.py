@@ -169,3 +169,17 @@ def test_infinite_logits_and_infinite_temperature(V):
     for t in (math.inf, 3e38, 1e30):
         for kw in ({}, dict(min_p=[0.5] * 4), dict(top_k=[30] * 4), dict(top_p=[0.6] * 4)):
             check(x, u, temperature=[t] * 4, **kw)
+
+
+@pytest.mark.parametrize("V", [20000, 40000])
+@pytest.mark.parametrize("top_p", [0.3, 0.99])
+def test_borders_around_what_is_sorted(V, top_p):
+    """Rows shared by several blocks, about as many likely tokens as are still sorted together (512), and as by count (3891): the blocks that gather
+    and the one that goes on agree about them."""
+    B = 24
+    rng = np.random.default_rng(V)
+    for least, step, kw in ((500, 1, dict(top_p=[top_p] * B)), (3860, 3, dict(top_k=[3700] * B, top_p=[top_p] * B))):
+        x = rng.random((B, V)) * 4 - 30
+        for b in range(B):
+            x[b, rng.choice(V, least + step * b, replace=False)] = 2.0 + rng.random(least + step * b) * 0.01
+        check(torch.from_numpy(x).float().to(DEV), rng.random(B).astype(np.float32), **kw)
