@@ -483,7 +483,8 @@ int moe_attn_forward(moe_attn_handle_t *h, const moe_kv_cache_t *cache, const vo
  *   temperature <= 0: the first of the order.
  * logprob [B] fp32 (may be NULL): the logarithm of the drawn token's share of the remaining w.  A row with nothing but
  * -infinity gives token -1 and logprob -infinity; where the largest logit is +infinity, w is 1 for those and 0 else.
- * w and all sums are held in 64 bits, and sums do not depend on the order in which they are formed.  1 <= V <= 2^19.
+ * w is computed in 64 bits and rounded to a multiple of 2^-f, f = min(50, 62 - ceil(log2 V)), so that sums are exact and
+ * do not depend on the order in which they are formed; a token with w below 2^-(f+1) is never drawn.  1 <= V <= 2^19.
  * Workspace: moe_sample_workspace_bytes(B, V). */
 #define MOE_SAMPLE_MAX_V (1 << 19)
 int64_t moe_sample_workspace_bytes(int32_t B, int32_t V);
