@@ -502,3 +502,27 @@ def test_windows_past_every_position_are_no_window(n, kv, causal, window):
     q, out, lse = b.attend(window=window, causal=causal)
     plain, plain_lse = b.att.moe_attn_forward(b.device_cache(), q, *b.args(), n, max(kv, 20), causal=causal)
     assert torch.equal(out, plain) and torch.equal(lse, plain_lse)
+
+
+@pytest.mark.parametrize("max_q", [40, 30])
+def test_append_to_more_sequences_than_a_wave_has_lanes(max_q):
+    """Ragged batches whose pages are counted: over 64 sequences at a time."""
+    rng = np.random.default_rng(8)
+    n = [int(x) for x in rng.choice([0, 0, 0, 1, 2, 5, 17], 150)]
+    n[140], n[70] = 40, 33
+    b = Batch(n, [x + int(y) for x, y in zip(n, rng.integers(0, 40, 150))], 2, 1, 64, 16, "f32", rot=16).fill()
+    (k, k64), (v, v64) = b.rows(1), b.rows(1)
+    dev = b.device_cache()
+    b.att.moe_kv_append(dev, None, k, v, torch.from_numpy(b.inv_freq).to(DEV), *b.args(), max_q)
+    od.append(b.cache, None, k64, v64, b.inv_freq, b.interleaved, b.offsets, b.kv, b.table, b.page, max_q)
+    for name in ("k", "v", "k_scale", "v_scale"):
+        assert np.array_equal(getattr(dev, name).cpu().numpy(), b.cache[name], equal_nan=name.endswith("scale")), name
+
+
+def test_decode_of_more_sequences_than_a_block_has_threads():
+    """Places of 600 sequences among the tiles, added up 256 at a time; some of them are long, some have no token or no key."""
+    rng = np.random.default_rng(9)
+    kv = [int(x) for x in rng.choice([0, 1, 15, 16, 40, 90], 600)]
+    kv[3], kv[300], kv[599] = 1500, 2500, 700
+    b = Batch([int(x) for x in rng.choice([0, 1, 1, 1], 600)], kv, 2, 1, 64, 16).fill()
+    b.attend(max_q=1, max_kv=9000)

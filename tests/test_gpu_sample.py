@@ -183,3 +183,55 @@ def test_borders_around_what_is_sorted(V, top_p):
         for b in range(B):
             x[b, rng.choice(V, least + step * b, replace=False)] = 2.0 + rng.random(least + step * b) * 0.01
         check(torch.from_numpy(x).float().to(DEV), rng.random(B).astype(np.float32), **kw)
+
+
+@pytest.mark.parametrize("V", [20000, 40001])
+def test_infinities_and_nan_of_rows_shared_by_blocks(V):
+    """As above, in vocabularies that several blocks share."""
+    inf = math.inf
+    x = torch.full((9, V), -inf, device=DEV)
+    x[1, V - 3] = -3.0
+    x[2] = math.nan
+    x[3, ::2], x[3, 1::2] = math.nan, 0.5
+    x[4, 8100:8300] = inf
+    x[5] = torch.finfo(torch.float32).min
+    x[6], x[6, V // 2] = torch.finfo(torch.float32).min, 0.0
+    x[7, 9000:9004] = torch.tensor([-0.0, 0.0, -0.0, 0.0], device=DEV)
+    x[8, 17000], x[8, 6] = inf, 1.0
+    u = np.full(9, 0.6)
+    for kw in ({}, dict(top_p=[0.5] * 9), dict(top_k=[3] * 9), dict(min_p=[0.2] * 9), dict(temperature=[0.0] * 9), dict(temperature=[1e-3] * 9),
+               dict(temperature=[1e3] * 9), dict(top_k=[2] * 9, top_p=[0.9] * 9, min_p=[0.1] * 9)):
+        check(x, u, **kw)
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_ties_and_flat_rows_shared_by_blocks(dtype):
+    """Borders among ties, in steps of more tokens than are sorted: by weight first, by count first, both."""
+    V, B = 20000, 6
+    x = torch.zeros((B, V), dtype=dtype, device=DEV)
+    x[1::3] = (torch.arange(V, device=DEV) % 2).to(dtype)
+    x[2::3] = (torch.arange(V, device=DEV) // 700 * 0.25).to(dtype)
+    u = np.linspace(0.0, 0.9999, B)
+    for kw in ({}, dict(top_k=[7] * B), dict(top_k=[6000] * B), dict(top_p=[0.37] * B), dict(top_p=[0.37] * B, top_k=[9100] * B), dict(top_p=[1e-6] * B),
+               dict(min_p=[0.4] * B)):
+        check(x, u, **kw)
+
+
+def test_spread_and_crowded_values_of_rows_shared_by_blocks():
+    rng = np.random.default_rng(6)
+    B, V = 4, 20000
+    x = rng.standard_normal((B, V)) * 300
+    x[2:] = 20 + rng.random((2, V)) * 1e-3
+    x = torch.from_numpy(x).float().to(DEV)
+    u = rng.random(B).astype(np.float32)
+    for kw in ({}, dict(top_k=[9000] * B), dict(top_p=[0.6] * B), dict(top_p=[0.999] * B, top_k=[18000] * B), dict(temperature=[50.0] * B, top_p=[0.8] * B)):
+        check(x, u, **kw)
+
+
+@pytest.mark.parametrize("V", [6500, 20000])
+def test_more_tokens_in_a_step_than_their_weight_says(V):
+    """A temperature below the normal range: 6000 tokens lie in the step of the largest logit and weigh nothing beside it, so the guess of how many there
+    are, which goes by weight, is far off."""
+    x = torch.full((3, V), -5.0, device=DEV)
+    x[:, :6000] = torch.arange(6000, device=DEV, dtype=torch.float64).mul(-1e-43).float().roll(11)
+    check(x, np.array([0.0, 0.5, 0.99]), temperature=[1e-45] * 3, top_p=[0.9] * 3)
