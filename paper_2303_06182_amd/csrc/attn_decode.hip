@@ -220,9 +220,10 @@ __global__ __launch_bounds__(64 * W, M) void attn_decode_kernel(AttnParams p)
             run = min(each, count - tile0);
             if (run <= 0) break;
         } else {
-            const int local = (int)(t - begin[bu]);
-            unit = local / count;
-            tile0 = local - unit * count;
+            // a sequence's tiles of all its units may pass 32 bits; a division of 64 is left for those
+            const int64_t local = t - begin[bu];
+            unit = local <= 0x7fffffff ? (int)local / count : (int)(local / count);
+            tile0 = (int)(local - (int64_t)unit * count);
             run = (int)min(w_end - t, (int64_t)(count - tile0));
         }
         unit = __builtin_amdgcn_readfirstlane(unit);

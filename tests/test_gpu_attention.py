@@ -526,3 +526,15 @@ def test_decode_of_more_sequences_than_a_block_has_threads():
     kv[3], kv[300], kv[599] = 1500, 2500, 700
     b = Batch([int(x) for x in rng.choice([0, 1, 1, 1], 600)], kv, 2, 1, 64, 16).fill()
     b.attend(max_q=1, max_kv=9000)
+
+
+def test_more_tiles_than_32_bits_count():
+    """A table of nearly 2^30 positions, of which all but the first and the last page are missing, times 33 heads and four tiles of rows."""
+    b = Batch([64], [256], 33, 33, 64, 128).fill()
+    slots = (1 << 23) - 1
+    far = binding.PagedAttention(1, 64, 33, 33, 64, 128, b.pages, slots, "bf16")
+    table = torch.full((1, slots), -1, dtype=torch.int32, device=DEV)
+    table[0, 0], table[0, -1] = b.table[0][0], b.table[0][1]
+    q, q64 = b.rows(33, 1.5)
+    out, lse = far.moe_attn_forward(b.device_cache(), q, ints([0, 64]), ints([128 * slots]), table, 64, 128 * slots, causal=False)
+    b.check(out, lse, od.attend(b.cache, q64, b.offsets, b.kv, b.table, b.page, np.float32(0.125), causal=False))
