@@ -123,21 +123,22 @@ __global__ __launch_bounds__(64 * W, NS == 1 && DH <= 128 ? 2 : 1) void attn_pre
     any_begin = __builtin_amdgcn_readfirstlane(any_begin);
     any_end = __builtin_amdgcn_readfirstlane(any_end);
 
-    // queries; a negative scale is theirs, so that the factor in front of the exponent is positive
-    const bool negative = p.scale_log2e < 0.f;
-    const float scale = fmaxf(fabsf(p.scale_log2e), 1e-30f);  // not zero: times a masked score's infinity that is none
+    // queries; a negative scale and one of zero are theirs, so that the factor in front of the exponent is positive (times a masked score's infinity
+    // zero is no number)
+    const bool negative = p.scale_log2e < 0.f, asks = live && p.scale_log2e != 0.f;
+    const float scale = p.scale_log2e != 0.f ? fabsf(p.scale_log2e) : 1.f;
     Pieces<NS> q[kSteps];
 #pragma unroll
     for (int s = 0; s < kSteps; ++s) {
         const int64_t at = (int64_t)(sq.first + tok) * p.q_stride + (int64_t)head * DH + 16 * s + 8 * half;
         if (NS == 1) {
             uint4 x = make_uint4(0, 0, 0, 0);
-            if (live) x = *reinterpret_cast<const uint4 *>(static_cast<const uint16_t *>(p.q) + at);
+            if (asks) x = *reinterpret_cast<const uint4 *>(static_cast<const uint16_t *>(p.q) + at);
             if (negative) x = make_uint4(x.x ^ 0x80008000u, x.y ^ 0x80008000u, x.z ^ 0x80008000u, x.w ^ 0x80008000u);
             q[s].x[0] = __builtin_bit_cast(bf16x8, x);
         } else {
             float x[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-            if (live) {
+            if (asks) {
                 const float4 lo = *reinterpret_cast<const float4 *>(static_cast<const float *>(p.q) + at);
                 const float4 hi = *reinterpret_cast<const float4 *>(static_cast<const float *>(p.q) + at + 4);
                 x[0] = lo.x, x[1] = lo.y, x[2] = lo.z, x[3] = lo.w, x[4] = hi.x, x[5] = hi.y, x[6] = hi.z, x[7] = hi.w;

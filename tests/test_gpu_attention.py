@@ -538,3 +538,14 @@ def test_more_tiles_than_32_bits_count():
     q, q64 = b.rows(33, 1.5)
     out, lse = far.moe_attn_forward(b.device_cache(), q, ints([0, 64]), ints([128 * slots]), table, 64, 128 * slots, causal=False)
     b.check(out, lse, od.attend(b.cache, q64, b.offsets, b.kv, b.table, b.page, np.float32(0.125), causal=False))
+
+
+@pytest.mark.parametrize("n", [1, 100])
+@pytest.mark.parametrize("scale", [0.0, 1e-35, -1e-36, 1e-40])
+def test_tiny_scales_over_large_products(n, scale):
+    """q . key of about 1e34, which no scale but a tiny one fits: the scale is taken as it is."""
+    b = Batch([n, 2], [n + 150, 70], 4, 2, 64, 16, "f32").fill()
+    b.cache["k_scale"][:] *= np.float32(2.0 ** 46)
+    q, q64 = b.rows(4, 1e18)
+    out, lse = b.att.moe_attn_forward(b.device_cache(), q, *b.args(), max(b.n), n + 150, scale=scale)
+    b.check(out, lse, od.attend(b.cache, q64, b.offsets, b.kv, b.table, b.page, np.float32(scale)))
