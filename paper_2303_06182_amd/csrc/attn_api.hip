@@ -213,8 +213,9 @@ int moe_attn_forward(moe_attn_handle_t *h, const moe_kv_cache_t *cache, const vo
     AttnParams p;
     const int rc = check_batch(h, cache, q_offsets, kv_len, page_table, B, T, max_q, max_kv, p);
     if (rc != MOE_OK) return rc;
-    if ((causal != 0 && causal != 1) || window < 0 || !(scale - scale == 0.f)) {
-        set_error("causal = %d (0 or 1), window = %d (0 or more), scale = %g (finite)", causal, window, (double)scale);
+    const float scale_log2e = scale * 1.44269504088896340736f;
+    if ((causal != 0 && causal != 1) || window < 0 || !(scale_log2e - scale_log2e == 0.f)) {
+        set_error("causal = %d (0 or 1), window = %d (0 or more), scale = %g (finite, and times log2(e))", causal, window, (double)scale);
         return MOE_ERR_INVALID_ARG;
     }
     if (p.B == 0) return MOE_OK;
@@ -228,7 +229,7 @@ int moe_attn_forward(moe_attn_handle_t *h, const moe_kv_cache_t *cache, const vo
     }
     p.q = q;
     p.q_stride = q_stride;
-    p.scale_log2e = scale * 1.44269504088896340736f;
+    p.scale_log2e = scale_log2e;
     p.causal = causal;
     p.window = window < 1 << 30 ? window : 1 << 30;  // positions lie in (-2^24, 2^30): a difference of one and a window stays in 32 bits
     p.out = out;

@@ -549,3 +549,11 @@ def test_tiny_scales_over_large_products(n, scale):
     q, q64 = b.rows(4, 1e18)
     out, lse = b.att.moe_attn_forward(b.device_cache(), q, *b.args(), max(b.n), n + 150, scale=scale)
     b.check(out, lse, od.attend(b.cache, q64, b.offsets, b.kv, b.table, b.page, np.float32(scale)))
+
+
+@pytest.mark.parametrize("scale", [3e38, -3e38, math.nan])
+def test_scales_that_pass_fp32_are_refused(scale):
+    b = Batch([1, 1], [20, 30], 4, 2, 64, 16).fill()
+    with pytest.raises(binding.MoeError) as e:
+        b.att.moe_attn_forward(b.device_cache(), b.rows(4)[0], *b.args(), 1, 30, scale=scale)
+    assert e.value.code == binding.MOE_ERR_INVALID_ARG
