@@ -214,9 +214,16 @@ def _addr(t: Optional[torch.Tensor]) -> Optional[int]:
     return t.data_ptr()
 
 
-def _stream_on(device: torch.device) -> int:
-    """The current stream of a device (index 0 where it has none), without making a stream object."""
-    return torch._C._cuda_getCurrentRawStream(device.index or 0)
+def _stream_on(index: int) -> int:
+    """The current stream of a device, without making a stream object."""
+    return torch._C._cuda_getCurrentRawStream(index)
+
+
+def _output(t: torch.Tensor, shape: tuple, dtype: torch.dtype, index: int, name: str) -> torch.Tensor:
+    """An output that the caller has allocated, as it has to be."""
+    if tuple(t.shape) != shape or t.dtype != dtype or t.get_device() != index or not t.is_contiguous():
+        raise ValueError("%s must be %s of %s, contiguous, on cuda:%d" % (name, list(shape), dtype, index))
+    return t
 
 
 def moe_capacity(T: int, E: int, k: int, cf: float, convention: int = MOE_CAPACITY_SHARE) -> int:
@@ -566,6 +573,9 @@ class KvCache:
             raise ValueError("k and v must have the same shape, the scales their first two dimensions")
         if k_scale.dtype != torch.float32 or v_scale.dtype != torch.float32:
             raise ValueError("scales must be float32")
+        self.index = k.get_device()
+        if any(t.get_device() != self.index for t in (v, k_scale, v_scale)):
+            raise ValueError("k, v and their scales must be on one device")
         self.k, self.v, self.k_scale, self.v_scale = k, v, k_scale, v_scale
         self.shape = tuple(k.shape)
         self.struct = MoeKvCache(_ptr(k), _ptr(v), _ptr(k_scale), _ptr(v_scale))
@@ -581,8 +591,12 @@ class PagedAttention:
         self.lib = load_library()
         self.cfg = MoeAttnConfig(B_max, T_max, n_heads, n_kv_heads, head_dim, page_size, num_pages, max_pages,
                                  MOE_DTYPE_BF16 if dtype == "bf16" else MOE_DTYPE_F32, rot_dim, int(interleaved))
+        self.cache_shape = (num_pages, n_kv_heads, page_size, head_dim)
         self.torch_dtype = torch.bfloat16 if dtype == "bf16" else torch.float32
         self.device = torch.device(device)
+        if self.device.index is None:
+            self.device = torch.device("cuda", torch.cuda.current_device())
+        self.index = self.device.index
         h = ctypes.c_void_p()
         with torch.cuda.device(self.device):
             _check(self.lib.moe_attn_create(ctypes.byref(self.cfg), ctypes.byref(h)))
@@ -598,8 +612,7 @@ class PagedAttention:
             pass
 
     def new_cache(self) -> KvCache:
-        c = self.cfg
-        shape = (c.num_pages, c.n_kv_heads, c.page_size, c.head_dim)
+        shape = self.cache_shape
         k, v = (torch.empty(shape, dtype=torch.uint8, device=self.device).view(torch.float8_e4m3fn) for _ in range(2))
         ks, vs = (torch.empty(shape[:2], dtype=torch.float32, device=self.device) for _ in range(2))
         return KvCache(k, v, ks, vs)
@@ -613,17 +626,21 @@ class PagedAttention:
             raise ValueError("%s must be [T, %d, %d] of %s" % (name, heads, dim, self.torch_dtype))
         if shape[0] and (strides[2] != 1 or (heads > 1 and strides[1] != dim)):
             raise ValueError("%s: the heads of a token must lie together" % name)
+        if t.get_device() != self.index:
+            raise ValueError("%s must be on %s" % (name, self.device))
         return t.data_ptr(), strides[0] if shape[0] > 1 else heads * dim
 
     def _batch(self, cache: KvCache, q_offsets, kv_len, page_table):
-        c = self.cfg
-        if cache.shape != (c.num_pages, c.n_kv_heads, c.page_size, c.head_dim):
+        if cache.shape != self.cache_shape:
             raise ValueError("the cache has shape %s, the handle another geometry" % (cache.shape,))
         B = kv_len.shape[0]
-        if q_offsets.shape[0] != B + 1 or page_table.shape != (B, c.max_pages):
+        if q_offsets.shape[0] != B + 1 or page_table.shape != (B, self.cfg.max_pages):
             raise ValueError("q_offsets must be [B + 1], kv_len [B] and page_table [B, max_pages]")
         if q_offsets.dtype != torch.int32 or kv_len.dtype != torch.int32 or page_table.dtype != torch.int32:
             raise ValueError("q_offsets, kv_len and page_table must be int32")
+        i = self.index
+        if q_offsets.get_device() != i or kv_len.get_device() != i or page_table.get_device() != i or cache.index != i:
+            raise ValueError("the cache, q_offsets, kv_len and page_table must be on %s" % self.device)
         return B
 
     def moe_kv_append(self, cache: KvCache, q, k, v, inv_freq, q_offsets, kv_len, page_table, max_q: int, q_out=None):
@@ -633,11 +650,15 @@ class PagedAttention:
             raise ValueError("q, k and v must have the same number of tokens")
         if inv_freq is not None and (inv_freq.dtype != torch.float64 or inv_freq.numel() != c.rot_dim // 2):
             raise ValueError("inv_freq must be [rot_dim / 2] float64")
-        if q is not None and q_out is None:
+        if inv_freq is not None and inv_freq.get_device() != self.index:
+            raise ValueError("inv_freq must be on %s" % self.device)
+        if q_out is not None:
+            _output(q_out, (T, c.n_heads, c.head_dim), self.torch_dtype, self.index, "q_out")
+        elif q is not None:
             q_out = torch.empty((T, c.n_heads, c.head_dim), dtype=self.torch_dtype, device=self.device)
         (qp, qs), (kp, ks), (vp, vs) = self._rows(q, c.n_heads, "q"), self._rows(k, c.n_kv_heads, "k"), self._rows(v, c.n_kv_heads, "v")
         _check(self.lib.moe_kv_append(self.h, cache.ref, qp, qs, kp, ks, vp, vs, _addr(inv_freq), _addr(q_offsets), _addr(kv_len),
-                                      _addr(page_table), B, T, max_q, _addr(q_out), _stream_on(self.device)))
+                                      _addr(page_table), B, T, max_q, _addr(q_out), _stream_on(self.index)))
         return q_out
 
     def moe_attn_forward(self, cache: KvCache, q, q_offsets, kv_len, page_table, max_q: int, max_kv: int, scale: Optional[float] = None,
@@ -646,12 +667,16 @@ class PagedAttention:
         B, T, c = self._batch(cache, q_offsets, kv_len, page_table), q.shape[0], self.cfg
         if out is None:
             out = torch.empty((T, c.n_heads, c.head_dim), dtype=self.torch_dtype, device=self.device)
-        if lse is None and want_lse:
+        else:
+            _output(out, (T, c.n_heads, c.head_dim), self.torch_dtype, self.index, "out")
+        if lse is not None:
+            _output(lse, (T, c.n_heads), torch.float32, self.index, "lse")
+        elif want_lse:
             lse = torch.empty((T, c.n_heads), dtype=torch.float32, device=self.device)
         qp, qs = self._rows(q, c.n_heads, "q")
         _check(self.lib.moe_attn_forward(self.h, cache.ref, qp, qs, _addr(q_offsets), _addr(kv_len), _addr(page_table), B, T, max_q,
                                          max_kv, c.head_dim ** -0.5 if scale is None else scale, int(causal), window, _addr(out), _addr(lse),
-                                         self.workspace.data_ptr(), self.workspace.numel(), _stream_on(self.device)))
+                                         self.workspace.data_ptr(), self.workspace.numel(), _stream_on(self.index)))
         return out, lse
 
 
@@ -669,15 +694,20 @@ def moe_sample(logits, u, temperature=None, top_k=None, top_p=None, min_p=None, 
     if logits.dim() != 2 or logits.dtype not in (torch.float32, torch.bfloat16) or (logits.shape[1] > 1 and logits.stride(1) != 1):
         raise ValueError("logits must be [B, V] of float32 or bfloat16 with dense rows")
     B, V = logits.shape
+    index = logits.get_device()
+    if index < 0 or index != torch.cuda.current_device():
+        raise ValueError("logits are on %s, which is not the current GPU" % logits.device)
     for t, dtype in ((u, torch.float32), (temperature, torch.float32), (top_k, torch.int32), (top_p, torch.float32), (min_p, torch.float32)):
-        if t is not None and (t.dtype != dtype or t.numel() != B):
-            raise ValueError("u, temperature, top_p and min_p must be [B] float32, top_k [B] int32")
+        if t is not None and (t.dtype != dtype or t.numel() != B or t.get_device() != index):
+            raise ValueError("u, temperature, top_p and min_p must be [B] float32, top_k [B] int32, on %s" % logits.device)
     new = lambda dtype: torch.empty((B,), dtype=dtype, device=logits.device)  # noqa: E731
-    token = new(torch.int32) if token is None else token
-    logprob = new(torch.float32) if logprob is None else logprob
+    token = new(torch.int32) if token is None else _output(token, (B,), torch.int32, index, "token")
+    logprob = new(torch.float32) if logprob is None else _output(logprob, (B,), torch.float32, index, "logprob")
     if workspace is None:
         workspace = torch.empty(moe_sample_workspace_bytes(B, V), dtype=torch.uint8, device=logits.device)
+    elif workspace.dtype != torch.uint8 or workspace.get_device() != index:
+        raise ValueError("workspace must be uint8 on %s" % logits.device)
     _check(lib.moe_sample(logits.data_ptr(), MOE_DTYPE_BF16 if logits.dtype == torch.bfloat16 else MOE_DTYPE_F32,
                           logits.stride(0) if B > 1 else V, B, V, _addr(u), _addr(temperature), _addr(top_k), _addr(top_p), _addr(min_p), _addr(token),
-                          _addr(logprob), _addr(workspace), workspace.numel(), _stream_on(logits.device)))
+                          _addr(logprob), _addr(workspace), workspace.numel(), _stream_on(index)))
     return token, logprob

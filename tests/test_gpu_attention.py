@@ -557,3 +557,26 @@ def test_scales_that_pass_fp32_are_refused(scale):
     with pytest.raises(binding.MoeError) as e:
         b.att.moe_attn_forward(b.device_cache(), b.rows(4)[0], *b.args(), 1, 30, scale=scale)
     assert e.value.code == binding.MOE_ERR_INVALID_ARG
+
+
+def test_outputs_that_do_not_fit_are_refused():
+    """Other shapes, types, layouts and memory than the call writes."""
+    b = Batch([1, 2], [20, 30], 4, 2, 64, 16, rot=64).fill()
+    cache, (q, _), (k, _), (v, _) = b.device_cache(), b.rows(4), b.rows(2), b.rows(2)
+    f, batch = torch.from_numpy(b.inv_freq).to(DEV), b.args()
+    for bad in (q[:2], q[:, :2], q.float(), torch.empty_like(q, device="cpu"), torch.empty((3, 64, 4), dtype=torch.bfloat16, device=DEV).transpose(1, 2)):
+        for call in (lambda: b.att.moe_kv_append(cache, q, k, v, f, *batch, 2, q_out=bad), lambda: b.att.moe_attn_forward(cache, q, *batch, 2, 30, out=bad)):
+            with pytest.raises(ValueError):
+                call()
+    for bad in (torch.empty((3, 2), device=DEV), torch.empty((3, 4), dtype=torch.float64, device=DEV), torch.empty((3, 4))):
+        with pytest.raises(ValueError):
+            b.att.moe_attn_forward(cache, q, *batch, 2, 30, lse=bad)
+    for i in range(3):
+        with pytest.raises(ValueError):
+            b.att.moe_attn_forward(cache, q, *[x.cpu() if j == i else x for j, x in enumerate(batch)], 2, 30)
+    for args in ((q.cpu(), k, v, f), (q, k.cpu(), v, f), (q, k, v.cpu(), f), (q, k, v, f.cpu())):
+        with pytest.raises(ValueError):
+            b.att.moe_kv_append(cache, *args, *batch, 2)
+    with pytest.raises(ValueError):
+        binding.KvCache(cache.k, cache.v.cpu(), cache.k_scale, cache.v_scale)
+    b.attend(max_q=2)                                                        # and the handle is as it was

@@ -235,3 +235,18 @@ def test_more_tokens_in_a_step_than_their_weight_says(V):
     x = torch.full((3, V), -5.0, device=DEV)
     x[:, :6000] = torch.arange(6000, device=DEV, dtype=torch.float64).mul(-1e-43).float().roll(11)
     check(x, np.array([0.0, 0.5, 0.99]), temperature=[1e-45] * 3, top_p=[0.9] * 3)
+
+
+def test_outputs_and_settings_that_do_not_fit_are_refused():
+    x, rng = logits_of(3, 40, torch.float32, 0)
+    u = f32(rng.random(3))
+    for kw in (dict(token=torch.empty(3, dtype=torch.int64, device=DEV)), dict(token=torch.empty(2, dtype=torch.int32, device=DEV)),
+               dict(token=torch.empty(3, dtype=torch.int32)), dict(logprob=torch.empty(4, device=DEV)), dict(logprob=torch.empty(3, dtype=torch.float64, device=DEV)),
+               dict(workspace=torch.empty(4096, dtype=torch.uint8)), dict(workspace=torch.empty(4096, device=DEV)), dict(top_p=torch.ones(3))):
+        with pytest.raises(ValueError):
+            binding.moe_sample(x, u, **kw)
+    with pytest.raises(ValueError):
+        binding.moe_sample(x, u.cpu())
+    with pytest.raises(ValueError):
+        binding.moe_sample(x.cpu(), u.cpu())
+    check(x, u.cpu().numpy())
