@@ -425,7 +425,8 @@ typedef struct moe_attn_config {
 typedef struct moe_attn_handle moe_attn_handle_t; /* opaque: the config plus device properties */
 
 /* As moe_create / moe_destroy / moe_workspace_bytes.  One handle and one workspace serve every layer of the same
- * geometry.  Only moe_attn_forward takes the workspace. */
+ * geometry, on the device that was current when it was made, which has to be current in every call.  Only
+ * moe_attn_forward takes the workspace. */
 int moe_attn_create(const moe_attn_config_t *cfg, moe_attn_handle_t **out);
 int moe_attn_destroy(moe_attn_handle_t *h);
 int64_t moe_attn_workspace_bytes(const moe_attn_handle_t *h);

@@ -84,6 +84,12 @@ int check_batch(const moe_attn_handle_t *h, const moe_kv_cache_t *cache, const i
     }
     p = AttnParams{};
     if (B == 0 || T == 0 || max_q == 0) return MOE_OK;
+    int dev = -1;
+    MOE_HIP_CHECK(hipGetDevice(&dev));
+    if (dev != h->device) {
+        set_error("current device %d is not the handle's device %d", dev, h->device);
+        return MOE_ERR_INVALID_ARG;
+    }
     if (!cache) {
         set_error("cache is NULL");
         return MOE_ERR_INVALID_ARG;

@@ -11,6 +11,7 @@ sum_d |q_d key_pd|, half a step of bf16 2^-8 and of fp32 2^-24 relative to the v
 lse: ds + (kv + 16) 2^-24 + 4 * 2^-24 |lse|.  Appending: bytes and scales are equal; queries are off by one rounding of the value
 (bf16: after one to fp32) and 1e-11 of the pair's size for the angle.
 """
+import ctypes
 import math
 
 import numpy as np
@@ -580,3 +581,18 @@ def test_outputs_that_do_not_fit_are_refused():
     with pytest.raises(ValueError):
         binding.KvCache(cache.k, cache.v.cpu(), cache.k_scale, cache.v_scale)
     b.attend(max_q=2)                                                        # and the handle is as it was
+
+
+def test_another_device_than_the_handles_is_refused():
+    """The handle's note of its device, which follows its configuration, says another one than the current."""
+    b = Batch([1, 2], [20, 30], 4, 2, 64, 16).fill()
+    cache, (q, _), (k, _), (v, _), batch = b.device_cache(), b.rows(4), b.rows(2), b.rows(2), b.args()
+    device = ctypes.c_int.from_address(b.att.h.value + ctypes.sizeof(binding.MoeAttnConfig))
+    assert device.value == torch.cuda.current_device()
+    device.value += 1
+    for call in (lambda: b.att.moe_kv_append(cache, q, k, v, None, *batch, 2), lambda: b.att.moe_attn_forward(cache, q, *batch, 2, 30)):
+        with pytest.raises(binding.MoeError, match="device") as e:
+            call()
+        assert e.value.code == binding.MOE_ERR_INVALID_ARG
+    device.value -= 1
+    b.attend(max_q=2)
