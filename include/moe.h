@@ -464,9 +464,10 @@ int moe_kv_append(moe_attn_handle_t *h, const moe_kv_cache_t *cache, const void 
  * for batches of all of them:
  *   out[t, h] = sum_p softmax_p(scale * q[t, h] . key[p]) value[p]
  * over the positions p < kv_len[b] with p <= pos(t) if causal, and pos(t) - p < window if window > 0.  Scores, softmax
- * and sums in fp32 (bf16: the weights are rounded to bf16 for the product with the values).  lse [T, n_heads] fp32, NULL or
- * the natural logarithm of the softmax's denominator, which lets outputs over parts of a sequence be joined.  A query
- * that sees nothing gets zeros, and -infinity.  Cache bytes of rows that nothing was written to may hold anything.
+ * and sums in fp32 (bf16: the weights, relative to a row's largest, are rounded to bf16 for the product with the values;
+ * fp32: not).  lse [T, n_heads] fp32, NULL or the natural logarithm of the softmax's denominator, which lets outputs over
+ * parts of a sequence be joined.  A query that sees nothing gets zeros, and -infinity.  Cache bytes of rows that nothing
+ * was written to may hold anything.
  * Needs the workspace. */
 int moe_attn_forward(moe_attn_handle_t *h, const moe_kv_cache_t *cache, const void *q, int64_t q_stride,
                      const int32_t *q_offsets, const int32_t *kv_len, const int32_t *page_table, int32_t B, int32_t T,

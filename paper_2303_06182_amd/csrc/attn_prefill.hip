@@ -9,8 +9,13 @@
 // The maximum, the sum and the rescaling of a query are its lane's own; two lanes share a query.  The scales are powers of two, which the
 // conversion to bf16 multiplies by for nothing, and no later step knows of them.  (In the exponent instead, a key's as part of its factor and
 // a value's as its offset, they cost instructions per 16 keys, and the scale of a page of zeros, 2^-126, takes its weights out of fp32.)
-// Products below 2^-126 may be lost: what they weigh is less than that, too.  The output is rescaled only where the maximum has grown by more
-// than 8 (a factor of 256 on the weights, which fp32 and bf16 both hold), for most tiles not at all.
+// Products below 2^-126 may be lost: what they weigh is less than that, too.
+//
+// With bf16 queries a weight is rounded once to bf16 for the second product, 2^-9 of it; the sum has it unrounded.  The weights are relative to the row's
+// largest so far, so that the largest is 1 and rounds to itself: where a key or two take nearly all of a row, as they do, little else is left to round.
+// (A maximum that may be behind by a factor of 256 rescales the output less often, but rounds the largest weight like the rest: 8192 tokens 298 us and an
+// error of 2.2e-3 of the outputs, with this 303 and 1.8e-3; fp32 weights rounded to bf16 at the output alone 1.6e-3.  Weights as two bf16 numbers: 390.
+// fp32 queries have three pieces of everything, and none of this.)
 //
 // Bound by the matrix cores and the exponentials (a quarter of the rate of other instructions) in about equal parts: per 32 x 64 weights
 // and wave 32 MFMAs of 32 cycles, 32 exponentials of 16 and some 110 others of 4.  Two waves a SIMD overlap them.  Measured: 8192 tokens, 16
@@ -320,7 +325,7 @@ __global__ __launch_bounds__(64 * W, NS == 1 && DH <= 128 ? 2 : 1) void attn_pre
 #pragma unroll
                 for (int i = 0; i < 16; ++i) top = fmaxf(top, s[n][i]);
             top = fmaxf(top, __shfl_xor(top, 32, 64)) * scale;
-            if (__any(top > m + 8.f)) {  // m is -infinity until a row has seen a key
+            if (__any(top > m)) {  // m is -infinity until a row has seen a key
                 const float m_new = fmaxf(m, top);
                 const float alpha = m_new == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m - m_new);
                 m = m_new;

@@ -596,3 +596,27 @@ def test_another_device_than_the_handles_is_refused():
         assert e.value.code == binding.MOE_ERR_INVALID_ARG
     device.value -= 1
     b.attend(max_q=2)
+
+
+@pytest.mark.parametrize("n", [30, 200, 600])
+def test_bf16_weights_add_only_what_the_smaller_ones_round_to(n):
+    """With bf16 queries a weight is rounded to bf16, relative to the largest of its row, which is 1 and loses nothing.  Against the exact result, rounding
+    the output is off by a half step of either sign, and the weights p_i but the largest by as much of p_i |value|, each independently; values of
+    either sign make out^2 about sum p_i^2 value^2.  So the mean square error is 1 + sum' p_i^2 / sum p_i^2 times that of the output's rounding alone (sum':
+    without the largest); a tenth more for the draw.  Scores spread so that a few keys take nearly all of a row, not all in its first tile."""
+    kv, dim = 1000, 64
+    b = Batch([n], [kv], 2, 1, dim, 32, seed=n).fill()
+    q, q64 = b.rows(2, 1.0)
+    deq = lambda x: np.concatenate([od.VALUES[b.cache[x][p, 0]] * float(b.cache[x + "_scale"][p, 0]) for p in b.table[0]])[:kv]  # noqa: E731
+    key, value = deq("k"), deq("v")
+    s = np.einsum("thd,kd->thk", q64, key)
+    scale = float(np.float32(2.0 * math.log(2.0) / s.std()))
+    out, _ = b.att.moe_attn_forward(b.device_cache(), q, *b.args(), n, kv, scale=scale, causal=False)
+    p = np.exp(scale * (s - s.max(-1, keepdims=True)))
+    p /= p.sum(-1, keepdims=True)
+    want = p @ value
+    rounded = torch.from_numpy(want).to(torch.bfloat16).double().numpy()
+    alone = ((rounded - want) ** 2).sum()
+    more = 1.0 - (p.max(-1) ** 2).sum() / (p ** 2).sum()
+    assert more < 0.4                                                       # or the test would not tell
+    assert ((out.double().cpu().numpy() - want) ** 2).sum() <= 1.1 * (1.0 + more) * alone
