@@ -93,8 +93,10 @@ __global__ __launch_bounds__(64 * W, NS == 1 && DH <= 128 ? 2 : 1) void attn_pre
     const int l31 = lane & 31, half = lane >> 5;
 
     const int per_tile = p.B * p.n_kv_heads * pp.splits;
-    const int rt = pp.row_tiles - 1 - (int)blockIdx.x / per_tile;
-    const int rest = (int)blockIdx.x % per_tile;
+    const int index = (int)(blockIdx.y * gridDim.x + blockIdx.x);
+    const int rt = pp.row_tiles - 1 - index / per_tile;
+    if (rt < 0) return;  // the last row of the grid may have too many
+    const int rest = index % per_tile;
     const int part = rest % pp.splits, h = rest / pp.splits % p.n_kv_heads, b = rest / pp.splits / p.n_kv_heads;
     const Seq sq = load_seq(p, b);
     if (sq.n * p.group <= p.few_rows || rt * kRows >= sq.n * p.group) return;
@@ -459,11 +461,13 @@ int launch_as(PrefillParams pp, int num_cus, hipStream_t s)
     const int64_t units = (int64_t)pp.row_tiles * p.B * p.n_kv_heads;
     const int64_t filled = ((int64_t)p.T * p.group / (32 * W) + p.B) * p.n_kv_heads;
     pp.splits = splits_for(units, filled < units ? filled : units, ceil_div(p.max_kv, kTile), num_cus);
-    if (units * pp.splits >= 1ll << 31) {
-        set_error("moe_attn_forward: %lld blocks", (long long)units);
+    // rows of the grid of 2^22 blocks: a launch of 2^32 threads in one dimension starts fewer and says nothing
+    const int64_t blocks = units * pp.splits, row = 1 << 22;
+    if (blocks >= (1ll << 31) - row) {
+        set_error("moe_attn_forward: %lld blocks", (long long)blocks);
         return MOE_ERR_INVALID_ARG;
     }
-    hipLaunchKernelGGL((attn_prefill_kernel<DH, NS, W>), dim3((unsigned)(units * pp.splits)), dim3(64 * W), kLds, s, pp);
+    hipLaunchKernelGGL((attn_prefill_kernel<DH, NS, W>), dim3((unsigned)(blocks < row ? blocks : row), (unsigned)((blocks + row - 1) / row)), dim3(64 * W), kLds, s, pp);
     MOE_LAUNCH_CHECK("attn_prefill_kernel");
     if (pp.splits > 1) {
         hipLaunchKernelGGL((attn_prefill_join_kernel<DH, NS, W>), dim3((unsigned)(units * 2 * W)), dim3(256), 0, s, pp);

@@ -620,3 +620,29 @@ def test_bf16_weights_add_only_what_the_smaller_ones_round_to(n):
     more = 1.0 - (p.max(-1) ** 2).sum() / (p ** 2).sum()
     assert more < 0.4                                                       # or the test would not tell
     assert ((out.double().cpu().numpy() - want) ** 2).sum() <= 1.1 * (1.0 + more) * alone
+
+
+def test_many_ragged_sequences_with_a_long_one():
+    """More blocks than 2^32 threads make: 2048 sequences, of which one has 17025 new tokens and the others one, by 64 heads."""
+    B, long, heads = 2048, 17025, 64
+    n = [1] * B
+    n[1000] = long
+    T, pages = sum(n), -(-long // 128) + B - 1
+    att = binding.PagedAttention(B, T, heads, heads, 64, 128, pages, -(-long // 128))
+    gen = torch.Generator(device=DEV).manual_seed(3)
+    cache = att.new_cache()
+    for name in "kv":
+        getattr(cache, name).copy_(torch.empty(cache.shape, dtype=torch.bfloat16, device=DEV).normal_(0, 60, generator=gen).clamp_(-448, 448).to(torch.float8_e4m3fn))
+        getattr(cache, name + "_scale").fill_(2.0 ** -6)
+    table = torch.full((B, att.cfg.max_pages), -1, dtype=torch.int32, device=DEV)
+    table[:, 0] = torch.arange(B, device=DEV)
+    table[1000, 1:] = torch.arange(B, pages, device=DEV)
+    q = torch.empty((T, heads, 64), dtype=torch.bfloat16, device=DEV).normal_(0, 1, generator=gen)
+    offsets = torch.tensor([0] + n).cumsum(0).int().to(DEV)
+    out, lse = att.moe_attn_forward(cache, q, offsets, ints(n), table, long, long)
+    one = binding.PagedAttention(1, long, heads, heads, 64, 128, pages, att.cfg.max_pages)
+    want, want_lse = one.moe_attn_forward(cache, q[1000:1000 + long].contiguous(), ints([0, long]), ints([long]), table[1000:1001].contiguous(), long, long)
+    assert torch.equal(out[1000:1000 + long], want) and torch.equal(lse[1000:1000 + long], want_lse)
+    others = torch.cat((torch.arange(1000), torch.arange(1000 + long, T))).to(DEV)
+    v = cache.v[torch.cat((torch.arange(1000), torch.arange(1001, B))).to(DEV), :, 0].float() * 2.0 ** -6                  # their only key has all weight
+    assert torch.equal(out[others].float(), v)
