@@ -629,7 +629,9 @@ template <bool BF16, bool SHARED_ROW>
 __global__ __launch_bounds__(kThreads) void sample_kernel(SampleParams p)
 {
     Shared &sh = shared();
-    const int b = blockIdx.x, tid = threadIdx.x, lane = tid & 63;
+    const int64_t index = (int64_t)blockIdx.y * gridDim.x + blockIdx.x;
+    if (index >= p.B) return;
+    const int b = (int)index, tid = threadIdx.x, lane = tid & 63;
     const char *row = row_of<BF16>(p, b);
     if (tid < 32) sh.roots[tid] = kRoots[tid];
     if (tid == 0) sh.token = 0x7fffffff;
@@ -840,8 +842,11 @@ int launch_as(const SampleParams &p, hipStream_t s)
         hipLaunchKernelGGL(sample_gather_kernel<BF16>, grid, dim3(kThreads), kListLds, s, p);
         MOE_LAUNCH_CHECK("sample_gather_kernel");
     }
-    if (p.chunks > 1) hipLaunchKernelGGL((sample_kernel<BF16, true>), dim3(p.B), dim3(kThreads), sizeof(Shared), s, p);
-    else hipLaunchKernelGGL((sample_kernel<BF16, false>), dim3(p.B), dim3(kThreads), sizeof(Shared), s, p);
+    // rows of the grid of 2^21 blocks: a launch of 2^32 threads in one dimension starts fewer and says nothing
+    const int across = p.B < 1 << 21 ? p.B : 1 << 21;
+    const dim3 rows(across, (p.B - 1) / across + 1);
+    if (p.chunks > 1) hipLaunchKernelGGL((sample_kernel<BF16, true>), rows, dim3(kThreads), sizeof(Shared), s, p);
+    else hipLaunchKernelGGL((sample_kernel<BF16, false>), rows, dim3(kThreads), sizeof(Shared), s, p);
     MOE_LAUNCH_CHECK("sample_kernel");
     return MOE_OK;
 }

@@ -250,3 +250,20 @@ def test_outputs_and_settings_that_do_not_fit_are_refused():
     with pytest.raises(ValueError):
         binding.moe_sample(x.cpu(), u.cpu())
     check(x, u.cpu().numpy())
+
+
+def test_more_rows_than_2_32_threads():
+    """4.2 million rows of three tokens: a block each."""
+    B = (1 << 22) + 1000
+    gen = torch.Generator(device=DEV).manual_seed(4)
+    x = torch.empty((B, 3), device=DEV).normal_(0, 1, generator=gen)
+    u = torch.rand(B, device=DEV, generator=gen)
+    token, logprob = binding.moe_sample(x, u, token=torch.full((B,), -7, dtype=torch.int32, device=DEV))
+    p = torch.softmax(x.double(), 1)
+    c = p.cumsum(1)
+    want = (u.double()[:, None] >= c[:, :2]).sum(1)
+    near = ((u.double()[:, None] - c[:, :2]).abs() < 1e-9).any(1)            # sums of another order
+    assert ((token.long() == want) | near).all()
+    # log(p) is rounded once to fp32, 2^-24 of it; both sides' 64-bit weights 1e-12
+    lp = torch.log(torch.gather(p, 1, token.long()[:, None]))[:, 0]
+    assert ((logprob.double() - lp).abs() <= 2.0 ** -24 * lp.abs() + 1e-11).all()
