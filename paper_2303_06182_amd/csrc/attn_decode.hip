@@ -20,7 +20,7 @@
 // or two that do not are left in LDS, where the block joins them; what reaches past the block is joined by a second kernel.
 // (With the waves of a block on one unit at a time, joined after each, short sequences cost a block 8 us a unit: 32 sequences of up to
 // 1111 keys, 16 heads of 64, fp32 41 us.)
-// Measured: 64 sequences of up to 16384 keys, 32 heads over 4 of 128, 116 MB: 31 us, 3.7 TB/s (a kernel that only sums reads 4.0), and 7 to join.
+// Measured: 64 sequences of up to 16384 keys, 32 heads over 4 of 128, 116 MB: 31 us, 3.7 TB/s (a kernel that only sums reads 4.0), and 6 to join.
 #include "attn_dev.h"
 
 #include <mutex>
@@ -553,6 +553,7 @@ int launch_as(AttnParams p, int num_cus, hipStream_t s)
     //    1 x 1000 keys, 16 heads of 64     10.5 / 13.5 / 10.4       1 x 1000, 8 heads of 128    14.3 / 19.2 / 12.7
     //    8 x 2000 keys, 16 heads of 64        - / 18.1 / 14.1       8 x 2000, 8 heads of 128       - / 19.4 / 19.6
     //   64 x 2000 keys, 16 heads of 64     51.7 / 74.0 / 56.5     256 x 500, 16 heads of 64     55.6 / -    / 92.0
+    // It goes by the caller's bound, as the lengths are on the device: 900 keys of 16 heads of 64, captured, 7.9 us with bounds of 2048 and less, 12.8 above.
     static constexpr bool kTwice = blocks_per_cu<DH, NS>() == 2;
     const int tiles = ceil_div(p.max_kv, tile_keys(DH));
     const bool every = (int64_t)p.units * p.B >= num_cus;

@@ -19,8 +19,9 @@
 //
 // Bound by the matrix cores and the exponentials (a quarter of the rate of other instructions) in about equal parts: per 32 x 64 weights
 // and wave 32 MFMAs of 32 cycles, 32 exponentials of 16 and some 110 others of 4.  Two waves a SIMD overlap them.  Measured: 8192 tokens, 16
-// heads of 128, bf16, causal: 294 us, 934 TFLOP/s; matrix pipes busy 37 %, vector issue 44 %, LDS reads about 40 %.  (Half of the waves held half a tile behind
-// the others by barriers, so that products meet exponentials: 327; other priorities of the waves: no difference.)
+// heads of 128, bf16, causal: 299 to 305 us, 900 to 920 TFLOP/s; matrix pipes busy 36 %, vector issue 45 %, LDS reads about 40 %.  (Half of the waves held half
+// a tile behind the others by barriers, so that products meet exponentials: 327 where this took 307; other priorities of the waves: no difference.)
+// Over 256 dimensions a wave has no registers left: 25 of them spill with bf16 queries, 161 with fp32.
 //
 // Blocks begin with the last rows, which see the most keys; a sequence's heads stay on one XCD and its L2.  Where there are too few
 // blocks for the chip, the keys are cut into parts, joined by a second kernel.
@@ -69,7 +70,7 @@ __device__ __forceinline__ void tile_range(const AttnParams &p, const Seq &sq, i
 }
 
 // Tiles between two barriers: while these are computed the next ones are stored.  With two, waves need not keep step so closely, and 8 waves' block
-// has the LDS for four buffers (8192 tokens of 16 heads of 128: 294 us, with one 307).  A block of 4 shares its CU with another.
+// has the LDS for four buffers (8192 tokens of 16 heads of 128: 294 us where one takes 307).  A block of 4 shares its CU with another.
 template <int W>
 constexpr int kTogether = W == 8 ? 2 : 1;
 

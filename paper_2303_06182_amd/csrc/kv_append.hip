@@ -377,7 +377,8 @@ int launch_sized(const AppendParams &p, hipStream_t s)
 {
     const int rows = p.a.max_q < (1 << p.a.page_shift) ? p.a.max_q : 1 << p.a.page_shift;
     const int items = 2 * rows * (DH / 16);  // of keys and values in a block
-    // a key's and a value's item a thread, so that a block's loads are all in flight at once and registers leave room for five waves a SIMD
+    // A key's and a value's item a thread, so that a block's loads are all in flight at once; 124 registers leave room for four waves a SIMD (fp32: 148,
+    // three).  Blocks of 1024 threads have 128 a thread: fp32 spills 24 of them, four items a thread (pages of 128 rows of 256) 56, fp32 104.
     if (items <= 64) return launch_as<DH, BF16, 64, 1>(p, s);
     if (items <= 128) return launch_as<DH, BF16, 64, 2>(p, s);
     if (items <= 512) return launch_as<DH, BF16, 256, 2>(p, s);

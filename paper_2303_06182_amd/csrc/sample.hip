@@ -13,7 +13,7 @@
 // before a token can fall on another token than in exact sums.  A token that weighs less than 2^-(f+1) (2^-46 for 128000) counts as nothing.
 //
 // Bound by the 64-bit weights and by the passes over the row, for few rows by latency.  Measured, all filters mixed, the four kernels: 256 rows of
-// 128000 fp32 logits (131 MB) 22 + 35 + 41 + 35 us; 64 rows of 51201 in bf16 5 + 9 + 15 + 32; one row of 128000 by top-p 3 + 9 + 8 + 19.
+// 128000 fp32 logits (131 MB) 22 + 34 + 41 + 31 us; 64 rows of 51201 in bf16 6 + 9 + 15 + 29; one row of 128000 by top-p 3 + 10 + 8 + 17.
 #include <stddef.h>
 
 #include <mutex>
