@@ -13,8 +13,9 @@
  * expert, one-hot dispatch masks multiplied with the tokens, drops and zero
  * padding) is exported as a baseline for comparison.  Expert Buffering (Sec. 6:
  * expert parameters in host memory behind a small device cache), expert weights
- * of 8 and 4 bits and the rest of a decoder step (a paged cache of keys and
- * values, attention over it, sampling) are at the end.
+ * of 8 and 4 bits, the rest of a decoder step (a paged cache of keys and
+ * values, attention over it, sampling) and the layer with other scores than a
+ * softmax and with its experts' products in 8 bits are at the end.
  *
  * Conventions for every call
  *   - Plain C.  Returns MOE_OK (0) or a negative MOE_ERR_* code; after an error
@@ -493,6 +494,91 @@ int64_t moe_sample_workspace_bytes(int32_t B, int32_t V);
 int moe_sample(const void *logits, int32_t dtype, int64_t row_stride, int32_t B, int32_t V, const float *u,
                const float *temperature, const int32_t *top_k, const float *top_p, const float *min_p, int32_t *token,
                float *logprob, void *workspace, int64_t workspace_bytes, void *stream);
+
+/* ---- The layer with experts chosen by scores, a bias and groups, and with the experts' products in 8 bits ---- */
+/* ---- (not in the paper)                                                                                   ---- */
+
+#define MOE_SCORE_SOFTMAX 0
+#define MOE_SCORE_SIGMOID 1
+#define MOE_MAX_GROUPS 64
+
+/* Supported: 1 <= E <= MOE_MAX_E; n_groups a divisor of E, at most MOE_MAX_GROUPS; 1 <= groups_kept <= n_groups;
+ * 1 <= k <= MOE_MAX_K, and no more than the experts of groups_kept groups; group_top 1 or 2; a finite scale. */
+typedef struct moe_select_config {
+    int32_t E;
+    int32_t k;
+    int32_t score;       /* MOE_SCORE_* */
+    int32_t n_groups;    /* groups of E / n_groups consecutive experts */
+    int32_t groups_kept; /* equal to n_groups: groups play no part */
+    int32_t group_top;
+    int32_t renormalize; /* 1: the weights are divided by their sum */
+    float scale;         /* of the weights */
+} moe_select_config_t;
+
+/* Experts of every row of logits [T, E] (dtype F32 or BF16, row_stride elements from row to row), with the bias [E] fp32 that
+ * balancing has found, or NULL:
+ *   s[e] = 1 / (1 + exp(-logit[e]))  or  exp(logit[e]) / sum over all experts of exp(logit)
+ *   key[e] = s[e] + bias[e]
+ *   groups: those groups_kept whose group_top largest keys add up to most stay, equal ones to the lower index
+ *   topk_idx[t, 0 .. k-1] = the experts of these groups with the largest keys, slot 0 the largest, equal ones to the lower index
+ *   topk_w[t, j] = scale * s[topk_idx[t, j]], divided by the sum over j if renormalize
+ * in 64 bits, the weights rounded once to fp32.  The bias moves the selection and not the weights.  An expert with a logit or a bias that is
+ * NaN or -infinity has no key: it adds nothing to its group's sum (a group of such experts comes last), is selected only where there are no k
+ * others in the groups that stay, in ascending index, and then has weight 0.  A finite logit, however low, has a key.
+ * Where all weights of a row are 0, renormalising leaves them.  The indices of a row are distinct and lie in [0, E).
+ * With softmax scores and a largest logit of +infinity, those that are +infinity share 1 among them.
+ * logits and bias are aligned to their elements only, topk_idx and topk_w [T, k] to 4 bytes.  No workspace. */
+int moe_select_experts(const moe_select_config_t *cfg, const void *logits, int32_t dtype, int64_t row_stride, const float *bias, int32_t T,
+                       int32_t *topk_idx, float *topk_w, void *stream);
+
+/* e4m3 operands with a scale per block of 128.  A row of `cols` elements (cols a multiple of 16, the last block may be short) is cols
+ * bytes, OCP e4m3, row after row; the scale of block b is 2^(byte - 127) with byte b of the row's moe_b128_scale_cols(cols) scale bytes, that is
+ * one for each block, in groups of four (those behind the last block hold 127).  Activations have such scales for every row, weights for every
+ * 128 rows of a matrix.  Bytes are in 1 .. 254. */
+int64_t moe_b128_scale_cols(int32_t cols);
+
+/* Quantises x [matrices, rows, cols] (dtype F32 or BF16, row_stride elements from each row to the next, a multiple of 16 bytes) in blocks of block_rows
+ * (1 or 128) rows and 128 columns: scale = the smallest power of two, at least 2^-126, that the largest finite |x| of the block does
+ * not exceed 448 times (1 for a block of zeros), q = e4m3(x / scale), to nearest even; elements that are not finite become NaN.
+ * q_out [matrices, rows, cols] bytes, scale_out [matrices, rows or ceil(rows / 128), moe_b128_scale_cols(cols)] bytes. */
+int moe_quantize_b128(const void *x, int32_t dtype, int64_t row_stride, int32_t matrices, int32_t rows, int32_t cols, int32_t block_rows,
+                      void *q_out, void *scale_out, void *stream);
+
+/* Product of such operands, grouped by expert:
+ *   for r in [offsets[e], offsets[e+1]):  c[r, n] = sum_k A[a_rows[r], k] * W[e][n, k]
+ * a_q [a_count, K] with a scale per row and block, a_rows [n_rows] int32 or NULL (row r is row r of a_q; indices are clamped to
+ * [0, a_count)); w_q [E, N, K] with w_scale [E, ceil(N / 128), moe_b128_scale_cols(K)]; offsets [E + 1] int32 on the device, ascending and within
+ * [0, n_rows] (clamped to that), or NULL with E = 1: all rows.  c [n_rows, N] of c_dtype; rows outside every expert's range are left as they are, and
+ * an expert without rows is not read.  N a multiple of 8, K of 16, 1 <= E <= MOE_MAX_E, 0 <= n_rows < 2^30.
+ * Sums are formed in fp32.  With c_dtype BF16 the matrix cores' 8-bit instruction forms them, which aligns the products of 8 neighbouring k to
+ * the largest of them and drops what is less than about 2^-14 of that; it is off by 1.4e-5 of the results' standard deviation on
+ * normally distributed operands (their rounding to bf16: 1.7e-3).  With F32 nothing is dropped, at half the rate.  A scaled element
+ * below 2^-126 may count as 0. */
+int moe_gemm_b128(const void *a_q, const void *a_scale, int32_t a_count, const int32_t *a_rows, const void *w_q, const void *w_scale,
+                  const int32_t *offsets, int32_t E, int32_t n_rows, int32_t N, int32_t K, void *c, int32_t c_dtype, void *stream);
+
+#define MOE_ACT_RELU 0
+#define MOE_ACT_SILU 1 /* gated: silu(g) * u */
+
+/* The experts' feed-forward on such weights: x [x_rows, D] elem is quantised by rows, and for r in [offsets[e], offsets[e+1])
+ *   MOE_ACT_RELU:  h = relu(W1[e] x[src_tok[r]]),                                w1_q [E, F, D]
+ *   MOE_ACT_SILU:  h = silu(g) * u, g = W1[e][0] x[src_tok[r]], u = W1[e][1] x[src_tok[r]],  w1_q [E, 2, F, D], scales [E, 2, ceil(F / 128), ..]
+ *   yp[r] = W2[e] h',  h' = h quantised by rows,                                 w2_q [E, D, F]
+ * src_tok [n_rows] int32 (as moe_route_counts writes it; clamped to [0, x_rows)) or NULL: row r of x.  Offsets as in moe_gemm_b128.  silu(g) = g / (1 +
+ * exp(-g)); h in fp32, from the sums of the first product, and rounded to e4m3 only.  yp [n_rows, D] elem.  The handle's D and F are multiples of 16;
+ * x_rows and n_rows at most k * T_max.  The handle's device has to be the current one.
+ * Workspace: moe_b128_workspace_bytes(). */
+int64_t moe_b128_workspace_bytes(const moe_handle_t *h);
+int moe_expert_ffn_b128(moe_handle_t *h, const void *x, int32_t x_rows, const int32_t *src_tok, const int32_t *offsets, const void *w1_q,
+                        const void *w2_q, const void *w1_scale, const void *w2_scale, int32_t activation, int32_t n_rows, void *yp,
+                        void *workspace, int64_t workspace_bytes, void *stream);
+
+/* moe_layer_forward with these experts, chosen by moe_select_experts from the gate's logits (gate_bias is added to those, as ever, select_bias to the
+ * scores).  select->E and select->k are the handle's; its `renormalize` plays no part.  Same workspace as moe_expert_ffn_b128. */
+int moe_layer_forward_b128(moe_handle_t *h, const void *x, const void *wg, const float *gate_bias, const moe_select_config_t *select,
+                           const float *select_bias, const void *w1_q, const void *w2_q, const void *w1_scale, const void *w2_scale,
+                           int32_t activation, int32_t T, void *y, const moe_routing_t *routing_out, void *workspace, int64_t workspace_bytes,
+                           void *stream);
 
 #ifdef __cplusplus
 }

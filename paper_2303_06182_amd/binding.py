@@ -26,6 +26,10 @@ MOE_STATIC_EINSUM = 0
 MOE_STATIC_INDEXED = 1
 MOE_CAPACITY_PAPER = 0
 MOE_CAPACITY_SHARE = 1
+MOE_SCORE_SOFTMAX = 0
+MOE_SCORE_SIGMOID = 1
+MOE_ACT_RELU = 0
+MOE_ACT_SILU = 1
 
 EXPORTS = [
     "moe_create", "moe_destroy", "moe_last_error", "moe_workspace_bytes", "moe_static_workspace_bytes",
@@ -40,6 +44,8 @@ EXPORTS = [
     "moe_expert_cache_bytes_q", "moe_expert_cache_create_q", "moe_layer_forward_noalloc",
     "moe_attn_create", "moe_attn_destroy", "moe_attn_workspace_bytes", "moe_kv_append", "moe_attn_forward",
     "moe_sample", "moe_sample_workspace_bytes",
+    "moe_select_experts", "moe_b128_scale_cols", "moe_quantize_b128", "moe_gemm_b128", "moe_b128_workspace_bytes", "moe_expert_ffn_b128",
+    "moe_layer_forward_b128",
 ]
 MOE_NOALLOC_SCRATCH_BYTES = 8 * 1024 * 1024
 
@@ -62,6 +68,10 @@ class MoeKvCache(ctypes.Structure):
 class MoeAttnConfig(ctypes.Structure):
     _fields_ = [(n, ctypes.c_int32) for n in ("B_max", "T_max", "n_heads", "n_kv_heads", "head_dim", "page_size", "num_pages",
                                               "max_pages", "dtype", "rot_dim", "rot_interleaved")]
+
+
+class MoeSelectConfig(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("E", "k", "score", "n_groups", "groups_kept", "group_top", "renormalize")] + [("scale", ctypes.c_float)]
 
 
 class MoeError(RuntimeError):
@@ -184,6 +194,21 @@ def load_library() -> ctypes.CDLL:
     lib.moe_sample_workspace_bytes.restype = i64
     lib.moe_sample.argtypes = [vp, i32, i64, i32, i32, vp, vp, vp, vp, vp, vp, vp, vp, i64, vp]
     lib.moe_sample.restype = ctypes.c_int
+    lib.moe_select_experts.argtypes = [ctypes.POINTER(MoeSelectConfig), vp, i32, i64, vp, i32, vp, vp, vp]
+    lib.moe_select_experts.restype = ctypes.c_int
+    lib.moe_b128_scale_cols.argtypes = [i32]
+    lib.moe_b128_scale_cols.restype = i64
+    lib.moe_quantize_b128.argtypes = [vp, i32, i64, i32, i32, i32, i32, vp, vp, vp]
+    lib.moe_quantize_b128.restype = ctypes.c_int
+    lib.moe_gemm_b128.argtypes = [vp, vp, i32, vp, vp, vp, vp, i32, i32, i32, i32, vp, i32, vp]
+    lib.moe_gemm_b128.restype = ctypes.c_int
+    lib.moe_b128_workspace_bytes.argtypes = [vp]
+    lib.moe_b128_workspace_bytes.restype = i64
+    lib.moe_expert_ffn_b128.argtypes = [vp, vp, i32, vp, vp, vp, vp, vp, vp, i32, i32, vp, vp, i64, vp]
+    lib.moe_expert_ffn_b128.restype = ctypes.c_int
+    lib.moe_layer_forward_b128.argtypes = [vp, vp, vp, vp, ctypes.POINTER(MoeSelectConfig), vp, vp, vp, vp, vp, i32, i32, vp,
+                                           ctypes.POINTER(MoeRouting), vp, i64, vp]
+    lib.moe_layer_forward_b128.restype = ctypes.c_int
     _lib = lib
     return lib
 
@@ -247,12 +272,15 @@ class MoeLayer:
         self.dtype = dtype
         self.torch_dtype = torch.bfloat16 if dtype == "bf16" else torch.float32
         self.device = torch.device(device)
+        if self.device.index is None:
+            self.device = torch.device("cuda", torch.cuda.current_device())
         h = ctypes.c_void_p()
         with torch.cuda.device(self.device):
             _check(self.lib.moe_create(ctypes.byref(self.cfg), ctypes.byref(h)))
         self.h = h
         self.workspace_bytes = int(self.lib.moe_workspace_bytes(self.h))
         self.workspace = None
+        self.workspace_b128 = None
         if alloc_workspace:
             self.workspace = torch.empty(self.workspace_bytes, dtype=torch.uint8, device=self.device)
 
@@ -408,6 +436,63 @@ class MoeLayer:
         _check(self.lib.moe_layer_forward_w4(self.h, _ptr(x), _ptr(wg), _ptr(gate_bias), _ptr(w1_q), _ptr(w2_q),
                                              _ptr(w1_scale), _ptr(w2_scale), _ptr(b1), _ptr(b2), T, _ptr(y),
                                              self._routing_struct(routing_out), ws, wsb, _stream()))
+        return y
+
+    # -- experts in e4m3 with a scale per block of 128 -------------------------------------------
+    def b128_workspace(self) -> torch.Tensor:
+        """The workspace of the two calls below, allocated on first use (before a capture, so that no graph owns it)."""
+        if self.workspace_b128 is None:
+            self.workspace_b128 = torch.empty(int(self.lib.moe_b128_workspace_bytes(self.h)), dtype=torch.uint8, device=self.device)
+        return self.workspace_b128
+
+    def _b128_weights(self, w1_q, w2_q, w1_scale, w2_scale, activation: str) -> int:
+        act = _choice("activation", activation, {"relu": MOE_ACT_RELU, "silu": MOE_ACT_SILU})
+        E, D, F = self.E, self.D, self.F
+        halves = (2,) if act == MOE_ACT_SILU else ()
+        _b128_operand(w1_q, w1_scale, (E, *halves, F, D), (E, *halves), 128, self.device.index, "w1")
+        _b128_operand(w2_q, w2_scale, (E, D, F), (E,), 128, self.device.index, "w2")
+        return act
+
+    def _rows_of(self, t, shape, dtype, name: str):
+        if t is not None and (tuple(t.shape) != shape or t.dtype != dtype or t.get_device() != self.device.index):
+            raise ValueError("%s must be %s of %s on %s" % (name, list(shape), dtype, self.device))
+        return _addr(t)
+
+    def moe_expert_ffn_b128(self, x, offsets, w1_q, w2_q, w1_scale, w2_scale, activation: str = "silu", src_tok=None, yp=None):
+        """x [x_rows, D]; w1_q [E, 2, F, D] (silu: gate, up) or [E, F, D] (relu), w2_q [E, D, F] and their scales from moe_quantize_b128 ->
+        yp, a row for each of src_tok (None: of x)."""
+        act = self._b128_weights(w1_q, w2_q, w1_scale, w2_scale, activation)
+        x_rows = x.shape[0]
+        n_rows = x_rows if src_tok is None else src_tok.shape[0]
+        if yp is None:
+            yp = self._new((n_rows, self.D), self.torch_dtype)
+        else:
+            _output(yp, (n_rows, self.D), self.torch_dtype, self.device.index, "yp")
+        ws = self.b128_workspace()
+        _check(self.lib.moe_expert_ffn_b128(self.h, self._rows_of(x, (x_rows, self.D), self.torch_dtype, "x"), x_rows,
+                                            self._rows_of(src_tok, (n_rows,), torch.int32, "src_tok"),
+                                            self._rows_of(offsets, (self.E + 1,), torch.int32, "offsets"), _addr(w1_q), _addr(w2_q), _addr(w1_scale),
+                                            _addr(w2_scale), act, n_rows, _addr(yp), ws.data_ptr(), ws.numel(), _stream_on(self.device.index)))
+        return yp
+
+    def moe_layer_forward_b128(self, x, wg, w1_q, w2_q, w1_scale, w2_scale, activation: str = "silu", score: str = "sigmoid", select_bias=None,
+                               n_groups: int = 1, groups_kept: int = 1, group_top: int = 2, renormalize: bool = True, scale: float = 1.0,
+                               gate_bias=None, y=None, routing_out=None):
+        """The layer with experts chosen as moe_select_experts does, and moe_expert_ffn_b128."""
+        act = self._b128_weights(w1_q, w2_q, w1_scale, w2_scale, activation)
+        cfg = _select_config(self.E, self.k, score, n_groups, groups_kept, group_top, renormalize, scale)
+        T = x.shape[0]
+        if y is None:
+            y = self._new((T, self.D), self.torch_dtype)
+        else:
+            _output(y, (T, self.D), self.torch_dtype, self.device.index, "y")
+        ws = self.b128_workspace()
+        _check(self.lib.moe_layer_forward_b128(self.h, self._rows_of(x, (T, self.D), self.torch_dtype, "x"),
+                                               self._rows_of(wg, (self.E, self.D), self.torch_dtype, "wg"),
+                                               self._rows_of(gate_bias, (self.E,), torch.float32, "gate_bias"), ctypes.byref(cfg),
+                                               self._rows_of(select_bias, (self.E,), torch.float32, "select_bias"), _addr(w1_q), _addr(w2_q),
+                                               _addr(w1_scale), _addr(w2_scale), act, T, _addr(y), self._routing_struct(routing_out), ws.data_ptr(),
+                                               ws.numel(), _stream_on(self.device.index)))
         return y
 
     def moe_profile_begin(self) -> None:
@@ -711,3 +796,108 @@ def moe_sample(logits, u, temperature=None, top_k=None, top_p=None, min_p=None, 
                           logits.stride(0) if B > 1 else V, B, V, _addr(u), _addr(temperature), _addr(top_k), _addr(top_p), _addr(min_p), _addr(token),
                           _addr(logprob), _addr(workspace), workspace.numel(), _stream_on(index)))
     return token, logprob
+
+
+def _choice(name: str, value: str, choices: dict) -> int:
+    if value not in choices:
+        raise ValueError("%s must be one of %s, not %r" % (name, sorted(choices), value))
+    return choices[value]
+
+
+def _current_gpu(t: torch.Tensor, name: str) -> int:
+    index = t.get_device()
+    if index < 0 or index != torch.cuda.current_device():
+        raise ValueError("%s is on %s, which is not the current GPU" % (name, t.device))
+    return index
+
+
+def _select_config(E: int, k: int, score: str, n_groups: int, groups_kept: int, group_top: int, renormalize: bool, scale: float) -> MoeSelectConfig:
+    return MoeSelectConfig(E, k, _choice("score", score, {"softmax": MOE_SCORE_SOFTMAX, "sigmoid": MOE_SCORE_SIGMOID}), n_groups, groups_kept, group_top,
+                           int(renormalize), scale)
+
+
+def moe_select_experts(logits, k: int, bias=None, score: str = "sigmoid", n_groups: int = 1, groups_kept: int = 1, group_top: int = 2,
+                       renormalize: bool = True, scale: float = 1.0, topk_idx=None, topk_w=None):
+    """logits [T, E] (float32 or bfloat16, rows at any stride), bias [E] fp32 or None -> (topk_idx [T, k] int32, topk_w [T, k] fp32)."""
+    if logits.dim() != 2 or logits.dtype not in (torch.float32, torch.bfloat16) or (logits.shape[1] > 1 and logits.stride(1) != 1):
+        raise ValueError("logits must be [T, E] of float32 or bfloat16 with dense rows")
+    T, E = logits.shape
+    index = _current_gpu(logits, "logits")
+    if bias is not None and (tuple(bias.shape) != (E,) or bias.dtype != torch.float32 or bias.get_device() != index):
+        raise ValueError("bias must be [%d] of float32 on %s" % (E, logits.device))
+    cfg = _select_config(E, k, score, n_groups, groups_kept, group_top, renormalize, scale)
+    new = lambda dtype: torch.empty((T, max(k, 0)), dtype=dtype, device=logits.device)  # noqa: E731
+    topk_idx = new(torch.int32) if topk_idx is None else _output(topk_idx, (T, k), torch.int32, index, "topk_idx")
+    topk_w = new(torch.float32) if topk_w is None else _output(topk_w, (T, k), torch.float32, index, "topk_w")
+    _check(load_library().moe_select_experts(ctypes.byref(cfg), logits.data_ptr(), MOE_DTYPE_BF16 if logits.dtype == torch.bfloat16 else MOE_DTYPE_F32,
+                                             logits.stride(0) if T > 1 else E, _addr(bias), T, topk_idx.data_ptr(), topk_w.data_ptr(), _stream_on(index)))
+    return topk_idx, topk_w
+
+
+def b128_scale_cols(cols: int) -> int:
+    """Scale bytes of a row of `cols` elements: one for each block of 128, in groups of four."""
+    n = int(load_library().moe_b128_scale_cols(cols))
+    if n < 0:
+        _check(n)
+    return n
+
+
+def _b128_operand(q, scale, shape: tuple, scale_rows: tuple, block_rows: int, index: int, name: str) -> None:
+    """q of `shape` and its scales; scale_rows: the dimensions in front of a matrix's rows, of the scales."""
+    scales = scale_rows + (-(-shape[-2] // block_rows), -(-shape[-1] // 512) * 4)
+    if tuple(q.shape) != shape or q.element_size() != 1 or not q.is_contiguous() or q.get_device() != index:
+        raise ValueError("%s_q must be %s of one byte each, contiguous, on cuda:%d" % (name, list(shape), index))
+    if tuple(scale.shape) != scales or scale.dtype != torch.uint8 or not scale.is_contiguous() or scale.get_device() != index:
+        raise ValueError("%s_scale must be %s of uint8, contiguous, on cuda:%d" % (name, list(scales), index))
+
+
+def moe_quantize_b128(x, block_rows: int = 1, q=None, scale=None):
+    """x [rows, cols] or [..., rows, cols] (float32 or bfloat16; rows at one stride throughout) -> (q of the same shape, torch.float8_e4m3fn, scale
+    bytes [..., rows or blocks of 128 rows, b128_scale_cols(cols)])."""
+    if x.dim() < 2 or x.dtype not in (torch.float32, torch.bfloat16) or (x.shape[-1] > 1 and x.stride(-1) != 1):
+        raise ValueError("x must be [..., rows, cols] of float32 or bfloat16 with dense rows")
+    index = _current_gpu(x, "x")
+    lead, (rows, cols) = tuple(x.shape[:-2]), x.shape[-2:]
+    matrices = 1
+    for n in lead:
+        matrices *= n
+    # all rows, of all matrices, at one stride
+    outer = [(n, s) for n, s in zip(x.shape[:-1], x.stride()[:-1]) if n > 1] if x.numel() else []
+    stride = outer[-1][1] if outer else cols
+    step = stride
+    for n, s in reversed(outer):
+        if s != step:
+            raise ValueError("the rows of x must lie at one stride")
+        step *= n
+    if block_rows not in (1, 128):
+        raise ValueError("block_rows must be 1 or 128")
+    scales = lead + (-(-rows // block_rows), b128_scale_cols(cols))
+    q = torch.empty(x.shape, dtype=torch.float8_e4m3fn, device=x.device) if q is None else _output(q, tuple(x.shape), torch.float8_e4m3fn, index, "q")
+    scale = torch.empty(scales, dtype=torch.uint8, device=x.device) if scale is None else _output(scale, scales, torch.uint8, index, "scale")
+    _check(load_library().moe_quantize_b128(x.data_ptr(), MOE_DTYPE_BF16 if x.dtype == torch.bfloat16 else MOE_DTYPE_F32, stride, matrices, rows, cols,
+                                            block_rows, q.data_ptr(), scale.data_ptr(), _stream_on(index)))
+    return q, scale
+
+
+def moe_gemm_b128(a_q, a_scale, w_q, w_scale, offsets=None, a_rows=None, out_dtype=torch.bfloat16, out=None):
+    """a_q [a_count, K] and w_q [E, N, K] (or [N, K]) with their scales from moe_quantize_b128 -> [rows, N]; a_rows: which row of a_q each row is
+    (None: all, in order); offsets [E + 1] int32: where every expert's rows begin (None: one expert)."""
+    if a_q.dim() != 2 or w_q.dim() not in (2, 3):
+        raise ValueError("a_q must be [rows, K], w_q [E, N, K]")
+    index = _current_gpu(a_q, "a_q")
+    (count, K), N = a_q.shape, w_q.shape[-2]
+    E = w_q.shape[0] if w_q.dim() == 3 else 1
+    _b128_operand(a_q, a_scale, (count, K), (), 1, index, "a")
+    _b128_operand(w_q, w_scale, (*w_q.shape[:-1], K), tuple(w_q.shape[:-2]), 128, index, "w")
+    rows = count if a_rows is None else a_rows.shape[0]
+    for name, t, shape in (("a_rows", a_rows, (rows,)), ("offsets", offsets, (E + 1,))):
+        if t is not None and (tuple(t.shape) != shape or t.dtype != torch.int32 or t.get_device() != index):
+            raise ValueError("%s must be %s of int32 on cuda:%d" % (name, list(shape), index))
+    if out is not None:
+        out_dtype = out.dtype
+    if out_dtype not in (torch.bfloat16, torch.float32):
+        raise ValueError("out_dtype must be bfloat16 or float32")
+    out = torch.empty((rows, N), dtype=out_dtype, device=a_q.device) if out is None else _output(out, (rows, N), out_dtype, index, "out")
+    _check(load_library().moe_gemm_b128(a_q.data_ptr(), a_scale.data_ptr(), count, _addr(a_rows), w_q.data_ptr(), w_scale.data_ptr(), _addr(offsets), E, rows, N,
+                                        K, out.data_ptr(), MOE_DTYPE_BF16 if out_dtype == torch.bfloat16 else MOE_DTYPE_F32, _stream_on(index)))
+    return out

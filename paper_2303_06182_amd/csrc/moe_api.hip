@@ -10,6 +10,7 @@
 #include <new>
 #include <vector>
 
+#include "b128_internal.h"
 #include "moe_internal.h"
 
 namespace moe355 {
@@ -257,6 +258,38 @@ static int validate_config(const moe_config_t *c)
 }
 
 // ---- the five steps ------------------------------------------------------------------------------
+// The gate's logits [T,E] as a plain GEMM.  parts: room for slices along K (see do_gate_topk) or NULL; *split slices were written, the first
+// to logits, the others to parts, *split_stride apart.
+static int run_gate_gemm(moe_handle_t *h, const void *x, const void *wg, const float *gate_bias, int T, float *logits, float *parts,
+                         hipStream_t s, int *split, int64_t *split_stride)
+{
+    const moe_config_t &c = h->cfg;
+    *split = 1;
+    if (parts && c.dtype == MOE_DTYPE_BF16 && T <= kGateSplitTokens) {
+        *split = gemm_bf16_gate_split(T, c.E, c.D, h->num_cus);
+        if (*split > kGateSplitMax) *split = kGateSplitMax;
+    }
+    GemmParams p;
+    memset(&p, 0, sizeof(p));
+    p.A = x;
+    p.lda = c.D;
+    p.B = wg;
+    p.ldb = c.D;
+    p.bias_f32 = gate_bias;
+    p.C = logits;
+    p.ldc = c.E;
+    p.M = T;
+    p.N = c.E;
+    p.K = c.D;
+    if (*split > 1) {
+        p.k_split = *split;
+        p.c_parts = parts;
+        p.split_stride = (int64_t)T * c.E;
+    }
+    *split_stride = p.split_stride;
+    return launch_gemm(c.dtype, p, false, 0, true, false, h->num_cus, s);
+}
+
 // logits_req: where the caller wants the [T,E] logits, or NULL; logits_ws: room for them in the workspace, used
 // when a kernel needs them in memory and the caller did not ask (NULL only together with a non-NULL logits_req).
 // parts: room for (kGateSplitMax - 1) * min(T_max, kGateSplitTokens) * E floats, or NULL.  A decoder step's
@@ -286,34 +319,14 @@ static int do_gate_topk(moe_handle_t *h, const void *x, const void *wg, const fl
     }
     float *logits = logits_req ? logits_req : logits_ws;
     int split = 1;
-    if (parts && c.dtype == MOE_DTYPE_BF16 && T <= kGateSplitTokens) {
-        split = gemm_bf16_gate_split(T, c.E, c.D, h->num_cus);
-        if (split > kGateSplitMax) split = kGateSplitMax;
-    }
-    GemmParams p;
-    memset(&p, 0, sizeof(p));
-    p.A = x;
-    p.lda = c.D;
-    p.B = wg;
-    p.ldb = c.D;
-    p.bias_f32 = gate_bias;
-    p.C = logits;
-    p.ldc = c.E;
-    p.M = T;
-    p.N = c.E;
-    p.K = c.D;
-    if (split > 1) {
-        p.k_split = split;
-        p.c_parts = parts;
-        p.split_stride = (int64_t)T * c.E;
-    }
-    int rc = launch_gemm(c.dtype, p, false, 0, true, false, h->num_cus, s);
+    int64_t split_stride = 0;
+    int rc = run_gate_gemm(h, x, wg, gate_bias, T, logits, parts, s, &split, &split_stride);
     if (rc != MOE_OK) return rc;
     if (route) {
-        rc = launch_route_topk(logits, T, c.E, c.k, c.renormalize, idx, w, s, split, parts, p.split_stride, *route, routed);
+        rc = launch_route_topk(logits, T, c.E, c.k, c.renormalize, idx, w, s, split, parts, split_stride, *route, routed);
         if (rc != MOE_OK || *routed) return rc;
     }
-    return launch_topk(logits, T, c.E, c.k, c.renormalize, idx, w, s, split, parts, p.split_stride);
+    return launch_topk(logits, T, c.E, c.k, c.renormalize, idx, w, s, split, parts, split_stride);
 }
 
 // scale bytes of one expert's [rows, cols] matrix in the 4-bit layout: 16 per row and 512 columns
@@ -1045,6 +1058,217 @@ int moe_layer_forward_w4(moe_handle_t *h, const void *x, const void *wg, const f
     return layer_forward_impl(h, nullptr, x, wg, gate_bias, w1_q, w2_q, b1, b2, T, y, routing_out, workspace,
                               workspace_bytes, stream, nullptr, nullptr, static_cast<const uint8_t *>(w1_scale),
                               static_cast<const uint8_t *>(w2_scale));
+}
+
+// ---- experts in e4m3 with a scale per block of 128 ------------------------------------------------
+struct B128Layout {
+    int64_t logits, topk_idx, topk_w, counts, offsets, dst_row, src_tok, block_hist, gate_parts, xq, xs, gu, hq, hs, yp, total;
+};
+
+static B128Layout b128_layout(const moe_config_t &c)
+{
+    B128Layout L;
+    const int64_t T = c.T_max, N = T * c.k, E = c.E, es = elem_size(c.dtype);
+    int64_t off = 0;
+    auto take = [&](int64_t bytes) {
+        const int64_t at = off;
+        off = align_up(off + (bytes > 0 ? bytes : 1), 256);
+        return at;
+    };
+    L.logits = take(T * E * 4);
+    L.topk_idx = take(N * 4);
+    L.topk_w = take(N * 4);
+    L.counts = take(E * 4);
+    L.offsets = take((E + 1) * 4);
+    L.dst_row = take(N * 4);
+    L.src_tok = take(N * 4);
+    L.block_hist = take((int64_t)route_blocks((int)T) * E * 4);
+    L.gate_parts = take((int64_t)(kGateSplitMax - 1) * (T < kGateSplitTokens ? T : kGateSplitTokens) * E * 4);
+    L.xq = take(N * c.D);  // of as many rows as the first product has: they may come without src_tok
+    L.xs = take(N * b128_scale_cols(c.D));
+    L.gu = take(N * 2 * c.F * 4);
+    L.hq = take(N * c.F);
+    L.hs = take(N * b128_scale_cols(c.F));
+    L.yp = take(N * c.D * es);
+    L.total = off;
+    return L;
+}
+
+static int check_b128(const moe_handle_t *h, int32_t activation, const void *workspace, int64_t workspace_bytes)
+{
+    const moe_config_t &c = h->cfg;
+    if (c.D % 16 != 0 || c.F % 16 != 0) {
+        set_error("experts in blocks of 128 need D and F that are multiples of 16 (D = %d, F = %d)", c.D, c.F);
+        return MOE_ERR_UNSUPPORTED;
+    }
+    if (activation != MOE_ACT_RELU && activation != MOE_ACT_SILU) {
+        set_error("unsupported activation %d", activation);
+        return MOE_ERR_UNSUPPORTED;
+    }
+    const int64_t need = b128_layout(c).total;
+    if (!workspace || reinterpret_cast<uintptr_t>(workspace) % 256 != 0 || workspace_bytes < need) {
+        set_error("workspace: %lld bytes at a multiple of 256 are needed", (long long)need);
+        return MOE_ERR_WORKSPACE;
+    }
+    int dev = -1;
+    MOE_HIP_CHECK(hipGetDevice(&dev));
+    if (dev != h->device) {
+        set_error("current device %d is not the handle's device %d", dev, h->device);
+        return MOE_ERR_INVALID_ARG;
+    }
+    return MOE_OK;
+}
+
+static int run_expert_ffn_b128(moe_handle_t *h, const void *x, int32_t x_rows, const int32_t *src_tok, const int32_t *offsets, const void *w1_q,
+                               const void *w2_q, const void *w1_scale, const void *w2_scale, int32_t activation, int32_t n_rows, void *yp,
+                               void *workspace, hipStream_t s)
+{
+    const moe_config_t &c = h->cfg;
+    const B128Layout L = b128_layout(c);
+    const bool gated = activation == MOE_ACT_SILU;
+    uint8_t *xq = at<uint8_t>(workspace, L.xq), *xs = at<uint8_t>(workspace, L.xs);
+    int rc;
+    {
+        ProfScope ps("quantize_rows", s);
+        rc = launch_quantize_b128(x, c.dtype, c.D, 1, x_rows, c.D, 1, xq, xs, s);
+    }
+    if (rc != MOE_OK) return rc;
+    GemmB128 g = {};
+    g.a = xq;
+    g.a_scale = xs;
+    g.a_count = x_rows;
+    g.a_rows = src_tok;
+    g.w = static_cast<const uint8_t *>(w1_q);
+    g.w_scale = static_cast<const uint8_t *>(w1_scale);
+    g.offsets = offsets;
+    g.E = c.E;
+    g.n_rows = n_rows;
+    g.N = gated ? 2 * c.F : c.F;
+    g.Nh = c.F;
+    g.K = c.D;
+    g.c = at<void>(workspace, L.gu);
+    g.c_dtype = MOE_DTYPE_F32;
+    g.precise = c.dtype == MOE_DTYPE_F32;
+    g.name = "expert_gemm1";
+    rc = launch_gemm_b128(g, s);
+    if (rc != MOE_OK) return rc;
+    uint8_t *hq = at<uint8_t>(workspace, L.hq), *hs = at<uint8_t>(workspace, L.hs);
+    rc = launch_act_quantize(at<float>(workspace, L.gu), gated, n_rows, c.F, offsets, c.E, hq, hs, s);
+    if (rc != MOE_OK) return rc;
+    g.a = hq;
+    g.a_scale = hs;
+    g.a_count = n_rows;
+    g.a_rows = nullptr;
+    g.w = static_cast<const uint8_t *>(w2_q);
+    g.w_scale = static_cast<const uint8_t *>(w2_scale);
+    g.N = g.Nh = c.D;
+    g.K = c.F;
+    g.c = yp;
+    g.c_dtype = c.dtype;
+    g.name = "expert_gemm2";
+    return launch_gemm_b128(g, s);
+}
+
+int64_t moe_b128_workspace_bytes(const moe_handle_t *h)
+{
+    g_err[0] = 0;
+    if (!h) {
+        set_error("handle is NULL");
+        return MOE_ERR_INVALID_ARG;
+    }
+    return b128_layout(h->cfg).total;
+}
+
+int moe_expert_ffn_b128(moe_handle_t *h, const void *x, int32_t x_rows, const int32_t *src_tok, const int32_t *offsets, const void *w1_q,
+                        const void *w2_q, const void *w1_scale, const void *w2_scale, int32_t activation, int32_t n_rows, void *yp,
+                        void *workspace, int64_t workspace_bytes, void *stream)
+{
+    g_err[0] = 0;
+    ProfBind bind(h);
+    if (!h) {
+        set_error("handle is NULL");
+        return MOE_ERR_INVALID_ARG;
+    }
+    const int64_t most = (int64_t)h->cfg.T_max * h->cfg.k;
+    if (n_rows < 0 || (int64_t)n_rows > most || x_rows < 0 || (int64_t)x_rows > most || (!src_tok && x_rows < n_rows) || (n_rows > 0 && x_rows == 0)) {
+        set_error("n_rows = %d, x_rows = %d: both in [0, k*T_max = %lld], and each of the rows is one of x", n_rows, x_rows, (long long)most);
+        return MOE_ERR_INVALID_ARG;
+    }
+    const int rc = check_b128(h, activation, workspace, workspace_bytes);
+    if (rc != MOE_OK || n_rows == 0) return rc;
+    if (bad_ptr(x, "x") || bad_ptr(src_tok, "src_tok", true) || bad_ptr(offsets, "offsets") || bad_ptr(w1_q, "w1_q") || bad_ptr(w2_q, "w2_q") ||
+        bad_ptr(w1_scale, "w1_scale") || bad_ptr(w2_scale, "w2_scale") || bad_ptr(yp, "yp"))
+        return MOE_ERR_INVALID_ARG;
+    return run_expert_ffn_b128(h, x, x_rows, src_tok, offsets, w1_q, w2_q, w1_scale, w2_scale, activation, n_rows, yp, workspace, (hipStream_t)stream);
+}
+
+int moe_layer_forward_b128(moe_handle_t *h, const void *x, const void *wg, const float *gate_bias, const moe_select_config_t *select,
+                           const float *select_bias, const void *w1_q, const void *w2_q, const void *w1_scale, const void *w2_scale,
+                           int32_t activation, int32_t T, void *y, const moe_routing_t *routing_out, void *workspace, int64_t workspace_bytes,
+                           void *stream)
+{
+    g_err[0] = 0;
+    ProfBind bind(h);
+    int rc = check_handle_T(h, T);
+    if (rc != MOE_OK) return rc;
+    rc = check_select(select);
+    if (rc != MOE_OK) return rc;
+    const moe_config_t &c = h->cfg;
+    if (select->E != c.E || select->k != c.k) {
+        set_error("select has E = %d and k = %d, the handle %d and %d", select->E, select->k, c.E, c.k);
+        return MOE_ERR_INVALID_ARG;
+    }
+    rc = check_b128(h, activation, workspace, workspace_bytes);
+    if (rc != MOE_OK) return rc;
+    moe_routing_t r;
+    memset(&r, 0, sizeof(r));
+    if (routing_out) r = *routing_out;
+    const bool empty = T == 0;
+    if (bad_ptr(x, "x", empty) || bad_ptr(wg, "wg", empty) || bad_ptr(gate_bias, "gate_bias", true) || bad_ptr(select_bias, "select_bias", true) ||
+        bad_ptr(w1_q, "w1_q", empty) || bad_ptr(w2_q, "w2_q", empty) || bad_ptr(w1_scale, "w1_scale", empty) || bad_ptr(w2_scale, "w2_scale", empty) ||
+        bad_ptr(y, "y", empty) || bad_ptr(r.logits, "routing_out.logits", true) || bad_ptr(r.topk_idx, "routing_out.topk_idx", true) ||
+        bad_ptr(r.topk_w, "routing_out.topk_w", true) || bad_ptr(r.counts, "routing_out.counts", true) ||
+        bad_ptr(r.offsets, "routing_out.offsets", true) || bad_ptr(r.dst_row, "routing_out.dst_row", true) ||
+        bad_ptr(r.src_tok, "routing_out.src_tok", true))
+        return MOE_ERR_INVALID_ARG;
+    const B128Layout L = b128_layout(c);
+    hipStream_t s = (hipStream_t)stream;
+    float *logits = r.logits ? r.logits : at<float>(workspace, L.logits);
+    int32_t *idx = r.topk_idx ? r.topk_idx : at<int32_t>(workspace, L.topk_idx);
+    float *w = r.topk_w ? r.topk_w : at<float>(workspace, L.topk_w);
+    int32_t *counts = r.counts ? r.counts : at<int32_t>(workspace, L.counts);
+    int32_t *offsets = r.offsets ? r.offsets : at<int32_t>(workspace, L.offsets);
+    int32_t *dst_row = r.dst_row ? r.dst_row : at<int32_t>(workspace, L.dst_row);
+    int32_t *src_tok = r.src_tok ? r.src_tok : at<int32_t>(workspace, L.src_tok);
+    const RouteOut route = {counts, offsets, dst_row, src_tok, 0, nullptr, nullptr, nullptr, 0, 0, 0};
+    if (empty) return launch_route(idx, 0, c.E, c.k, route, at<int32_t>(workspace, L.block_hist), s);
+    {
+        ProfScope nothing("event_pair_overhead", s);
+    }
+    int split = 1;
+    SelectParams p = select_params(*select);
+    rc = run_gate_gemm(h, x, wg, gate_bias, T, logits, at<float>(workspace, L.gate_parts), s, &split, &p.part_stride);
+    if (rc != MOE_OK) return rc;
+    p.logits = logits;
+    p.stride = c.E;
+    p.bias = select_bias;
+    p.T = T;
+    p.idx = idx;
+    p.w = w;
+    p.n_parts = split - 1;
+    p.parts = at<float>(workspace, L.gate_parts);
+    p.sum_out = logits;
+    {
+        ProfScope ps("select", s);
+        rc = launch_select(p, MOE_DTYPE_F32, s);
+    }
+    if (rc != MOE_OK) return rc;
+    rc = launch_route(idx, T, c.E, c.k, route, at<int32_t>(workspace, L.block_hist), s);
+    if (rc != MOE_OK) return rc;
+    void *yp = at<void>(workspace, L.yp);
+    rc = run_expert_ffn_b128(h, x, T, src_tok, offsets, w1_q, w2_q, w1_scale, w2_scale, activation, T * c.k, yp, workspace, s);
+    if (rc != MOE_OK) return rc;
+    return launch_combine(c.dtype, yp, dst_row, w, T, c.D, c.k, y, s);
 }
 
 // ---- expert buffering ------------------------------------------------------------------------
