@@ -6,6 +6,8 @@ namespace moe355 {
 
 namespace {
 
+constexpr int kMostColumns = 1 << 24;  // 16 rows of them have 32-bit offsets
+
 bool bad_ptr(const void *p, const char *name, int align, bool nullable = false)
 {
     if (!p && nullable) return false;
@@ -115,7 +117,7 @@ int moe_quantize_b128(const void *x, int32_t dtype, int64_t row_stride, int32_t 
     set_error("%s", "");
     if (dtype != MOE_DTYPE_F32 && dtype != MOE_DTYPE_BF16) return unsupported("dtype", dtype);
     if (block_rows != 1 && block_rows != kBlock) return unsupported("block_rows", block_rows);
-    if (cols < 16 || cols % 16 != 0) return unsupported("cols", cols);
+    if (cols < 16 || cols % 16 != 0 || cols > kMostColumns) return unsupported("cols", cols);
     if (matrices < 0 || rows < 0) {
         set_error("matrices = %d, rows = %d: 0 or more", matrices, rows);
         return MOE_ERR_INVALID_ARG;
@@ -139,8 +141,8 @@ int moe_gemm_b128(const void *a_q, const void *a_scale, int32_t a_count, const i
         set_error("E = %d outside [1, %d], or more than one expert without offsets", E, MOE_MAX_E);
         return MOE_ERR_INVALID_ARG;
     }
-    if (N < 8 || N % 8 != 0) return unsupported("N", N);
-    if (K < 16 || K % 16 != 0) return unsupported("K", K);
+    if (N < 8 || N % 8 != 0 || N > kMostColumns) return unsupported("N", N);
+    if (K < 16 || K % 16 != 0 || K > kMostColumns) return unsupported("K", K);
     if (n_rows < 0 || n_rows > 0x3fffffff || a_count < 0 || (!a_rows && a_count < n_rows) || (n_rows > 0 && a_count == 0)) {
         set_error("n_rows = %d, a_count = %d: rows in [0, 2^30), each of them a row of a_q", n_rows, a_count);
         return MOE_ERR_INVALID_ARG;

@@ -2,6 +2,7 @@
 #pragma once
 
 #include "b128_internal.h"
+#include "gemm_bf16_dev.h"
 
 namespace moe355 {
 
@@ -13,19 +14,154 @@ __device__ __forceinline__ int b128_scale_byte(uint32_t largest_bits)
     const int n = (int)(largest_bits >> 23) - 8 + ((largest_bits & 0x7fffffu) > 0x600000u);
     return n < 1 ? 1 : n;
 }
-// 1 / scale: 2^(127 - byte), for bytes of 1 to 253 (a finite number's byte is at most 247)
-__device__ __forceinline__ float b128_inverse(int byte) { return __uint_as_float((uint32_t)(254 - byte) << 23); }
+__device__ __forceinline__ float scale_value(int byte) { return __uint_as_float((uint32_t)byte << 23); }  // bytes of 1 to 254
 
-__device__ __forceinline__ uint32_t finite_bits(float x)
+// N consecutive elements of a row, as they are stored.  The scaled conversions divide by the scale and round to nearest even once, as a
+// multiplication by its inverse and the plain conversion do (compared on all bf16 numbers and 7e8 fp32 ones), and turn NaN into NaN.
+template <bool BF16, int N> struct Elements;
+typedef __attribute__((ext_vector_type(2))) short i16x2_b128;
+typedef __attribute__((ext_vector_type(2))) unsigned short u16x2_b128;
+template <int N> struct Elements<true, N> {
+    uint32_t x[N / 2];
+    __device__ __forceinline__ void zero()
+    {
+#pragma unroll
+        for (int i = 0; i < N / 2; ++i) x[i] = 0;
+    }
+    // elements at .. at + 7, a load of 16 bytes; i: in the row
+    __device__ __forceinline__ void load8(const void *row, int64_t i, int at)
+    {
+        const uint4 r = *reinterpret_cast<const uint4 *>(static_cast<const uint16_t *>(row) + i);
+        x[at / 2] = r.x, x[at / 2 + 1] = r.y, x[at / 2 + 2] = r.z, x[at / 2 + 3] = r.w;
+    }
+    // bits of the largest absolute value as fp32; those of infinity or more if an element is not finite
+    __device__ __forceinline__ uint32_t largest() const
+    {
+        u16x2_b128 m = {0, 0};
+#pragma unroll
+        for (int i = 0; i < N / 2; ++i) m = __builtin_elementwise_max(m, __builtin_bit_cast(u16x2_b128, x[i] & 0x7fff7fffu));
+        return (uint32_t)(m[0] > m[1] ? m[0] : m[1]) << 16;
+    }
+    // the rare way: infinities become NaN, -> bits of the largest finite one
+    __device__ __forceinline__ uint32_t largest_finite()
+    {
+        uint32_t m = 0;
+#pragma unroll
+        for (int i = 0; i < N / 2; ++i) {
+            const uint32_t lo = x[i] & 0x7fffu, hi = x[i] >> 16 & 0x7fffu;
+            if (lo >= 0x7f80u) x[i] = (x[i] & 0xffff0000u) | 0x7fc0u;
+            else m = max(m, lo);
+            if (hi >= 0x7f80u) x[i] = (x[i] & 0xffffu) | 0x7fc00000u;
+            else m = max(m, hi);
+        }
+        return m << 16;
+    }
+    // four of them over the scale, as e4m3
+    __device__ __forceinline__ uint32_t pack4(int at, float scale) const
+    {
+        i16x2_b128 w = {0, 0};
+        w = __builtin_amdgcn_cvt_scalef32_pk_fp8_bf16(w, __builtin_bit_cast(bf16x2, x[at / 2]), scale, false);
+        w = __builtin_amdgcn_cvt_scalef32_pk_fp8_bf16(w, __builtin_bit_cast(bf16x2, x[at / 2 + 1]), scale, true);
+        return __builtin_bit_cast(uint32_t, w);
+    }
+};
+template <int N> struct Elements<false, N> {
+    float x[N];
+    __device__ __forceinline__ void zero()
+    {
+#pragma unroll
+        for (int i = 0; i < N; ++i) x[i] = 0.f;
+    }
+    __device__ __forceinline__ void load8(const void *row, int64_t i, int at)
+    {
+        const float4 a = *reinterpret_cast<const float4 *>(static_cast<const float *>(row) + i);
+        const float4 b = *reinterpret_cast<const float4 *>(static_cast<const float *>(row) + i + 4);
+        x[at] = a.x, x[at + 1] = a.y, x[at + 2] = a.z, x[at + 3] = a.w, x[at + 4] = b.x, x[at + 5] = b.y, x[at + 6] = b.z, x[at + 7] = b.w;
+    }
+    __device__ __forceinline__ uint32_t largest() const
+    {
+        float m = 0.f;  // fmaxf leaves NaN out, which the conversion then finds by itself
+#pragma unroll
+        for (int i = 0; i < N; ++i) m = fmaxf(m, fabsf(x[i]));
+        return __float_as_uint(m);
+    }
+    __device__ __forceinline__ uint32_t largest_finite()
+    {
+        uint32_t m = 0;
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            const uint32_t b = __float_as_uint(x[i]) & 0x7fffffffu;
+            if (b >= 0x7f800000u) x[i] = __uint_as_float(0x7fc00000u);
+            else m = max(m, b);
+        }
+        return m;
+    }
+    __device__ __forceinline__ uint32_t pack4(int at, float scale) const
+    {
+        i16x2_b128 w = {0, 0};
+        w = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(w, x[at], x[at + 1], scale, false);
+        w = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(w, x[at + 2], x[at + 3], scale, true);
+        return __builtin_bit_cast(uint32_t, w);
+    }
+};
+// Scale byte of the block whose elements lie in the lanes that `join` finds the maximum over (the same for all of them).
+template <typename Elem, typename Join>
+__device__ __forceinline__ int b128_block_byte(Elem &e, const Join &join)
 {
-    const uint32_t b = __float_as_uint(x) & 0x7fffffffu;
-    return b < 0x7f800000u ? b : 0;
+    uint32_t most = join(e.largest());
+    if (most >= 0x7f800000u) most = join(e.largest_finite());
+    return b128_scale_byte(most);
 }
-// Four numbers of at most 448, NaN or infinity to e4m3 to nearest even; the latter two to NaN.
-__device__ __forceinline__ uint32_t pack_e4m3(float a, float b, float c, float d)
+__device__ __forceinline__ uint32_t lanes_max(uint32_t m, int off) { return max(m, (uint32_t)__shfl_xor((int)m, off, 64)); }
+
+// ---- operands of the matrix instructions: a lane's 32 bytes of a block of a row, 16 at k and 16 at k + 64
+typedef __attribute__((ext_vector_type(8))) int Fragment;
+typedef __attribute__((ext_vector_type(4))) uint32_t u32x4;
+
+// k: a multiple of 16, as K is
+__device__ __forceinline__ Fragment load_fragment(const uint8_t *row, int k, int K, bool live)
 {
-    int word = __builtin_amdgcn_cvt_pk_fp8_f32(a, b, 0, false);
-    return (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(c, d, word, true);
+    uint4 lo = make_uint4(0, 0, 0, 0), hi = lo;
+    if (live && k < K) lo = *reinterpret_cast<const uint4 *>(row + k);
+    if (live && k + 64 < K) hi = *reinterpret_cast<const uint4 *>(row + k + 64);
+    return Fragment{(int)lo.x, (int)lo.y, (int)lo.z, (int)lo.w, (int)hi.x, (int)hi.y, (int)hi.z, (int)hi.w};
 }
+
+// The same of a row of bf16 or fp32 that is quantised here; lanes l, l ^ 16, l ^ 32 and l ^ 48 hold one block of a row.
+template <bool BF16>
+__device__ __forceinline__ void load_elements(Elements<BF16, 32> &e, const uint8_t *row, int k, int K, bool live)
+{
+    e.zero();
+#pragma unroll
+    for (int h = 0; h < 2; ++h)
+        if (live && k + 64 * h < K) {
+            e.load8(row, k + 64 * h, 16 * h);
+            e.load8(row, k + 64 * h + 8, 16 * h + 8);
+        }
+}
+template <bool BF16>
+__device__ __forceinline__ Fragment quantize_fragment(Elements<BF16, 32> &e, int &byte)
+{
+    byte = b128_block_byte(e, [](uint32_t m) { return lanes_max(lanes_max(m, 16), 32); });
+    const float scale = scale_value(byte);
+    Fragment f;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) f[j] = (int)e.pack4(4 * j, scale);
+    return f;
+}
+
+// Eight of them as bf16, times a power of two: exact, as bf16 has four more bits.
+__device__ __forceinline__ bf16x8 widen(const Fragment &f, int q, float scale)
+{
+    u32x4 w;
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        w[2 * i] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(f[2 * q + i], scale, false));
+        w[2 * i + 1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(f[2 * q + i], scale, true));
+    }
+    return __builtin_bit_cast(bf16x8, w);
+}
+__device__ __forceinline__ float silu(float g) { return g / (1.f + expf(-g)); }
+__device__ __forceinline__ float relu(float g) { return g > 0.f ? g : g != g ? g : 0.f; }
 
 }  // namespace moe355

@@ -35,23 +35,32 @@ SelectParams select_params(const moe_select_config_t &c);
 // ---- quantisation (quant_b128.hip)
 int launch_quantize_b128(const void *x, int dtype, int64_t stride, int64_t matrices, int rows, int cols, int block_rows, uint8_t *q, uint8_t *scale,
                          hipStream_t s);
-// h = act(gu) and its quantised rows: gu fp32 [rows, gated ? 2 : 1, F]; rows from offsets[0] to offsets[E] (NULL: all n_rows)
-int launch_act_quantize(const float *gu, int gated, int n_rows, int F, const int32_t *offsets, int E, uint8_t *q, uint8_t *scale, hipStream_t s);
-
-// ---- products (gemm_b128.hip)
+// ---- products
+enum { kRowsE4m3, kRowsBf16, kRowsF32 };    // what A is: bytes and scales, or rows that are quantised on the way (few rows only)
+enum { kActNone, kActRelu, kActSilu };      // of the results; silu: of the first matrix's, times the second's
 struct GemmB128 {
+    int rows, act;
     const uint8_t *a, *a_scale;  // [a_count, K], [a_count, scale columns]
     int a_count;
-    const int32_t *a_rows;  // row r of the product is row a_rows[r] of a (NULL: r)
-    const uint8_t *w, *w_scale;  // [E, N, K], [E, ceil(N / 128), scale columns]
-    const int32_t *offsets;  // [E + 1] or NULL: one expert with all rows
+    const int32_t *a_rows;       // row r of the product is row a_rows[r] of a (NULL: r)
+    const uint8_t *w, *w_scale;  // [E, N, K], [E, N / Nh, ceil(Nh / 128), scale columns]
+    const int32_t *offsets;      // [E + 1] or NULL: one expert with all rows
     int E, n_rows, N, K;
     int Nh;  // weight rows of a matrix: an expert has N / Nh of them one after the other, each with scales of its own
-    void *c;
+    void *c;  // [n_rows, N], with an activation [n_rows, Nh]; tiles with an activation: bytes, with
+    uint8_t *c_scale;  // [n_rows, scale columns of Nh]
     int c_dtype;
-    bool precise;  // sums in fp32 throughout: see gemm_b128.hip
+    bool precise;  // sums in fp32 throughout (gemm_b128_tile.hip)
     const char *name;  // of the launch for the event profiler
 };
-int launch_gemm_b128(const GemmB128 &g, hipStream_t s);
+// few rows an expert, and what the tiles cannot address (gemm_b128_stream.hip)
+constexpr int kStreamRows = 32;  // rows that are multiplied with one reading of the weights
+bool b128_few_rows(int n_rows, int E);
+int64_t b128_few_rows_most(int E);  // rows that are few, at most
+int launch_gemm_b128_stream(const GemmB128 &g, hipStream_t s);
+// many (gemm_b128_tile.hip)
+bool b128_tiles_ok(const GemmB128 &g);
+int launch_gemm_b128_tile(const GemmB128 &g, hipStream_t s);
+int launch_gemm_b128(const GemmB128 &g, hipStream_t s);  // the one or the other, of operands in e4m3
 
 }  // namespace moe355

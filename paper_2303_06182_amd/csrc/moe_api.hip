@@ -1062,8 +1062,22 @@ int moe_layer_forward_w4(moe_handle_t *h, const void *x, const void *wg, const f
 
 // ---- experts in e4m3 with a scale per block of 128 ------------------------------------------------
 struct B128Layout {
-    int64_t logits, topk_idx, topk_w, counts, offsets, dst_row, src_tok, block_hist, gate_parts, xq, xs, gu, hq, hs, yp, total;
+    int64_t logits, topk_idx, topk_w, counts, offsets, dst_row, src_tok, block_hist, gate_parts, xq, xs, h, hq, hs, yp, total;
 };
+
+// Whether both products of a call of many rows run in tiles, for any number of rows up to T_max * k.
+static bool b128_experts_in_tiles(const moe_config_t &c)
+{
+    GemmB128 g = {};
+    g.E = c.E;
+    g.a_count = g.n_rows = c.T_max * c.k;
+    g.N = 2 * c.F;
+    g.K = c.D;
+    GemmB128 second = g;
+    second.N = c.D;
+    second.K = c.F;
+    return b128_tiles_ok(g) && b128_tiles_ok(second);
+}
 
 static B128Layout b128_layout(const moe_config_t &c)
 {
@@ -1086,9 +1100,12 @@ static B128Layout b128_layout(const moe_config_t &c)
     L.gate_parts = take((int64_t)(kGateSplitMax - 1) * (T < kGateSplitTokens ? T : kGateSplitTokens) * E * 4);
     L.xq = take(N * c.D);  // of as many rows as the first product has: they may come without src_tok
     L.xs = take(N * b128_scale_cols(c.D));
-    L.gu = take(N * 2 * c.F * 4);
-    L.hq = take(N * c.F);
-    L.hs = take(N * b128_scale_cols(c.F));
+    // hidden rows: of few rows in fp32, of many as bytes and scales, of one kind in a call
+    L.hq = off;
+    const int64_t bytes = align_up(N * c.F, 256);
+    L.hs = off + bytes;
+    const int64_t as_tiles = bytes + N * b128_scale_cols(c.F), most = b128_few_rows_most(c.E), as_rows = (b128_experts_in_tiles(c) && most < N ? most : N) * c.F * 4;
+    L.h = take(as_tiles > as_rows ? as_tiles : as_rows);
     L.yp = take(N * c.D * es);
     L.total = off;
     return L;
@@ -1126,6 +1143,43 @@ static int run_expert_ffn_b128(moe_handle_t *h, const void *x, int32_t x_rows, c
     const moe_config_t &c = h->cfg;
     const B128Layout L = b128_layout(c);
     const bool gated = activation == MOE_ACT_SILU;
+    GemmB128 g = {};
+    g.offsets = offsets;
+    g.E = c.E;
+    g.n_rows = n_rows;
+    g.a_count = x_rows;
+    g.a_rows = src_tok;
+    g.w = static_cast<const uint8_t *>(w1_q);
+    g.w_scale = static_cast<const uint8_t *>(w1_scale);
+    g.N = gated ? 2 * c.F : c.F;
+    g.Nh = c.F;
+    g.K = c.D;
+    g.act = gated ? kActSilu : kActRelu;
+    g.precise = true;
+    g.name = "expert_gemm1";
+    GemmB128 g2 = g;
+    g2.a_count = n_rows;
+    g2.a_rows = nullptr;
+    g2.w = static_cast<const uint8_t *>(w2_q);
+    g2.w_scale = static_cast<const uint8_t *>(w2_scale);
+    g2.N = g2.Nh = c.D;
+    g2.K = c.F;
+    g2.act = kActNone;
+    g2.c = yp;
+    g2.c_dtype = c.dtype;
+    g2.precise = c.dtype == MOE_DTYPE_F32;
+    g2.name = "expert_gemm2";
+    if (b128_few_rows(n_rows, c.E) || !b128_experts_in_tiles(c)) {  // both products quantise their rows themselves
+        g.rows = c.dtype == MOE_DTYPE_F32 ? kRowsF32 : kRowsBf16;
+        g.a = static_cast<const uint8_t *>(x);
+        g.c = at<void>(workspace, L.h);
+        g.c_dtype = MOE_DTYPE_F32;
+        const int rc = launch_gemm_b128_stream(g, s);
+        if (rc != MOE_OK) return rc;
+        g2.rows = kRowsF32;
+        g2.a = at<uint8_t>(workspace, L.h);
+        return launch_gemm_b128_stream(g2, s);
+    }
     uint8_t *xq = at<uint8_t>(workspace, L.xq), *xs = at<uint8_t>(workspace, L.xs);
     int rc;
     {
@@ -1133,40 +1187,15 @@ static int run_expert_ffn_b128(moe_handle_t *h, const void *x, int32_t x_rows, c
         rc = launch_quantize_b128(x, c.dtype, c.D, 1, x_rows, c.D, 1, xq, xs, s);
     }
     if (rc != MOE_OK) return rc;
-    GemmB128 g = {};
     g.a = xq;
     g.a_scale = xs;
-    g.a_count = x_rows;
-    g.a_rows = src_tok;
-    g.w = static_cast<const uint8_t *>(w1_q);
-    g.w_scale = static_cast<const uint8_t *>(w1_scale);
-    g.offsets = offsets;
-    g.E = c.E;
-    g.n_rows = n_rows;
-    g.N = gated ? 2 * c.F : c.F;
-    g.Nh = c.F;
-    g.K = c.D;
-    g.c = at<void>(workspace, L.gu);
-    g.c_dtype = MOE_DTYPE_F32;
-    g.precise = c.dtype == MOE_DTYPE_F32;
-    g.name = "expert_gemm1";
-    rc = launch_gemm_b128(g, s);
+    g.c = at<void>(workspace, L.hq);
+    g.c_scale = at<uint8_t>(workspace, L.hs);
+    rc = launch_gemm_b128_tile(g, s);
     if (rc != MOE_OK) return rc;
-    uint8_t *hq = at<uint8_t>(workspace, L.hq), *hs = at<uint8_t>(workspace, L.hs);
-    rc = launch_act_quantize(at<float>(workspace, L.gu), gated, n_rows, c.F, offsets, c.E, hq, hs, s);
-    if (rc != MOE_OK) return rc;
-    g.a = hq;
-    g.a_scale = hs;
-    g.a_count = n_rows;
-    g.a_rows = nullptr;
-    g.w = static_cast<const uint8_t *>(w2_q);
-    g.w_scale = static_cast<const uint8_t *>(w2_scale);
-    g.N = g.Nh = c.D;
-    g.K = c.F;
-    g.c = yp;
-    g.c_dtype = c.dtype;
-    g.name = "expert_gemm2";
-    return launch_gemm_b128(g, s);
+    g2.a = at<uint8_t>(workspace, L.hq);
+    g2.a_scale = at<uint8_t>(workspace, L.hs);
+    return launch_gemm_b128_tile(g2, s);
 }
 
 int64_t moe_b128_workspace_bytes(const moe_handle_t *h)
