@@ -90,6 +90,41 @@ def test_select_infinities_and_nan(score):
             check_select(t, 8, bias=b, score=score, **kw)
 
 
+@pytest.mark.parametrize("E,G,kept,k,top", [(1, 1, 1, 1, 1), (5, 1, 1, 2, 1), (16, 4, 2, 2, 2), (64, 8, 8, 6, 1), (100, 10, 3, 8, 2), (128, 8, 3, 6, 2), (128, 1, 1, 8, 1), (130, 13, 4, 3, 1),
+                                                (256, 64, 9, 8, 2), (257, 1, 1, 4, 1), (512, 16, 5, 8, 2), (1024, 64, 64, 8, 1), (1023, 1, 1, 1, 1)])
+@pytest.mark.parametrize("score", ["sigmoid", "softmax"])
+def test_select_many_tokens(E, G, kept, k, top, score):
+    """Batches of thousands of tokens: as the same rows in small batches, which the tests above hold against the oracle; rows with ties, infinities, NaN, numbers
+    far apart and a last, partly filled group of rows among them."""
+    g = torch.Generator(device=DEV).manual_seed(E + k)
+    T = 6157
+    x = torch.randn((T, E), device=DEV, generator=g) * 1.5
+    x[::7] = x[::7].bfloat16().float()                 # equal logits here and there
+    x[3::11] = (x[3::11] * 2).round() / 2              # and in most places
+    x[5::13] *= 40.0
+    x[6::17] = x[6::17].masked_fill(torch.rand((len(range(6, T, 17)), E), device=DEV, generator=g) < 0.6, -math.inf)
+    x[100], x[101], x[102], x[103], x[104] = 0.0, -math.inf, math.nan, 1e30, math.inf
+    x[105, ::2], x[106, ::3], x[107, 0] = math.nan, math.inf, math.inf
+    x[108:140] = x[108:109]
+    bias = torch.randn(E, device=DEV, generator=g) * 0.1
+    odd = bias.clone()
+    odd[::5] = -math.inf
+    if E > 3:
+        odd[1], odd[3] = math.inf, math.nan
+    kw = dict(score=score, n_groups=G, groups_kept=kept, group_top=top)
+    for b in (None, bias, bias * 1e6, odd):
+        for renormalize in (True, False):
+            for logits in (x, x.bfloat16(), torch.cat([x, x], 1)[:, 1:E + 1]):
+                idx, w = binding.moe_select_experts(logits, k, bias=b, renormalize=renormalize, **kw)
+                parts = [binding.moe_select_experts(logits[i:i + 2053], k, bias=b, renormalize=renormalize, **kw) for i in range(0, T, 2053)]
+                assert torch.equal(idx, torch.cat([i for i, _ in parts]))
+                # sums of 64 bits in another order: the weights are the same but where they lie within 2^-45 of a border between two fp32 numbers
+                other = torch.cat([v for _, v in parts])
+                assert torch.allclose(w, other, rtol=2.0 ** -23, atol=0.0) and (w != other).sum() <= 4
+    if E <= 16:  # and the oracle itself
+        check_select(x[:160].repeat(40, 1), k, bias=host(bias), **kw)
+
+
 def test_select_many_tokens_twice_and_captured():
     """More rows than the launch has waves; the same again, and from a graph, into the same tensors."""
     g = torch.Generator(device=DEV).manual_seed(1)
