@@ -118,36 +118,13 @@ __device__ __forceinline__ uint32_t lanes_max(uint32_t m, int off) { return max(
 typedef __attribute__((ext_vector_type(8))) int Fragment;
 typedef __attribute__((ext_vector_type(4))) uint32_t u32x4;
 
-// k: a multiple of 16, as K is
-__device__ __forceinline__ Fragment load_fragment(const uint8_t *row, int k, int K, bool live)
+// at: where the lane's bytes are; k and K, multiples of 16: zeros from K on
+__device__ __forceinline__ Fragment load_fragment(const uint8_t *at, int k, int K)
 {
     uint4 lo = make_uint4(0, 0, 0, 0), hi = lo;
-    if (live && k < K) lo = *reinterpret_cast<const uint4 *>(row + k);
-    if (live && k + 64 < K) hi = *reinterpret_cast<const uint4 *>(row + k + 64);
+    if (k < K) lo = *reinterpret_cast<const uint4 *>(at);
+    if (k + 64 < K) hi = *reinterpret_cast<const uint4 *>(at + 64);
     return Fragment{(int)lo.x, (int)lo.y, (int)lo.z, (int)lo.w, (int)hi.x, (int)hi.y, (int)hi.z, (int)hi.w};
-}
-
-// The same of a row of bf16 or fp32 that is quantised here; lanes l, l ^ 16, l ^ 32 and l ^ 48 hold one block of a row.
-template <bool BF16>
-__device__ __forceinline__ void load_elements(Elements<BF16, 32> &e, const uint8_t *row, int k, int K, bool live)
-{
-    e.zero();
-#pragma unroll
-    for (int h = 0; h < 2; ++h)
-        if (live && k + 64 * h < K) {
-            e.load8(row, k + 64 * h, 16 * h);
-            e.load8(row, k + 64 * h + 8, 16 * h + 8);
-        }
-}
-template <bool BF16>
-__device__ __forceinline__ Fragment quantize_fragment(Elements<BF16, 32> &e, int &byte)
-{
-    byte = b128_block_byte(e, [](uint32_t m) { return lanes_max(lanes_max(m, 16), 32); });
-    const float scale = scale_value(byte);
-    Fragment f;
-#pragma unroll
-    for (int j = 0; j < 8; ++j) f[j] = (int)e.pack4(4 * j, scale);
-    return f;
 }
 
 // Eight of them as bf16, times a power of two: exact, as bf16 has four more bits.
@@ -161,7 +138,41 @@ __device__ __forceinline__ bf16x8 widen(const Fragment &f, int q, float scale)
     }
     return __builtin_bit_cast(bf16x8, w);
 }
-__device__ __forceinline__ float silu(float g) { return g / (1.f + expf(-g)); }
+// g / (1 + exp(-g)) with the hardware's exponential and reciprocal: off by less than (|g| + 4) 2^-23 of it, as little as the sums that it is taken of.
+// Where the exponential passes fp32 the result is -0.
+__device__ __forceinline__ float silu(float g) { return g * __builtin_amdgcn_rcpf(1.f + __expf(-g)); }
 __device__ __forceinline__ float relu(float g) { return g > 0.f ? g : g != g ? g : 0.f; }
+
+// ---- the expert of a block and its rows
+struct ExpertRows {
+    int expert, first, end;
+};
+// The expert that a grid's row y is for: y itself, or, where the grid has fewer rows than there are experts (there are fewer rows of A then), the y-th that
+// has rows.  expert -1: there is none.
+__device__ __forceinline__ ExpertRows expert_rows(const GemmB128 &g, int y, int grid_rows)
+{
+    if (!g.offsets) return {0, 0, g.n_rows};
+    if (grid_rows == g.E) {
+        const int first = min(max(g.offsets[y], 0), g.n_rows);
+        return {y, first, min(max(g.offsets[y + 1], first), g.n_rows)};
+    }
+    const int lane = threadIdx.x & 63;
+    for (int base = 0; base < g.E; base += 64) {
+        int first = 0, end = 0;
+        if (base + lane < g.E) {
+            first = min(max(g.offsets[base + lane], 0), g.n_rows);
+            end = min(max(g.offsets[base + lane + 1], first), g.n_rows);
+        }
+        unsigned long long some = __ballot(end > first);
+        const int n = __popcll(some);
+        if (y < n) {
+            for (; y > 0; --y) some &= some - 1;
+            const int src = __builtin_ctzll(some);
+            return {base + src, __builtin_amdgcn_readlane(first, src), __builtin_amdgcn_readlane(end, src)};
+        }
+        y -= n;
+    }
+    return {-1, 0, 0};
+}
 
 }  // namespace moe355

@@ -53,14 +53,16 @@ struct GemmB128 {
     bool precise;  // sums in fp32 throughout (gemm_b128_tile.hip)
     const char *name;  // of the launch for the event profiler
 };
-// few rows an expert, and what the tiles cannot address (gemm_b128_stream.hip)
-constexpr int kStreamRows = 32;  // rows that are multiplied with one reading of the weights
+// few rows an expert, which it quantises itself (gemm_b128_stream.hip)
 bool b128_few_rows(int n_rows, int E);
 int64_t b128_few_rows_most(int E);  // rows that are few, at most
 int launch_gemm_b128_stream(const GemmB128 &g, hipStream_t s);
-// many (gemm_b128_tile.hip)
+// many (gemm_b128_tile.hip).  kTileTime: what a K tile of a tile of 64, 128, 192 or 256 rows takes, fast and precise, in units of 50 ns
+constexpr int kTileTime[2][4] = {{16, 16, 22, 28}, {22, 35, 46, 56}};
 bool b128_tiles_ok(const GemmB128 &g);
 int launch_gemm_b128_tile(const GemmB128 &g, hipStream_t s);
+// few output tiles, and what the tiles cannot address, without an activation (gemm_b128_small.hip)
+int launch_gemm_b128_small(const GemmB128 &g, hipStream_t s);
 int launch_gemm_b128(const GemmB128 &g, hipStream_t s);  // the one or the other, of operands in e4m3
 
 }  // namespace moe355

@@ -42,6 +42,7 @@ typedef __attribute__((ext_vector_type(16))) float f32x16_t;
 constexpr int BM = 256, BN = 256, WN = 4, NWAVE = 8, kThreads = NWAVE * 64;
 constexpr int SLOT = (BM + BN) * 64;
 constexpr int MI = 4, NI = 2;     // 32-row blocks of a wave, at most, and blocks of 32 weight rows
+constexpr int kFewItems = 1024;  // output tiles that are dealt to the XCDs by number
 constexpr int GROUP_M = 4;        // row tiles that are walked across all columns together
 constexpr uint32_t kNowhere = 0xfc000000u;  // byte offset past the end of every operand, also with a K tile's offset added
 
@@ -108,6 +109,7 @@ __global__ __launch_bounds__(kThreads, 1) void gemm_b128_tile_kernel(GemmB128 g)
     // ---- the block's tiles.  Experts, 64 at a time, one per lane: rows, tiles along them, output tiles before it.
     int w_base = 0, w_pos = 0, w_total = 0;
     int w_row0, w_row_end, w_cuts, w_excl;
+    int cap = 4;  // height of a tile, in units of 64 rows
     auto load_window = [&]() __attribute__((always_inline)) {
         w_row0 = 0, w_row_end = 0;
         const int e = w_base + lane;
@@ -119,7 +121,7 @@ __global__ __launch_bounds__(kThreads, 1) void gemm_b128_tile_kernel(GemmB128 g)
             }
         }
         const int units = (w_row_end - w_row0 + 63) >> 6;  // of 64 rows
-        w_cuts = (units + 3) >> 2;
+        w_cuts = cap == 4 ? (units + 3) >> 2 : cap == 3 ? (units + 2) / 3 : cap == 2 ? (units + 1) >> 1 : units;
         int incl = w_cuts;
 #pragma unroll
         for (int off = 1; off < 64; off <<= 1) {
@@ -129,6 +131,28 @@ __global__ __launch_bounds__(kThreads, 1) void gemm_b128_tile_kernel(GemmB128 g)
         w_excl = (incl - w_cuts) * n_tiles;
         w_total = __builtin_amdgcn_readlane(incl, 63) * n_tiles;
     };
+    // The height at which the rounds of all blocks take least: a round costs a K loop, whose K tiles take about so many units by a tile's height,
+    // and as much as six K tiles of the least for its beginning and end.
+    if (g.n_rows > 64) {
+        int tiles[4] = {0, 0, 0, 0};
+        for (w_base = 0; w_base < g.E; w_base += 64) {
+            load_window();
+            const int units = (w_row_end - w_row0 + 63) >> 6;
+#pragma unroll
+            for (int h = 1; h <= 4; ++h) tiles[h - 1] += (units + h - 1) / h;
+        }
+        float best = 0.f;
+#pragma unroll
+        for (int h = 4; h >= (PRECISE ? 1 : 2); --h) {
+            int n = tiles[h - 1];
+#pragma unroll
+            for (int off = 32; off >= 1; off >>= 1) n += __shfl_xor(n, off, 64);
+            const float out = (float)n * (float)n_tiles, rounds = ceilf(out * (1.f / 256.f));
+            const float t = rounds * (float)((KT + 6) * kTileTime[PRECISE][h - 1]);
+            if (h == 4 || t < 0.97f * best) best = t, cap = h;
+        }
+        cap = __builtin_amdgcn_readfirstlane(cap);
+    }
     // What a window's expert costs, in units of 64 rows by a column tile: its rows, but half a full tile at least for the weights' stream, and as much
     // as three units for a tile's beginning and end.
     auto cost = [&]() __attribute__((always_inline)) -> float {
@@ -174,6 +198,12 @@ __global__ __launch_bounds__(kThreads, 1) void gemm_b128_tile_kernel(GemmB128 g)
         }
         lo = x == 0 ? 0 : lo < 0 ? items : lo;
         hi = x == 7 || hi < 0 ? items : hi;
+        if (items <= kFewItems) {
+            // few rounds: as many tiles for each XCD, or one of them has a round more (24 experts, 238 tiles: 46 us by cost, 25 by number)
+            const int share = (items + 7) >> 3;
+            lo = min(x * share, items);
+            hi = min(lo + share, items);
+        }
         pos = __builtin_amdgcn_readfirstlane(lo) + (blockIdx.x >> 3);
         pos_last = __builtin_amdgcn_readfirstlane(hi);
     }
@@ -637,7 +667,7 @@ static int launch_tile_as(const GemmB128 &g, hipStream_t s)
 bool b128_tiles_ok(const GemmB128 &g)
 {
     return g.K > kBlock && g.K <= 1 << 24 && g.N <= 1 << 20 && (int64_t)g.a_count * g.K <= (int64_t)kNowhere && (int64_t)g.N * g.K <= (int64_t)kNowhere &&
-           ((int64_t)g.n_rows / 256 + g.E) * ceil_div(g.N, 128) < 1 << 30;
+           ((int64_t)g.n_rows / 64 + g.E) * ceil_div(g.N, 128) < 1 << 30;
 }
 
 int launch_gemm_b128_tile(const GemmB128 &g, hipStream_t s)

@@ -1180,7 +1180,7 @@ static int run_expert_ffn_b128(moe_handle_t *h, const void *x, int32_t x_rows, c
         g2.a = at<uint8_t>(workspace, L.h);
         return launch_gemm_b128_stream(g2, s);
     }
-    uint8_t *xq = at<uint8_t>(workspace, L.xq), *xs = at<uint8_t>(workspace, L.xs);
+    uint8_t *xq = at<uint8_t>(workspace, L.xq), *xs = at<uint8_t>(workspace, L.xs), *hq = at<uint8_t>(workspace, L.hq), *hs = at<uint8_t>(workspace, L.hs);
     int rc;
     {
         ProfScope ps("quantize_rows", s);
@@ -1189,13 +1189,13 @@ static int run_expert_ffn_b128(moe_handle_t *h, const void *x, int32_t x_rows, c
     if (rc != MOE_OK) return rc;
     g.a = xq;
     g.a_scale = xs;
-    g.c = at<void>(workspace, L.hq);
-    g.c_scale = at<uint8_t>(workspace, L.hs);
+    g2.a = hq;
+    g2.a_scale = hs;
+    g.c = hq;
+    g.c_scale = hs;
     rc = launch_gemm_b128_tile(g, s);
     if (rc != MOE_OK) return rc;
-    g2.a = at<uint8_t>(workspace, L.hq);
-    g2.a_scale = at<uint8_t>(workspace, L.hs);
-    return launch_gemm_b128_tile(g2, s);
+    return launch_gemm_b128(g2, s);
 }
 
 int64_t moe_b128_workspace_bytes(const moe_handle_t *h)
