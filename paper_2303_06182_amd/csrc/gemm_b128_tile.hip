@@ -150,6 +150,7 @@ __global__ __launch_bounds__(kThreads, 1) void gemm_b128_tile_kernel(GemmB128 g)
             const float out = (float)n * (float)n_tiles, rounds = ceilf(out * (1.f / 256.f));
             const float t = rounds * (float)((KT + 6) * kTileTime[PRECISE][h - 1]);
             if (h == 4 || t < 0.97f * best) best = t, cap = h;
+            if (h == 4 && rounds > 3.f) break;  // blocks of several rounds even out by themselves
         }
         cap = __builtin_amdgcn_readfirstlane(cap);
     }

@@ -29,6 +29,8 @@ constexpr int kManyFrom = 6144;  // tokens, see above
 constexpr int kManyTokens = 16;  // of a wave of select_many_kernel
 // words from row to row there: four lanes of a token read four neighbours, and the rows of 16 tokens lie four banks apart
 __host__ __device__ constexpr int many_row(int E) { return (E + 59) / 64 * 64 + 4; }
+// words for keys or groups' sums
+__host__ __device__ inline int many_groups(const SelectParams &p) { return p.kept == p.groups ? 0 : 2 * p.E > p.groups * kManyTokens ? 2 * p.E : p.groups * kManyTokens; }
 typedef unsigned long long u64;
 
 // Keys as whole numbers in the same order; 0: no key.
@@ -47,7 +49,7 @@ __device__ __forceinline__ float logit(const void *row, int e)
 
 __device__ __forceinline__ double sigmoid(float l) { return 1. / (1. + exp(-(double)l)); }
 
-// One token by a wave.  l: logits of the lane's experts lane + 64 i, -infinity past the last; keys: room for V * 64 numbers, of this wave alone.
+// One token by a wave.  l: logits of the lane's experts lane + 64 i, -infinity past the last; keys: room for E numbers, of this wave alone.
 // All waves of a block come here together.
 template <int V>
 __device__ __forceinline__ void select_token(const SelectParams &p, const float (&l)[V], double *keys, int64_t t, bool live)
@@ -81,7 +83,7 @@ __device__ __forceinline__ void select_token(const SelectParams &p, const float 
         const double k = e < E && l[i] != -INFINITY ? s[i] + (p.bias ? (double)p.bias[e] : 0.) : -INFINITY;
         key[i] = ordered(k);
         if (key[i] == 0) s[i] = 0.;
-        if (p.kept < p.groups) keys[e] = key[i] ? k : -INFINITY;
+        if (p.kept < p.groups && e < E) keys[e] = key[i] ? k : -INFINITY;
     }
     u64 groups = ~0ull;
     if (p.kept < p.groups) {
@@ -221,9 +223,9 @@ __global__ __launch_bounds__(64) void select_many_kernel(SelectParams p)
     const int lane = threadIdx.x, r = lane / S, q = lane % S, E = p.E, size = E / p.groups;
     const int ld = many_row(E);
     float *const rows = smem;                                         // [R][ld]
-    double *const keys = reinterpret_cast<double *>(rows + R * ld);   // [64 V], for a token done again
-    float *const bias = reinterpret_cast<float *>(keys + 64 * V);     // [E]
-    float *const of_group = bias + 64 * V;                            // [G][R], only with groups
+    double *const keys = reinterpret_cast<double *>(rows + R * ld);   // [E], for a token done again, behind the use of
+    float *const of_group = rows + R * ld;                            // [G][R]; both only with groups
+    float *const bias = rows + R * ld + many_groups(p);               // [E]
     const bool grouped = p.kept < p.groups;
     const bool by_logit = !p.bias && !grouped;  // without a bias keys are ordered as logits are, where they differ at all
     const bool wide = E % (BF16 ? 8 : 4) == 0 && p.stride % (BF16 ? 8 : 4) == 0 && reinterpret_cast<uintptr_t>(p.logits) % 16 == 0;
@@ -433,6 +435,7 @@ __global__ __launch_bounds__(64) void select_many_kernel(SelectParams p)
                 }
         }
         u64 todo = __ballot(live && failed && q == 0);
+        __syncthreads();
         while (todo) {
             const int row = __builtin_ctzll(todo) / S;
             todo &= todo - 1;
@@ -447,7 +450,7 @@ __global__ __launch_bounds__(64) void select_many_kernel(SelectParams p)
 template <bool BF16, int V, int KL>
 int launch_many_as(const SelectParams &p, hipStream_t s)
 {
-    const size_t smem = kManyTokens * many_row(p.E) * 4 + 64 * V * 12 + (p.kept < p.groups ? p.groups * kManyTokens * 4 : 0);
+    const size_t smem = (kManyTokens * many_row(p.E) + many_groups(p) + p.E) * 4;
     auto kern = select_many_kernel<BF16, V, KL>;
     static std::once_flag once;  // per instantiation
     static hipError_t setup_rc = hipSuccess;
