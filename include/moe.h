@@ -531,7 +531,7 @@ typedef struct moe_select_config {
 int moe_select_experts(const moe_select_config_t *cfg, const void *logits, int32_t dtype, int64_t row_stride, const float *bias, int32_t T,
                        int32_t *topk_idx, float *topk_w, void *stream);
 
-/* e4m3 operands with a scale per block of 128.  A row of `cols` elements (cols a multiple of 16, the last block may be short) is cols
+/* e4m3 operands with a scale per block of 128.  A row of `cols` elements (cols a multiple of 16 up to 2^24, the last block may be short) is cols
  * bytes, OCP e4m3, row after row; the scale of block b is 2^(byte - 127) with byte b of the row's moe_b128_scale_cols(cols) scale bytes, that is
  * one for each block, in groups of four (those behind the last block hold 127).  Activations have such scales for every row, weights for every
  * 128 rows of a matrix.  Bytes are in 1 .. 254. */
@@ -549,7 +549,7 @@ int moe_quantize_b128(const void *x, int32_t dtype, int64_t row_stride, int32_t 
  * a_q [a_count, K] with a scale per row and block, a_rows [n_rows] int32 or NULL (row r is row r of a_q; indices are clamped to
  * [0, a_count)); w_q [E, N, K] with w_scale [E, ceil(N / 128), moe_b128_scale_cols(K)]; offsets [E + 1] int32 on the device, ascending and within
  * [0, n_rows] (clamped to that), or NULL with E = 1: all rows.  c [n_rows, N] of c_dtype; rows outside every expert's range are left as they are, and
- * an expert without rows is not read.  N a multiple of 8, K of 16, 1 <= E <= MOE_MAX_E, 0 <= n_rows < 2^30.
+ * an expert without rows is not read.  N a multiple of 8, K of 16, both up to 2^24, 1 <= E <= MOE_MAX_E, 0 <= n_rows < 2^30.
  * Sums are formed in fp32.  With c_dtype BF16 the matrix cores' 8-bit instruction forms them, which aligns the products of 8 neighbouring k to
  * the largest of them and drops what is less than about 2^-14 of that; it is off by 1.4e-5 of the results' standard deviation on
  * normally distributed operands (their rounding to bf16: 1.7e-3).  With F32 nothing is dropped, at half the rate.  A scaled element
@@ -565,8 +565,8 @@ int moe_gemm_b128(const void *a_q, const void *a_scale, int32_t a_count, const i
  *   MOE_ACT_SILU:  h = silu(g) * u, g = W1[e][0] x[src_tok[r]], u = W1[e][1] x[src_tok[r]],  w1_q [E, 2, F, D], scales [E, 2, ceil(F / 128), ..]
  *   yp[r] = W2[e] h',  h' = h quantised by rows,                                 w2_q [E, D, F]
  * src_tok [n_rows] int32 (as moe_route_counts writes it; clamped to [0, x_rows)) or NULL: row r of x.  Offsets as in moe_gemm_b128.  silu(g) = g / (1 +
- * exp(-g)); h in fp32, from the sums of the first product, and rounded to e4m3 only.  yp [n_rows, D] elem.  The handle's D and F are multiples of 16;
- * x_rows and n_rows at most k * T_max.  The handle's device has to be the current one.
+ * exp(-g)); h in fp32, from the sums of the first product, and rounded to e4m3 only.  yp [n_rows, D] elem.  The handle's D and F are multiples of 16, up to
+ * 2^23; n_rows at most k * T_max, and x_rows with src_tok at most T_max, without it k * T_max.  The handle's device has to be the current one.
  * Workspace: moe_b128_workspace_bytes(). */
 int64_t moe_b128_workspace_bytes(const moe_handle_t *h);
 int moe_expert_ffn_b128(moe_handle_t *h, const void *x, int32_t x_rows, const int32_t *src_tok, const int32_t *offsets, const void *w1_q,

@@ -118,13 +118,18 @@ __device__ __forceinline__ uint32_t lanes_max(uint32_t m, int off) { return max(
 typedef __attribute__((ext_vector_type(8))) int Fragment;
 typedef __attribute__((ext_vector_type(4))) uint32_t u32x4;
 
+__device__ __forceinline__ Fragment whole(const u32x4 &lo, const u32x4 &hi)
+{
+    return Fragment{(int)lo[0], (int)lo[1], (int)lo[2], (int)lo[3], (int)hi[0], (int)hi[1], (int)hi[2], (int)hi[3]};
+}
+
 // at: where the lane's bytes are; k and K, multiples of 16: zeros from K on
 __device__ __forceinline__ Fragment load_fragment(const uint8_t *at, int k, int K)
 {
-    uint4 lo = make_uint4(0, 0, 0, 0), hi = lo;
-    if (k < K) lo = *reinterpret_cast<const uint4 *>(at);
-    if (k + 64 < K) hi = *reinterpret_cast<const uint4 *>(at + 64);
-    return Fragment{(int)lo.x, (int)lo.y, (int)lo.z, (int)lo.w, (int)hi.x, (int)hi.y, (int)hi.z, (int)hi.w};
+    u32x4 lo = {0, 0, 0, 0}, hi = lo;
+    if (k < K) lo = *reinterpret_cast<const u32x4 *>(at);
+    if (k + 64 < K) hi = *reinterpret_cast<const u32x4 *>(at + 64);
+    return whole(lo, hi);
 }
 
 // Eight of them as bf16, times a power of two: exact, as bf16 has four more bits.

@@ -24,8 +24,6 @@ constexpr int NW = 8, kThreads = NW * 64;
 constexpr int P = 3;   // blocks of k on their way: with two waves of rows, what 128 registers hold
 constexpr int NC = 2;  // blocks of 16 weight rows
 
-typedef __attribute__((ext_vector_type(4))) int i32x4_b128;
-
 // k of A that LDS holds at once: 64 KB, so that a CU has room for two blocks
 constexpr int held_k(int mr) { return 4096 / mr; }
 constexpr int kRowPad = 16;  // bytes behind a row, which put 16 rows' chunks of 16 bytes on all banks
@@ -94,7 +92,7 @@ __device__ __forceinline__ void stream_rows(const GemmB128 &g, uint8_t *smem, in
             }
         };
         struct Raw {
-            i32x4_b128 w[NC][2];
+            u32x4 w[NC][2];
             int s[NC];
         } raw[P];
         auto load = [&](Raw &f) __attribute__((always_inline)) {
@@ -140,7 +138,7 @@ __device__ __forceinline__ void stream_rows(const GemmB128 &g, uint8_t *smem, in
                     for (int m = 0; m < MR; ++m) {
                         const uint8_t *row = st.a + (16 * m + r) * st.ld + at * kBlock + part * 16;
                         const u32x4 lo = *reinterpret_cast<const u32x4 *>(row), hi = *reinterpret_cast<const u32x4 *>(row + 64);
-                        af[m] = Fragment{(int)lo[0], (int)lo[1], (int)lo[2], (int)lo[3], (int)hi[0], (int)hi[1], (int)hi[2], (int)hi[3]};
+                        af[m] = whole(lo, hi);
                         as[m] = scale_value(st.as[at * 16 * MR + 16 * m + r]);
                     }
 #pragma unroll
@@ -150,8 +148,7 @@ __device__ __forceinline__ void stream_rows(const GemmB128 &g, uint8_t *smem, in
                         for (int m = 0; m < MR; ++m) aw[m] = widen(af[m], q, as[m]);
 #pragma unroll
                         for (int c = 0; c < NC; ++c) {
-                            const Fragment wf = {f.w[c][0][0], f.w[c][0][1], f.w[c][0][2], f.w[c][0][3], f.w[c][1][0], f.w[c][1][1], f.w[c][1][2], f.w[c][1][3]};
-                            const bf16x8 ww = widen(wf, q, scale_value(f.s[c]));
+                            const bf16x8 ww = widen(whole(f.w[c][0], f.w[c][1]), q, scale_value(f.s[c]));
 #pragma unroll
                             for (int m = 0; m < MR; ++m) acc[m][c] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ww, aw[m], acc[m][c], 0, 0, 0);
                         }

@@ -250,9 +250,6 @@ __global__ __launch_bounds__(kThreads, 1) void gemm_b128_tile_kernel(GemmB128 g)
     auto chunk_of = [&](const uint8_t *frag, int slot, int at, int far) __attribute__((always_inline)) {
         return *reinterpret_cast<const u32x4 *>(frag + slot * SLOT + at + (far ? frag_far : frag_off));
     };
-    auto whole = [&](const u32x4 &lo, const u32x4 &hi) __attribute__((always_inline)) {
-        return Fragment{(int)lo[0], (int)lo[1], (int)lo[2], (int)lo[3], (int)hi[0], (int)hi[1], (int)hi[2], (int)hi[3]};
-    };
     auto read_a = [&](int slot, int mi) __attribute__((always_inline)) { return whole(chunk_of(fragA, slot, mi * 4096, 0), chunk_of(fragA, slot, mi * 4096, 1)); };
     auto read_b = [&](int slot, int ni) __attribute__((always_inline)) { return whole(chunk_of(fragB, slot, ni * 2048, 0), chunk_of(fragB, slot, ni * 2048, 1)); };
 
@@ -261,19 +258,23 @@ __global__ __launch_bounds__(kThreads, 1) void gemm_b128_tile_kernel(GemmB128 g)
     int l_kt = 0;
     bool l_more = true;
     int w_slot = 0;  // slot of the first half of the K tile the stream is at
-    const __amdgpu_buffer_rsrc_t bufA = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t *>(g.a), 0, (int)kNowhere, 0x00020000);
-    const __amdgpu_buffer_rsrc_t bufAS = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t *>(g.a_scale), 0, (int)kNowhere, 0x00020000);
+    // A and its scales: all of them where rows are chosen by index, else from the tile's first row on
+    __amdgpu_buffer_rsrc_t bufA = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t *>(g.a), 0, (int)kNowhere, 0x00020000);
+    __amdgpu_buffer_rsrc_t bufAS = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t *>(g.a_scale), 0, (int)kNowhere, 0x00020000);
     __amdgpu_buffer_rsrc_t bufB = bufA, bufBS = bufAS;  // the expert's weights and their scales
     uint32_t a_voff[2], b_voff[2], as_voff[MI], bs_off[NI];
     const int ld_row = lane >> 2;                         // row inside a 16-row group
     const int ld_chunk = (lane & 3) ^ ((lane >> 4) & 3);  // chunk this lane fetches for its LDS position
-    auto row_of = [&](int r) __attribute__((always_inline)) -> int {  // of A, of row r of the stream's tile
-        int at = min(nx.row0 + r, nx.row_end - 1);
-        if (g.a_rows) at = min(max(g.a_rows[at], 0), g.a_count - 1);
-        return at;
+    auto row_of = [&](int r) __attribute__((always_inline)) -> int {  // of bufA, of row r of the stream's tile
+        const int in = min(r, nx.row_end - 1 - nx.row0);
+        return g.a_rows ? min(max(g.a_rows[nx.row0 + in], 0), g.a_count - 1) : in;
     };
     auto set_ptrs = [&]() __attribute__((always_inline)) {
         const int64_t mats = (int64_t)nx.expert * (g.N / g.Nh);
+        if (!g.a_rows) {
+            bufA = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t *>(g.a + (int64_t)nx.row0 * K), 0, (int)kNowhere, 0x00020000);
+            bufAS = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t *>(g.a_scale + (int64_t)nx.row0 * scale_cols), 0, (int)kNowhere, 0x00020000);
+        }
         bufB = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t *>(g.w + (int64_t)nx.expert * g.N * K), 0, (int)kNowhere, 0x00020000);
         bufBS = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t *>(g.w_scale + mats * n_blocks * scale_cols), 0, (int)kNowhere, 0x00020000);
 #pragma unroll
@@ -663,11 +664,11 @@ static int launch_tile_as(const GemmB128 &g, hipStream_t s)
     return MOE_OK;
 }
 
-// The kernel addresses A, its scales, and an expert's weights with 32-bit byte offsets, counts output tiles in 32 bits, and its load stream is
-// two K tiles ahead.
+// The kernel addresses an expert's weights, a tile's rows of A, and all of A where rows are chosen by index, with 32-bit byte offsets, counts output tiles in
+// 32 bits, and its load stream is two K tiles ahead.
 bool b128_tiles_ok(const GemmB128 &g)
 {
-    return g.K > kBlock && g.K <= 1 << 24 && g.N <= 1 << 20 && (int64_t)g.a_count * g.K <= (int64_t)kNowhere && (int64_t)g.N * g.K <= (int64_t)kNowhere &&
+    return g.K > kBlock && g.K <= 1 << 23 && g.N <= 1 << 20 && (!g.a_rows || (int64_t)g.a_count * g.K <= (int64_t)kNowhere) && (int64_t)g.N * g.K <= (int64_t)kNowhere &&
            ((int64_t)g.n_rows / 64 + g.E) * ceil_div(g.N, 128) < 1 << 30;
 }
 

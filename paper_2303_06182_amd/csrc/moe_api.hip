@@ -1068,12 +1068,16 @@ struct B128Layout {
 // Whether both products of a call of many rows run in tiles, for any number of rows up to T_max * k.
 static bool b128_experts_in_tiles(const moe_config_t &c)
 {
+    static const int32_t some = 0;
     GemmB128 g = {};
     g.E = c.E;
-    g.a_count = g.n_rows = c.T_max * c.k;
+    g.n_rows = c.T_max * c.k;
+    g.a_rows = &some;  // rows by index, of T_max tokens at most (of more rows there are no indices)
+    g.a_count = c.T_max;
     g.N = 2 * c.F;
     g.K = c.D;
     GemmB128 second = g;
+    second.a_rows = nullptr;
     second.N = c.D;
     second.K = c.F;
     return b128_tiles_ok(g) && b128_tiles_ok(second);
@@ -1114,8 +1118,8 @@ static B128Layout b128_layout(const moe_config_t &c)
 static int check_b128(const moe_handle_t *h, int32_t activation, const void *workspace, int64_t workspace_bytes)
 {
     const moe_config_t &c = h->cfg;
-    if (c.D % 16 != 0 || c.F % 16 != 0) {
-        set_error("experts in blocks of 128 need D and F that are multiples of 16 (D = %d, F = %d)", c.D, c.F);
+    if (c.D % 16 != 0 || c.F % 16 != 0 || c.D > 1 << 23 || c.F > 1 << 23) {
+        set_error("experts in blocks of 128 need D and F that are multiples of 16, up to 2^23 (D = %d, F = %d)", c.D, c.F);
         return MOE_ERR_UNSUPPORTED;
     }
     if (activation != MOE_ACT_RELU && activation != MOE_ACT_SILU) {
@@ -1219,8 +1223,10 @@ int moe_expert_ffn_b128(moe_handle_t *h, const void *x, int32_t x_rows, const in
         return MOE_ERR_INVALID_ARG;
     }
     const int64_t most = (int64_t)h->cfg.T_max * h->cfg.k;
-    if (n_rows < 0 || (int64_t)n_rows > most || x_rows < 0 || (int64_t)x_rows > most || (!src_tok && x_rows < n_rows) || (n_rows > 0 && x_rows == 0)) {
-        set_error("n_rows = %d, x_rows = %d: both in [0, k*T_max = %lld], and each of the rows is one of x", n_rows, x_rows, (long long)most);
+    if (n_rows < 0 || (int64_t)n_rows > most || x_rows < 0 || (int64_t)x_rows > (src_tok ? (int64_t)h->cfg.T_max : most) || (!src_tok && x_rows < n_rows) ||
+        (n_rows > 0 && x_rows == 0)) {
+        set_error("n_rows = %d, x_rows = %d: both in [0, k*T_max = %lld], x_rows up to T_max with src_tok, and each of the rows is one of x", n_rows, x_rows,
+                  (long long)most);
         return MOE_ERR_INVALID_ARG;
     }
     const int rc = check_b128(h, activation, workspace, workspace_bytes);
