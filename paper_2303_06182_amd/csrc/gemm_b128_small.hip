@@ -143,23 +143,25 @@ int launch_gemm_b128_small(const GemmB128 &g, hipStream_t s)
 }
 
 // Which of the two takes less, estimated in units of 50 ns.  Here: rounds of blocks, each with a beginning and an end and its waves' blocks of k.  Tiles: rounds of
-// tiles, of the height that suits best.  Measured, small / tiles, us: 17 rows, 2048 -> 8192 7.1 / 19; 64 rows 13 / 20; 128 rows 24 / 21; 64 rows, 8192 -> 2048 34 / 57;
-// 256 rows 35 / 89; 512 rows 68 / 90; 8 experts of 8 rows, 2048 -> 8192 26 / 27, of 32 rows 61 / 28; 64 experts of 32 rows, 512 -> 4096 114 / 34.
+// tiles, of the height that suits best.  Measured, small / tiles, us, bf16 results: one expert 2048 -> 8192, 16 rows 6.4 / 19, 64 rows 11 / 20, 128 rows 20 / 21.5,
+// 192 rows 29 / 21; 8192 -> 2048, 64 to 256 rows 33 / 58 to 62, 512 rows 63 / 62; 8 experts of 16 rows, 2048 -> 8192 38 / 28, 8192 -> 2048 47 / 70, of 48 rows
+// 58 / 76 (taken for 64, which have as many rounds of blocks: 91 / 77), of 96 113 / 81; 64 experts of 16 rows, 512 -> 4096 49 / 31.  fp32 results: 128 rows, 2048 -> 8192
+// 21 / 28; 512 rows, 8192 -> 2048 65 / 82; 8 experts of 64 rows, 8192 -> 2048 92 / 107.
 static bool small_pays(const GemmB128 &g)
 {
     const int64_t active = g.E < g.n_rows ? g.E : g.n_rows, rows = (g.n_rows + active - 1) / active;
     const int KT = ceil_div(g.K, kBlock);
-    static const int kIteration[2][3] = {{32, 48, 90}, {34, 50, 110}};
-    const int mr = rows <= 16 ? 1 : rows <= 32 ? 2 : 4, resident = mr == 1 ? 512 : 256;
+    static const int kIteration[2][3] = {{32, 48, 80}, {34, 50, 84}};
+    const int mr = rows <= 16 ? 1 : rows <= 32 ? 2 : 4, resident = mr == 1 && !g.precise ? 512 : 256;  // by registers
     const int64_t blocks = active * ceil_div(g.N, COLS) * ((rows + 16 * mr - 1) / (16 * mr));
     const int64_t here = (blocks + resident - 1) / resident * (40 + (int64_t)ceil_div(KT, NW) * kIteration[g.precise][mr == 4 ? 2 : mr - 1]);
     int64_t there = INT64_MAX;
     for (int h = 1; h <= 4; ++h) {
         const int64_t tiles = active * ceil_div((int)((rows + 63) / 64), h) * ceil_div(g.N, 256);
-        const int64_t t = (tiles + 255) / 256 * ((KT + 6) * (int64_t)kTileTime[g.precise][h - 1]);
+        const int64_t t = (tiles + 255) / 256 * ((KT + 9) * (int64_t)kTileTime[g.precise][h - 1]);
         if (t < there) there = t;
     }
-    return here < there;
+    return here <= there;
 }
 
 int launch_gemm_b128(const GemmB128 &g, hipStream_t s) { return !b128_tiles_ok(g) || small_pays(g) ? launch_gemm_b128_small(g, s) : launch_gemm_b128_tile(g, s); }
