@@ -6,7 +6,10 @@ plain torch.  Weights are random, so the tokens mean nothing; what it shows is h
 workspace for all layers, a cache a layer, one page table, lengths that live on the device, and a decoder step that is captured into a graph
 and replayed with nothing but the random numbers and the lengths changing.
 
-    python examples/decoder_steps.py [--layers 4 --batch 8 --prompt 200 --steps 32 --graph]
+With --blocks the experts are gated ones with e4m3 weights and a scale per block of 128 (moe_quantize_b128), chosen by sigmoid scores, a bias that
+balances them and groups of experts, in moe_layer_forward_b128.
+
+    python examples/decoder_steps.py [--layers 4 --batch 8 --prompt 200 --steps 32 --graph --blocks]
 """
 from __future__ import annotations
 
@@ -23,7 +26,7 @@ from paper_2303_06182_amd import binding  # noqa: E402
 
 class Decoder:
     def __init__(self, layers=4, d_model=1024, d_ff=4096, experts=16, n_heads=16, n_kv_heads=4, vocab=32000, batch=8, max_tokens=4096, page=64,
-                 max_new=4096, seed=0, device="cuda:0"):
+                 max_new=4096, seed=0, device="cuda:0", blocks=False):
         self.n_heads, self.n_kv_heads, self.head_dim, self.d, self.vocab = n_heads, n_kv_heads, d_model // n_heads, d_model, vocab
         self.batch, self.device = batch, torch.device(device)
         g = torch.Generator(device=device)
@@ -38,6 +41,12 @@ class Decoder:
         self.layers = [dict(qkv=weight(d_model + 2 * kv, d_model, std=d_model ** -0.5), o=weight(d_model, d_model, std=d_model ** -0.5),
                             gate=weight(experts, d_model, std=d_model ** -0.5), w1=weight(experts, d_ff, d_model, std=d_model ** -0.5),
                             w2=weight(experts, d_model, d_ff, std=d_ff ** -0.5)) for _ in range(layers)]
+        self.blocks = blocks
+        if blocks:
+            for w in self.layers:
+                w["w1"], w["w1_scale"] = binding.moe_quantize_b128(weight(experts, 2, d_ff, d_model, std=d_model ** -0.5), 128)
+                w["w2"], w["w2_scale"] = binding.moe_quantize_b128(w["w2"], 128)
+                w["balance"] = torch.zeros(experts, dtype=torch.float32, device=device)  # a training run moves it; every expert may be chosen
         self.moe = binding.MoeLayer(max_new, d_model, d_ff, experts, 2, "bf16", device=device)
         per_seq = -(-max_tokens // page)
         self.attention = binding.PagedAttention(batch, max_new, n_heads, n_kv_heads, self.head_dim, page, batch * per_seq, per_seq, "bf16",
@@ -54,6 +63,12 @@ class Decoder:
     def _norm(x):
         return (x * torch.rsqrt(x.pow(2).mean(-1, keepdim=True) + 1e-6)).bfloat16()
 
+    def _experts(self, x, w):
+        if not self.blocks:
+            return self.moe.moe_layer_forward(x, w["gate"], w["w1"], w["w2"])
+        return self.moe.moe_layer_forward_b128(x, w["gate"], w["w1"], w["w2"], w["w1_scale"], w["w2_scale"], activation="silu", score="sigmoid",
+                                               select_bias=w["balance"], n_groups=4, groups_kept=2, scale=2.0)
+
     def forward(self, tokens, q_offsets, max_q, max_kv):
         """tokens [T] of all sequences, of which kv_len already counts them; -> logits [batch, vocab] of every sequence's last token."""
         x = self.embedding[tokens].float()
@@ -66,7 +81,7 @@ class Decoder:
             q = self.attention.moe_kv_append(cache, q, k, v, self.inv_freq, q_offsets, self.kv_len, self.page_table, max_q)
             a, _ = self.attention.moe_attn_forward(cache, q, q_offsets, self.kv_len, self.page_table, max_q, max_kv, want_lse=False)
             x = x + torch.nn.functional.linear(a.view(T, h * dim), w["o"]).float()
-            x = x + self.moe.moe_layer_forward(self._norm(x), w["gate"], w["w1"], w["w2"]).float()
+            x = x + self._experts(self._norm(x), w).float()
         last = x[(q_offsets[1:] - 1).long()]
         return torch.nn.functional.linear(self._norm(last), self.head)
 
@@ -125,8 +140,9 @@ def main():
     for name, value in (("layers", 4), ("batch", 8), ("prompt", 200), ("steps", 32)):
         ap.add_argument("--" + name, type=int, default=value)
     ap.add_argument("--graph", action="store_true")
+    ap.add_argument("--blocks", action="store_true")
     a = ap.parse_args()
-    model = Decoder(layers=a.layers, batch=a.batch, max_tokens=a.prompt + a.steps + 64, max_new=a.batch * a.prompt)
+    model = Decoder(layers=a.layers, batch=a.batch, max_tokens=a.prompt + a.steps + 64, max_new=a.batch * a.prompt, blocks=a.blocks)
     g = torch.Generator()
     g.manual_seed(0)
     prompts = [torch.randint(0, model.vocab, (a.prompt - 7 * b % a.prompt,), generator=g).tolist() for b in range(a.batch)]

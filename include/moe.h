@@ -574,7 +574,7 @@ int moe_expert_ffn_b128(moe_handle_t *h, const void *x, int32_t x_rows, const in
                         void *workspace, int64_t workspace_bytes, void *stream);
 
 /* moe_layer_forward with these experts, chosen by moe_select_experts from the gate's logits (gate_bias is added to those, as ever, select_bias to the
- * scores).  select->E and select->k are the handle's; its `renormalize` plays no part.  Same workspace as moe_expert_ffn_b128. */
+ * scores).  select->E and select->k have to be the handle's; the handle's own `renormalize` plays no part.  Same workspace as moe_expert_ffn_b128. */
 int moe_layer_forward_b128(moe_handle_t *h, const void *x, const void *wg, const float *gate_bias, const moe_select_config_t *select,
                            const float *select_bias, const void *w1_q, const void *w2_q, const void *w1_scale, const void *w2_scale,
                            int32_t activation, int32_t T, void *y, const moe_routing_t *routing_out, void *workspace, int64_t workspace_bytes,
