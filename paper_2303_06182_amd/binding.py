@@ -845,8 +845,8 @@ def b128_scale_cols(cols: int) -> int:
 def _b128_operand(q, scale, shape: tuple, scale_rows: tuple, block_rows: int, index: int, name: str) -> None:
     """q of `shape` and its scales; scale_rows: the dimensions in front of a matrix's rows, of the scales."""
     scales = scale_rows + (-(-shape[-2] // block_rows), -(-shape[-1] // 512) * 4)
-    if tuple(q.shape) != shape or q.element_size() != 1 or not q.is_contiguous() or q.get_device() != index:
-        raise ValueError("%s_q must be %s of one byte each, contiguous, on cuda:%d" % (name, list(shape), index))
+    if tuple(q.shape) != shape or q.dtype not in (torch.float8_e4m3fn, torch.uint8) or not q.is_contiguous() or q.get_device() != index:
+        raise ValueError("%s_q must be %s of float8_e4m3fn or its bytes, contiguous, on cuda:%d" % (name, list(shape), index))
     if tuple(scale.shape) != scales or scale.dtype != torch.uint8 or not scale.is_contiguous() or scale.get_device() != index:
         raise ValueError("%s_scale must be %s of uint8, contiguous, on cuda:%d" % (name, list(scales), index))
 

@@ -102,7 +102,7 @@ __global__ __launch_bounds__(kThreads, 1) void gemm_b128_tile_kernel(GemmB128 g)
     const int tid = threadIdx.x, lane = tid & 63;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int wm = wave / WN, wn = wave % WN;
-    const int K = g.K, KT = (K + kBlock - 1) / kBlock;
+    const int K = g.K, KT = max((K + kBlock - 1) / kBlock, 2);  // two at least, for the load stream; the second may be all zeros
     const int n_tiles = (g.Nh + TILE_N - 1) / TILE_N;
     const int scale_cols = (int)b128_scale_cols(K), n_blocks = (g.Nh + kBlock - 1) / kBlock;
 
@@ -345,7 +345,12 @@ __global__ __launch_bounds__(kThreads, 1) void gemm_b128_tile_kernel(GemmB128 g)
         else if ((kt & 3) == 0 && kt >> 2 < last_group) issue_scales((kt >> 2) + 1);
     };
     auto turn_scales = [&](int kt) __attribute__((always_inline)) {  // behind K tile kt
-        if (kt + 1 == KT || ((kt + 1) & 3) == 0) {
+        if (kt == 0 && K <= kBlock) {  // a K tile of zeros, whatever byte stands there
+#pragma unroll
+            for (int i = 0; i < MI; ++i) sa[i] = 127;
+#pragma unroll
+            for (int n = 0; n < NI; ++n) sb[n] = 127;
+        } else if (kt + 1 == KT || ((kt + 1) & 3) == 0) {
             take_scales();
         } else {
 #pragma unroll
@@ -664,11 +669,11 @@ static int launch_tile_as(const GemmB128 &g, hipStream_t s)
     return MOE_OK;
 }
 
-// The kernel addresses an expert's weights, a tile's rows of A, and all of A where rows are chosen by index, with 32-bit byte offsets, counts output tiles in
-// 32 bits, and its load stream is two K tiles ahead.
+// The kernel addresses an expert's weights, a tile's rows of A, and all of A where rows are chosen by index, with 32-bit byte offsets, and counts output tiles
+// in 32 bits.
 bool b128_tiles_ok(const GemmB128 &g)
 {
-    return g.K > kBlock && g.K <= 1 << 23 && g.N <= 1 << 20 && (!g.a_rows || (int64_t)g.a_count * g.K <= (int64_t)kNowhere) && (int64_t)g.N * g.K <= (int64_t)kNowhere &&
+    return g.K <= 1 << 23 && g.N <= 1 << 20 && (!g.a_rows || (int64_t)g.a_count * g.K <= (int64_t)kNowhere) && (int64_t)g.N * g.K <= (int64_t)kNowhere &&
            ((int64_t)g.n_rows / 64 + g.E) * ceil_div(g.N, 128) < 1 << 30;
 }
 

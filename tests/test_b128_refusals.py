@@ -4,6 +4,7 @@ import math
 
 import pytest
 import torch
+import torch
 
 from paper_2303_06182_amd import binding
 
@@ -97,3 +98,15 @@ def test_binding_refuses_before_the_library():
                  lambda: binding.moe_gemm_b128(x, x, x, x), lambda: binding.moe_gemm_b128(x[0], x, x, x)):
         with pytest.raises(ValueError):
             call()
+
+
+@pytest.mark.parametrize("dtype,fits", [(torch.float8_e4m3fn, True), (torch.uint8, True), (torch.int8, False), (torch.bool, False), (torch.float8_e5m2, False),
+                                        (torch.float8_e4m3fnuz, False)])
+def test_other_bytes_are_refused(dtype, fits):
+    """One byte an element is not enough: only e4m3 as it is here, or its bytes."""
+    q, scale = torch.empty((3, 128), dtype=dtype), torch.empty((3, 4), dtype=torch.uint8)
+    if fits:
+        binding._b128_operand(q, scale, (3, 128), (), 1, -1, "a")
+    else:
+        with pytest.raises(ValueError):
+            binding._b128_operand(q, scale, (3, 128), (), 1, -1, "a")

@@ -305,6 +305,34 @@ def test_gemm_nan_stays_in_its_row(dtype, rows):
     check_sums(got[keep_r][:, keep_c], want[np.ix_(keep_r, keep_c)], size[np.ix_(keep_r, keep_c)], 144, dtype)
 
 
+@pytest.mark.parametrize("rows,E,N,K", [(2000, 3, 512, 128), (1500, 2, 776, 112), (3000, 1, 264, 16), (900, 5, 1032, 80)])
+@pytest.mark.parametrize("dtype", [BF16, F32])
+def test_gemm_one_block_of_k(rows, E, N, K, dtype):
+    """Rows of one block and less, many of them; what stands in the scales' padding plays no part."""
+    (a, sa, av), (w, sw, wv) = operands(rows, E, N, K, 5)
+    sa[:, 1:] = 255
+    sw[:, :, 1:] = 255
+    offsets = split(rows, E, 6)
+    want, size = b128.gemm(av, wv, offsets)
+    check_sums(binding.moe_gemm_b128(a, sa, w, sw, offsets=ints(offsets), out_dtype=dtype), want, size, K, dtype)
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+def test_gemm_rows_past_32_bits(dtype):
+    K, N, rows = 8192, 264, 2 ** 32 // 8192 + 300
+    (a, sa, av), (w, sw, wv) = operands(300, 1, N, K, 7)
+    long, scales = torch.zeros((rows, K), dtype=torch.uint8, device=DEV), torch.full((rows, sa.shape[1]), 127, dtype=torch.uint8, device=DEV)
+    long[-300:] = a.view(torch.uint8)
+    scales[-300:] = sa
+    long = long.view(torch.float8_e4m3fn)
+    want, size = b128.gemm(av, wv, [0, 300])
+    got = binding.moe_gemm_b128(long, scales, w[0], sw[0], out_dtype=dtype)
+    assert (got[:-300] == 0).all()
+    check_sums(got[-300:], want, size, K, dtype)
+    pick = np.arange(rows - 1, rows - 300, -7)
+    check_sums(binding.moe_gemm_b128(long, scales, w[0], sw[0], a_rows=ints(pick), out_dtype=dtype), want[pick - rows], size[pick - rows], K, dtype)
+
+
 @pytest.mark.parametrize("dtype", [BF16, F32])
 def test_gemm_scales_far_apart(dtype):
     """Scale bytes over a wide range, the blocks of a row far from each other: small blocks beside large ones count as fp32 lets them."""
@@ -360,6 +388,14 @@ def test_ffn(T, rows, E, D, F, activation, dtype):
     assert torch.equal(y, again)
     # the rows themselves, as a dispatch has laid them out
     assert torch.equal(layer.moe_expert_ffn_b128(x[ints(src).long()].contiguous(), ints(offsets), *weights, activation=activation), y)
+
+
+@pytest.mark.parametrize("T,E,D,F", [(600, 4, 64, 48), (400, 3, 528, 128), (500, 5, 128, 400)])
+@pytest.mark.parametrize("activation", ["relu", "silu"])
+@pytest.mark.parametrize("dtype", [BF16, F32])
+def test_ffn_narrow(T, E, D, F, activation, dtype):
+    """One block of 128 and less, of rows or of hidden elements, and rows enough for tiles."""
+    test_ffn(T, T + 100, E, D, F, activation, dtype)
 
 
 def test_ffn_leaves_other_rows_and_refuses():
