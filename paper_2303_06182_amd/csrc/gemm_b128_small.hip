@@ -132,14 +132,35 @@ int launch_rows(const GemmB128 &g, hipStream_t s)
     return MOE_OK;
 }
 
+// What a call takes at 16 mr rows a block, estimated in units of 50 ns: rounds of blocks, each with a beginning and an end and its waves' blocks of k.
+int64_t small_time(const GemmB128 &g, int mr)
+{
+    static const int kIteration[2][3] = {{32, 48, 80}, {34, 50, 84}};
+    const int64_t active = g.E < g.n_rows ? g.E : g.n_rows, rows = (g.n_rows + active - 1) / active;
+    constexpr int resident = 256;  // where a CU has two, as it can of 16 rows, each takes twice as long (64 to 96 rows, 8192 -> 2048: 16 -> 28 us)
+    const int64_t blocks = active * ceil_div(g.N, COLS) * ((rows + 16 * mr - 1) / (16 * mr));
+    return (blocks + resident - 1) / resident * (40 + (int64_t)ceil_div(ceil_div(g.K, kBlock), NW) * kIteration[g.precise][mr == 4 ? 2 : mr - 1]);
+}
+
+// Few columns: more blocks of fewer rows, which read the same weights out of L2.
+int best_rows(const GemmB128 &g)
+{
+    int best = 4;
+    for (int mr = 2; mr >= 1; --mr)
+        if (small_time(g, mr) < small_time(g, best)) best = mr;
+    return best;
+}
+
 }  // namespace
 
 int launch_gemm_b128_small(const GemmB128 &g, hipStream_t s)
 {
     ProfScope ps(g.name ? g.name : "gemm_b128", s);
-    if (g.n_rows <= 16 * (int64_t)g.E) return g.precise ? launch_rows<true, 1>(g, s) : launch_rows<false, 1>(g, s);
-    if (g.n_rows <= 32 * (int64_t)g.E) return g.precise ? launch_rows<true, 2>(g, s) : launch_rows<false, 2>(g, s);
-    return g.precise ? launch_rows<true, 4>(g, s) : launch_rows<false, 4>(g, s);
+    switch (best_rows(g)) {
+    case 1: return g.precise ? launch_rows<true, 1>(g, s) : launch_rows<false, 1>(g, s);
+    case 2: return g.precise ? launch_rows<true, 2>(g, s) : launch_rows<false, 2>(g, s);
+    default: return g.precise ? launch_rows<true, 4>(g, s) : launch_rows<false, 4>(g, s);
+    }
 }
 
 // Which of the two takes less, estimated in units of 50 ns.  Here: rounds of blocks, each with a beginning and an end and its waves' blocks of k.  Tiles: rounds of
@@ -151,10 +172,7 @@ static bool small_pays(const GemmB128 &g)
 {
     const int64_t active = g.E < g.n_rows ? g.E : g.n_rows, rows = (g.n_rows + active - 1) / active;
     const int KT = ceil_div(g.K, kBlock);
-    static const int kIteration[2][3] = {{32, 48, 80}, {34, 50, 84}};
-    const int mr = rows <= 16 ? 1 : rows <= 32 ? 2 : 4, resident = mr == 1 && !g.precise ? 512 : 256;  // by registers
-    const int64_t blocks = active * ceil_div(g.N, COLS) * ((rows + 16 * mr - 1) / (16 * mr));
-    const int64_t here = (blocks + resident - 1) / resident * (40 + (int64_t)ceil_div(KT, NW) * kIteration[g.precise][mr == 4 ? 2 : mr - 1]);
+    const int64_t here = small_time(g, best_rows(g));
     int64_t there = INT64_MAX;
     for (int h = 1; h <= 4; ++h) {
         const int64_t tiles = active * ceil_div((int)((rows + 63) / 64), h) * ceil_div(g.N, 256);
