@@ -1,8 +1,9 @@
 // Products of e4m3 operands in blocks of 128 where whole tiles would leave most CUs without work.
 //
-// A block takes 16 MR rows by 32 weight rows of an expert; its 8 waves share the blocks of k (wave w takes w, w + 8, ...), read both operands from memory
-// (which for sizes like these is the L2) straight into registers, a block of k ahead, and work alone until one join in LDS.  What bounds it is
-// latency: a wave has two to eight blocks of k, one after the other.
+// A block takes 16 MR rows by 16 or 32 weight rows of an expert; its 8 waves share the blocks of k (wave w takes w, w + 8, ...), read both operands from memory
+// (which for sizes like these is the L2) straight into registers, up to P blocks of k at once, and work alone until one join in LDS.  What bounds it: latency, where
+// a wave has two blocks of k (17 rows, 2048 -> 8192: 7.5 us), and else what one CU can have on its way, about 20 bytes a ns; so that more and smaller blocks pay until every CU has
+// one (8192 -> 2048: 16 rows by 32 / by 16 columns 15.3 / 11.8 us; 64 rows in blocks of 64 / of 16 33 / 16 us).
 // Fragments: lane l holds bytes 16 (l / 16) and 64 + 16 (l / 16) of row l % 16's 128; either operand's k lie in that order.  Fast and precise: as in
 // gemm_b128_tile.hip, with the instructions for 16 x 16.
 #include "b128_dev.h"
@@ -11,11 +12,15 @@ namespace moe355 {
 
 namespace {
 
-constexpr int NW = 8, kThreads = NW * 64, NC = 2, COLS = NC * 16, LD = COLS + 4;
+constexpr int NW = 8, kThreads = NW * 64;
 
-template <bool PRECISE, int MR>
+// NC: blocks of 16 weight rows
+template <bool PRECISE, int MR, int NC>
 __global__ __launch_bounds__(kThreads) void gemm_b128_small_kernel(GemmB128 g)
 {
+    constexpr int COLS = NC * 16, LD = COLS + 4;
+    // blocks of k that a wave has at once
+    constexpr int P = MR == 1 ? 4 : MR == 2 ? 2 : 1;
     __shared__ __align__(16) float join[NW * 16 * LD];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int r = lane & 15, part = lane >> 4;
@@ -29,7 +34,7 @@ __global__ __launch_bounds__(kThreads) void gemm_b128_small_kernel(GemmB128 g)
         const uint8_t *w[NC], *a[MR], *as[MR];
 #pragma unroll
         for (int c = 0; c < NC; ++c) w[c] = g.w + ((int64_t)e * g.N + min(n0 + c * 16 + r, g.N - 1)) * K + part * 16;
-        const uint8_t *const ws = g.w_scale + ((int64_t)e * n_blocks + n0 / kBlock) * scale_cols;  // 32 weight rows lie in one block
+        const uint8_t *const ws = g.w_scale + ((int64_t)e * n_blocks + n0 / kBlock) * scale_cols;  // 32 neighbouring weight rows lie in one block
 #pragma unroll
         for (int m = 0; m < MR; ++m) {
             int at = min(row0 + 16 * m + r, end - 1);
@@ -80,24 +85,17 @@ __global__ __launch_bounds__(kThreads) void gemm_b128_small_kernel(GemmB128 g)
                     for (int c = 0; c < NC; ++c) acc[m][c] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(f.w[c], f.a[m], acc[m][c], 0, 0, 0, f.ws, 0, f.as[m]);
             }
         };
-        int b = wave;
-        if constexpr (MR < 4) {
-            Raw f[2];
-            if (b < KB) load(f[0], b);
-            while (b < KB) {
-                if (b + NW < KB) load(f[1], b + NW);
-                multiply(f[0]);
+        Raw f[P];
+#pragma unroll
+        for (int j = 0; j + 1 < P; ++j)
+            if (wave + j * NW < KB) load(f[j], wave + j * NW);
+        for (int b = wave; b < KB;) {
+#pragma unroll
+            for (int j = 0; j < P; ++j) {
+                if (b + (P - 1) * NW < KB) load(f[(j + P - 1) % P], b + (P - 1) * NW);
+                multiply(f[j]);
                 b += NW;
                 if (b >= KB) break;
-                if (b + NW < KB) load(f[0], b + NW);
-                multiply(f[1]);
-                b += NW;
-            }
-        } else {  // two blocks of k do not fit the registers beside the sums: 64 rows, 2048 -> 8192 13.1 us with them, 11.5 without (precise 17.4, 12.3)
-            for (; b < KB; b += NW) {
-                Raw f;
-                load(f, b);
-                multiply(f);
             }
         }
         const int waves = min(NW, KB);  // the others have nothing to add
@@ -122,33 +120,41 @@ __global__ __launch_bounds__(kThreads) void gemm_b128_small_kernel(GemmB128 g)
     }
 }
 
-template <bool PRECISE, int MR>
-int launch_rows(const GemmB128 &g, hipStream_t s)
+template <bool PRECISE, int MR, int NC>
+int launch_as(const GemmB128 &g, hipStream_t s)
 {
     const int per = ceil_div(g.n_rows, g.E * 16 * MR);
-    const dim3 grid(ceil_div(g.N, COLS), g.E < g.n_rows ? g.E : g.n_rows, per < 64 ? per : 64);
-    hipLaunchKernelGGL((gemm_b128_small_kernel<PRECISE, MR>), grid, dim3(kThreads), 0, s, g);
+    const dim3 grid(ceil_div(g.N, NC * 16), g.E < g.n_rows ? g.E : g.n_rows, per < 64 ? per : 64);
+    hipLaunchKernelGGL((gemm_b128_small_kernel<PRECISE, MR, NC>), grid, dim3(kThreads), 0, s, g);
     MOE_LAUNCH_CHECK("gemm_b128_small_kernel");
     return MOE_OK;
 }
 
-// What a call takes at 16 mr rows a block, estimated in units of 50 ns: rounds of blocks, each with a beginning and an end and its waves' blocks of k.
-int64_t small_time(const GemmB128 &g, int mr)
+struct Shape {
+    int mr, nc;
+    int64_t time;
+};
+// The rows and columns of a block that take least, estimated in units of 50 ns: rounds of blocks, each with a beginning and an end and its waves' blocks of k, which cost about
+// what they load.  Few columns: more blocks, of fewer rows or columns; those that read the same weights find them in the L2.  A CU runs one block a round: where it has two, as it
+// can of 16 rows, each takes twice as long (64 and 96 rows, 8192 -> 2048: 16 and 28 us).
+Shape best_shape(const GemmB128 &g)
 {
-    static const int kIteration[2][3] = {{32, 48, 80}, {34, 50, 84}};
+    static const struct { int mr, nc, iteration[2]; } kShapes[] = {{4, 2, {80, 84}}, {2, 2, {48, 50}}, {1, 2, {32, 34}}, {1, 1, {22, 24}}};
     const int64_t active = g.E < g.n_rows ? g.E : g.n_rows, rows = (g.n_rows + active - 1) / active;
-    constexpr int resident = 256;  // where a CU has two, as it can of 16 rows, each takes twice as long (64 to 96 rows, 8192 -> 2048: 16 -> 28 us)
-    const int64_t blocks = active * ceil_div(g.N, COLS) * ((rows + 16 * mr - 1) / (16 * mr));
-    return (blocks + resident - 1) / resident * (40 + (int64_t)ceil_div(ceil_div(g.K, kBlock), NW) * kIteration[g.precise][mr == 4 ? 2 : mr - 1]);
+    Shape best = {0, 0, INT64_MAX};
+    for (const auto &k : kShapes) {
+        const int64_t blocks = active * ceil_div(g.N, k.nc * 16) * ((rows + 16 * k.mr - 1) / (16 * k.mr));
+        const int64_t t = (blocks + 255) / 256 * (40 + (int64_t)ceil_div(ceil_div(g.K, kBlock), NW) * k.iteration[g.precise]);
+        if (t < best.time) best = {k.mr, k.nc, t};
+    }
+    return best;
 }
 
-// Few columns: more blocks of fewer rows, which read the same weights out of L2.
-int best_rows(const GemmB128 &g)
+template <bool PRECISE>
+int launch_shape(const GemmB128 &g, const Shape &shape, hipStream_t s)
 {
-    int best = 4;
-    for (int mr = 2; mr >= 1; --mr)
-        if (small_time(g, mr) < small_time(g, best)) best = mr;
-    return best;
+    if (shape.nc == 1) return launch_as<PRECISE, 1, 1>(g, s);
+    return shape.mr == 1 ? launch_as<PRECISE, 1, 2>(g, s) : shape.mr == 2 ? launch_as<PRECISE, 2, 2>(g, s) : launch_as<PRECISE, 4, 2>(g, s);
 }
 
 }  // namespace
@@ -156,23 +162,18 @@ int best_rows(const GemmB128 &g)
 int launch_gemm_b128_small(const GemmB128 &g, hipStream_t s)
 {
     ProfScope ps(g.name ? g.name : "gemm_b128", s);
-    switch (best_rows(g)) {
-    case 1: return g.precise ? launch_rows<true, 1>(g, s) : launch_rows<false, 1>(g, s);
-    case 2: return g.precise ? launch_rows<true, 2>(g, s) : launch_rows<false, 2>(g, s);
-    default: return g.precise ? launch_rows<true, 4>(g, s) : launch_rows<false, 4>(g, s);
-    }
+    return g.precise ? launch_shape<true>(g, best_shape(g), s) : launch_shape<false>(g, best_shape(g), s);
 }
 
-// Which of the two takes less, estimated in units of 50 ns.  Here: rounds of blocks, each with a beginning and an end and its waves' blocks of k.  Tiles: rounds of
-// tiles, of the height that suits best.  Measured, small / tiles, us, bf16 results: one expert 2048 -> 8192, 16 rows 6.4 / 19, 64 rows 11 / 20, 128 rows 20 / 21.5,
-// 192 rows 29 / 21; 8192 -> 2048, 64 to 256 rows 33 / 58 to 62, 512 rows 63 / 62; 8 experts of 16 rows, 2048 -> 8192 38 / 28, 8192 -> 2048 47 / 70, of 48 rows
-// 58 / 76 (taken for 64, which have as many rounds of blocks: 91 / 77), of 96 113 / 81; 64 experts of 16 rows, 512 -> 4096 49 / 31.  fp32 results: 128 rows, 2048 -> 8192
-// 21 / 28; 512 rows, 8192 -> 2048 65 / 82; 8 experts of 64 rows, 8192 -> 2048 92 / 107.
+// Which of the two takes less, this or tiles: rounds of tiles, of the height that suits best.  Measured, small / tiles, us, bf16 results: one expert 2048 -> 8192,
+// 16 rows 6.2 / 19, 64 rows 11 / 20, 128 rows 20 / 21.5, 192 rows 29 / 21; 8192 -> 2048, 16 rows 11.8 / 56, 64 rows 16 / 58, 256 rows 33 / 62, 512 rows 63 / 62; 8 experts of
+// 16 rows, 2048 -> 8192 38 / 28, 8192 -> 2048 44 / 70, of 48 rows 58 / 76 (tiles are taken), of 64 rows 91 / 77; 64 experts of 16 rows, 512 -> 4096 49 / 31.
+// fp32 results: 128 rows, 2048 -> 8192 21 / 28; 512 rows, 8192 -> 2048 65 / 82; 8 experts of 64 rows, 8192 -> 2048 92 / 107.
 static bool small_pays(const GemmB128 &g)
 {
     const int64_t active = g.E < g.n_rows ? g.E : g.n_rows, rows = (g.n_rows + active - 1) / active;
     const int KT = ceil_div(g.K, kBlock);
-    const int64_t here = small_time(g, best_rows(g));
+    const int64_t here = best_shape(g).time;
     int64_t there = INT64_MAX;
     for (int h = 1; h <= 4; ++h) {
         const int64_t tiles = active * ceil_div((int)((rows + 63) / 64), h) * ceil_div(g.N, 256);
