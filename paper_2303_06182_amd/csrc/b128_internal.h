@@ -51,6 +51,7 @@ struct GemmB128 {
     uint8_t *c_scale;  // [n_rows, scale columns of Nh]
     int c_dtype;
     bool precise;  // sums in fp32 throughout (gemm_b128_tile.hip)
+    bool deep;         // with an activation: sums of sums of 256 products (gemm_b128_tile.hip)
     const char *name;  // of the launch for the event profiler
 };
 // few rows an expert, which it quantises itself (gemm_b128_stream.hip)

@@ -20,6 +20,11 @@
 // their deviation) sends some elements in ten thousand to the other side of a border.  With it the output's error against 64 bits was 2.2e-3
 // to 2.5e-3, without it 1.7e-3, which is the output's own rounding to bf16.
 //
+// Deep (first product of a feed-forward in fp32): there nothing hides a hidden element that falls to the other side of a border of e4m3.  A sum of n roundings is off
+// by the sum of its partial sums' squares, n^2 / 2; sums of 16 steps (256 k) and then of those sums by 8 n + n^2 / 32, which at K = 2048 is 0.4 of the
+// error.  The second sums take registers, so a tile has 128 rows at most: 16384 tokens x 2 over 16 experts, 2048 -> 8192 -> 2048, 1.94 -> 2.17 ms.  Of 28 drawn cases 11 had
+// elements on the other side of a border than 64-bit sums, and 8 have (a plain program in fp32: 7).
+//
 // A slot row is 64 bytes: 16-byte chunk c of row r sits at position c ^ ((r >> 2) & 3), which keeps the 16 lanes x 16 bytes of a
 // fragment read on 16 different bank groups.  A lane's 16 bytes of a row are the same k for either operand, whatever their order.
 // Weight row permutation: LDS row i of a block of 32 holds column 16 * ((i >> 2) & 1) + 4 * (i >> 3) + (i & 3), so that the 16 sums of a lane are
@@ -93,9 +98,11 @@ __device__ __forceinline__ bf16x8 widen8(const u32x4 &c, int q, float scale)
 
 }  // namespace
 
-template <bool PRECISE, int EPI>
+// DEEP: precise, with sums of sums
+template <bool PRECISE, int EPI, bool DEEP>
 __global__ __launch_bounds__(kThreads, 1) void gemm_b128_tile_kernel(GemmB128 g)
 {
+    constexpr int MOST = DEEP ? 2 : MI;  // 32-row blocks of a wave
     constexpr int SLOTS = PRECISE ? 4 : 5;
     constexpr int TILE_N = EPI == kEpiSilu ? BN / 2 : BN;  // columns of the result
     extern __shared__ __attribute__((aligned(1024))) uint8_t smem[];
@@ -109,7 +116,7 @@ __global__ __launch_bounds__(kThreads, 1) void gemm_b128_tile_kernel(GemmB128 g)
     // ---- the block's tiles.  Experts, 64 at a time, one per lane: rows, tiles along them, output tiles before it.
     int w_base = 0, w_pos = 0, w_total = 0;
     int w_row0, w_row_end, w_cuts, w_excl;
-    int cap = 4;  // height of a tile, in units of 64 rows
+    int cap = MOST;  // height of a tile, in units of 64 rows
     auto load_window = [&]() __attribute__((always_inline)) {
         w_row0 = 0, w_row_end = 0;
         const int e = w_base + lane;
@@ -143,14 +150,14 @@ __global__ __launch_bounds__(kThreads, 1) void gemm_b128_tile_kernel(GemmB128 g)
         }
         float best = 0.f;
 #pragma unroll
-        for (int h = 4; h >= (PRECISE ? 1 : 2); --h) {
+        for (int h = MOST; h >= (PRECISE ? 1 : 2); --h) {
             int n = tiles[h - 1];
 #pragma unroll
             for (int off = 32; off >= 1; off >>= 1) n += __shfl_xor(n, off, 64);
             const float out = (float)n * (float)n_tiles, rounds = ceilf(out * (1.f / 256.f));
             const float t = rounds * (float)((KT + 6) * kTileTime[PRECISE][h - 1]);
-            if (h == 4 || t < 0.97f * best) best = t, cap = h;
-            if (h == 4 && rounds > 3.f) break;  // blocks of several rounds even out by themselves
+            if (h == MOST || t < 0.97f * best) best = t, cap = h;
+            if (h == MOST && rounds > 3.f) break;  // blocks of several rounds even out by themselves
         }
         cap = __builtin_amdgcn_readfirstlane(cap);
     }
@@ -568,6 +575,7 @@ __global__ __launch_bounds__(kThreads, 1) void gemm_b128_tile_kernel(GemmB128 g)
         auto run_tile = [&](const Tile &ti, auto blocks) __attribute__((always_inline)) {
             constexpr int M = decltype(blocks)::value;
             zero_acc(blocks);
+            f32x16_t sum[DEEP ? M : 1][NI] = {};
             read_phase(0, r_slot, 0, blocks);
             for (int kt = 0; kt < KT; ++kt) {
                 if (kt == KT - 2) next_tile();
@@ -621,6 +629,25 @@ __global__ __launch_bounds__(kThreads, 1) void gemm_b128_tile_kernel(GemmB128 g)
                 next_k();
                 r_slot = slot2;
                 turn_scales(kt);
+                if constexpr (DEEP) {
+                    if ((kt & 1) || kt + 1 == KT) {
+                        asm volatile("s_nop 15\n\ts_nop 15" ::: "memory");  // see mfma_fp8
+#pragma unroll
+                        for (int mi = 0; mi < M; ++mi)
+#pragma unroll
+                            for (int ni = 0; ni < NI; ++ni) {
+                                asm volatile("" : "+v"(acc[mi][ni]));
+                                sum[mi][ni] += acc[mi][ni];
+                            }
+                        zero_acc(blocks);
+                    }
+                }
+            }
+            if constexpr (DEEP) {
+#pragma unroll
+                for (int mi = 0; mi < M; ++mi)
+#pragma unroll
+                    for (int ni = 0; ni < NI; ++ni) acc[mi][ni] = sum[mi][ni];
             }
             epilogue(ti, blocks);
         };
@@ -644,8 +671,10 @@ __global__ __launch_bounds__(kThreads, 1) void gemm_b128_tile_kernel(GemmB128 g)
         __builtin_amdgcn_sched_barrier(0);
         while (true) {
             const int blocks = (t.row_end - t.row0 + 63) >> 6;
-            if (opaque(blocks) == 4) run_tile(t, std::integral_constant<int, 4>{});
-            if (opaque(blocks) == 3) run_tile(t, std::integral_constant<int, 3>{});
+            if constexpr (!DEEP) {
+                if (opaque(blocks) == 4) run_tile(t, std::integral_constant<int, 4>{});
+                if (opaque(blocks) == 3) run_tile(t, std::integral_constant<int, 3>{});
+            }
             if (opaque(blocks) == 2) run_tile(t, std::integral_constant<int, 2>{});
             if (opaque(blocks) == 1) run_tile(t, std::integral_constant<int, 1>{});
             if (!l_more) break;
@@ -655,11 +684,11 @@ __global__ __launch_bounds__(kThreads, 1) void gemm_b128_tile_kernel(GemmB128 g)
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // no LDS write may outlive the block
 }
 
-template <bool PRECISE, int EPI>
+template <bool PRECISE, int EPI, bool DEEP = false>
 static int launch_tile_as(const GemmB128 &g, hipStream_t s)
 {
     const size_t smem = (PRECISE ? 4 : 5) * SLOT + (EPI != kEpiPlain ? 4 * 256 * 4 : 0);
-    auto kern = gemm_b128_tile_kernel<PRECISE, EPI>;
+    auto kern = gemm_b128_tile_kernel<PRECISE, EPI, DEEP>;
     static std::once_flag once;  // per instantiation
     static hipError_t setup_rc = hipSuccess;
     std::call_once(once, [&]() { setup_rc = hipFuncSetAttribute(reinterpret_cast<const void *>(kern), hipFuncAttributeMaxDynamicSharedMemorySize, (int)smem); });
@@ -680,8 +709,8 @@ bool b128_tiles_ok(const GemmB128 &g)
 int launch_gemm_b128_tile(const GemmB128 &g, hipStream_t s)
 {
     ProfScope ps(g.name ? g.name : "gemm_b128", s);
-    if (g.act == kActSilu) return launch_tile_as<true, kEpiSilu>(g, s);
-    if (g.act == kActRelu) return launch_tile_as<true, kEpiRelu>(g, s);
+    if (g.act == kActSilu) return g.deep ? launch_tile_as<true, kEpiSilu, true>(g, s) : launch_tile_as<true, kEpiSilu>(g, s);
+    if (g.act == kActRelu) return g.deep ? launch_tile_as<true, kEpiRelu, true>(g, s) : launch_tile_as<true, kEpiRelu>(g, s);
     return g.precise ? launch_tile_as<true, kEpiPlain>(g, s) : launch_tile_as<false, kEpiPlain>(g, s);
 }
 

@@ -1160,6 +1160,7 @@ static int run_expert_ffn_b128(moe_handle_t *h, const void *x, int32_t x_rows, c
     g.K = c.D;
     g.act = gated ? kActSilu : kActRelu;
     g.precise = true;
+    g.deep = c.dtype == MOE_DTYPE_F32;
     g.name = "expert_gemm1";
     GemmB128 g2 = g;
     g2.a_count = n_rows;
