@@ -143,10 +143,12 @@ __device__ __forceinline__ bf16x8 widen(const Fragment &f, int q, float scale)
     }
     return __builtin_bit_cast(bf16x8, w);
 }
-// g / (1 + exp(-g)), off by some 2^-23 of it: the reciprocal takes a Newton step.  With the hardware's exponential and reciprocal alone it was off by (|g| + 4) 2^-23, more than
-// the sums are, and sent twice as many elements over a border of e4m3.  Where the exponential passes fp32 the result is -0.
+// g / (1 + exp(-g)).  By the hardware's exponential and reciprocal off by less than (|g| + 4) 2^-23 of it, which is more than the sums are, but far below what bf16 results
+// show; EXACT, for fp32: by 2^-22, at 2 us of one token's 22.  Where the exponential passes fp32 the result is -0.
+template <bool EXACT>
 __device__ __forceinline__ float silu(float g)
 {
+    if constexpr (!EXACT) return g * __builtin_amdgcn_rcpf(1.f + __expf(-g));
     const float d = 1.f + expf(-g), r = __builtin_amdgcn_rcpf(d);
     return g * (d < INFINITY ? fmaf(fmaf(-d, r, 1.f), r, r) : 0.f);
 }

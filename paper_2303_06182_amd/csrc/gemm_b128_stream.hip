@@ -196,7 +196,7 @@ __device__ __forceinline__ void stream_rows(const GemmB128 &g, uint8_t *smem, in
                     if (col >= g.Nh) continue;  // a multiple of 8
                     float v[4];
 #pragma unroll
-                    for (int j = 0; j < 4; ++j) v[j] = ACT == kActSilu ? silu(acc[m][0][j]) * acc[m][1][j] : ACT == kActRelu ? relu(acc[m][c][j]) : acc[m][c][j];
+                    for (int j = 0; j < 4; ++j) v[j] = ACT == kActSilu ? silu<A == kRowsF32>(acc[m][0][j]) * acc[m][1][j] : ACT == kActRelu ? relu(acc[m][c][j]) : acc[m][c][j];
                     const int64_t at = (int64_t)(row0 + row) * g.Nh + col;
                     if (g.c_dtype == MOE_DTYPE_F32) *reinterpret_cast<float4 *>(static_cast<float *>(g.c) + at) = make_float4(v[0], v[1], v[2], v[3]);
                     else *reinterpret_cast<uint2 *>(static_cast<uint16_t *>(g.c) + at) = make_uint2(pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]));

@@ -415,7 +415,7 @@ __global__ __launch_bounds__(kThreads, 1) void gemm_b128_tile_kernel(GemmB128 g)
             for (int mi = 0; mi < M; ++mi) {
                 Elements<false, H> h;
 #pragma unroll
-                for (int j = 0; j < H; ++j) h.x[j] = EPI == kEpiSilu ? silu(acc[mi][0][j & 15]) * acc[mi][1][j & 15] : relu(acc[mi][j >> 4][j & 15]);
+                for (int j = 0; j < H; ++j) h.x[j] = EPI == kEpiSilu ? silu<DEEP>(acc[mi][0][j & 15]) * acc[mi][1][j & 15] : relu(acc[mi][j >> 4][j & 15]);
                 // in place: the sums are not needed any more
 #pragma unroll
                 for (int j = 0; j < H; ++j) acc[mi][j >> 4][j & 15] = h.x[j];
