@@ -4,6 +4,9 @@
 // blocks of 32 rows and 2 of 32 weight rows (the weights are the first operand, so that a lane's sums are 16 neighbouring columns of one
 // row).  A tile costs what its rows cost: its 32-row blocks are dealt to the two rows of waves in turn and the K loop exists once per block count.
 //
+// Measured: 8192^3 fast 440 to 460 us (2.4 to 2.5 PFLOP/s, matrix cores 63 % busy at 1.85 GHz; a library product of e4m3 numbers 420), precise 877; 24 experts of 5003 rows in all,
+// 1200 -> 1640, 29 us in one round of tiles (66 MB: 13 us); 65536 rows, 128 -> 8192 311 us (3.5 TB/s, nearly all written).
+//
 // Fast (bf16 results): v_mfma_scale_f32_32x32x64_f8f6f4, which takes the scales as exponents.  A K tile of 128 bytes goes to LDS in two halves
 // of 64; five half slots of 32 KB make a ring that is filled by direct-to-LDS loads.  Step u (64 k) multiplies the fragments of slot u mod 5, which were
 // read into registers during step u - 1:

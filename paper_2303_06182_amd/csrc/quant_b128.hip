@@ -4,7 +4,8 @@
 // nearest even.  A power of two, so the division is exact: each element is rounded once, by half a step of e4m3 (2^-4 of it; below
 // 2^-6 s by 2^-10 s).  An element that is not finite becomes NaN and moves no scale.
 //
-// Bound by HBM: elements are read once, and wait in registers for their block's maximum.  16 lanes hold a row's 128 elements, 8 each.
+// Bound by HBM: elements are read once, and wait in registers for their block's maximum.  16 lanes hold a row's 128 elements, 8 each: 16 bytes of bf16
+// a lane and load, whole lines a row.  65536 x 2000 by rows 71 us, 16 x 8192 x 2048 by blocks 143 us (bf16; 5.5 TB/s read and written, a large copy 5.0); 64 x 2048 4 us, a launch.
 #include "b128_dev.h"
 
 namespace moe355 {
