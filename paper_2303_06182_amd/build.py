@@ -33,8 +33,9 @@ def _hipcc() -> str:
 
 # The MFMA GEMM kernels sit at the register limit (256 accumulators + staging registers): a harmless
 # looking edit can tip one of them into scratch spills and cost 10-20 % with no other symptom, so the
-# compiler's per-kernel resource report is read and a spill there fails the build.
-NO_SPILL_SOURCES = {"gemm_bf16.hip", "gemm_stream.hip", "gemm_ring.hip"}
+# compiler's per-kernel resource report is read and a spill there fails the build.  In gemm_b128_tile.hip it would
+# cost more than time: a spilled accumulator is read without the wait that its inline MFMA needs.
+NO_SPILL_SOURCES = {"gemm_bf16.hip", "gemm_stream.hip", "gemm_ring.hip", "gemm_b128_tile.hip"}
 
 
 def spilled_kernels(report: str):

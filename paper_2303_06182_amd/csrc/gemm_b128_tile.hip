@@ -410,7 +410,7 @@ __global__ __launch_bounds__(kThreads, 1) void gemm_b128_tile_kernel(GemmB128 g)
         } else {
             // h, its largest element over the block's 128 columns (16 or 32 a lane, two lanes, and 4 or 2 waves), and its bytes
             constexpr int H = EPI == kEpiSilu ? 16 : 32;
-            uint32_t *const most = reinterpret_cast<uint32_t *>(smem + SLOTS * SLOT);  // [4][256]
+            uint32_t *const most = reinterpret_cast<uint32_t *>(smem + opaque(SLOTS * SLOT));  // [4][256]; addresses made here, not held across the K loop
             const int F = g.Nh, hidden_cols = (int)b128_scale_cols(F);
             const int first = ti.n0 + (EPI == kEpiSilu ? wn * 32 : wn * 64) + kg * 16;
             uint8_t *const hq = static_cast<uint8_t *>(g.c);
