@@ -55,7 +55,7 @@ __global__ __launch_bounds__(kThreads) void quantize_blocks_kernel(const void *x
 {
     __shared__ uint32_t of_wave[kThreads / 64];
     const int part = threadIdx.x & 15, r0 = threadIdx.x >> 4;
-    const int row_blocks = ceil_div(rows, kBlock);
+    const int row_blocks = (rows - 1) / kBlock + 1;
     const int64_t items = matrices * row_blocks * blocks;
     for (int64_t item = blockIdx.x; item < items; item += gridDim.x) {
         const int64_t rb = item / blocks, m = rb / row_blocks;
@@ -103,7 +103,7 @@ int launch_quantize_b128(const void *x, int dtype, int64_t stride, int64_t matri
         else hipLaunchKernelGGL(quantize_rows_kernel<false>, grid, dim3(kThreads), 0, s, x, stride, all, cols, blocks, q, scale);
         MOE_LAUNCH_CHECK("quantize_rows_kernel");
     } else {
-        const dim3 grid(grid_for(matrices * ceil_div(rows, kBlock) * blocks, 1 << 20));
+        const dim3 grid(grid_for(matrices * ((rows - 1) / kBlock + 1) * blocks, 1 << 20));
         if (bf16) hipLaunchKernelGGL(quantize_blocks_kernel<true>, grid, dim3(kThreads), 0, s, x, stride, matrices, rows, cols, blocks, q, scale);
         else hipLaunchKernelGGL(quantize_blocks_kernel<false>, grid, dim3(kThreads), 0, s, x, stride, matrices, rows, cols, blocks, q, scale);
         MOE_LAUNCH_CHECK("quantize_blocks_kernel");
