@@ -461,9 +461,10 @@ class MoeLayer:
     def moe_expert_ffn_b128(self, x, offsets, w1_q, w2_q, w1_scale, w2_scale, activation: str = "silu", src_tok=None, yp=None):
         """x [x_rows, D]; w1_q [E, 2, F, D] (silu: gate, up) or [E, F, D] (relu), w2_q [E, D, F] and their scales from moe_quantize_b128 ->
         yp, a row for each of src_tok (None: of x)."""
-        act = self._b128_weights(w1_q, w2_q, w1_scale, w2_scale, activation)
         x_rows = x.shape[0]
         n_rows = x_rows if src_tok is None else src_tok.shape[0]
+        _fit_32_bits(x_rows, n_rows)
+        act = self._b128_weights(w1_q, w2_q, w1_scale, w2_scale, activation)
         if yp is None:
             yp = self._new((n_rows, self.D), self.torch_dtype)
         else:
@@ -479,9 +480,10 @@ class MoeLayer:
                                n_groups: int = 1, groups_kept: int = 1, group_top: int = 2, renormalize: bool = True, scale: float = 1.0,
                                gate_bias=None, y=None, routing_out=None):
         """The layer with experts chosen as moe_select_experts does, and moe_expert_ffn_b128."""
+        T = x.shape[0]
+        _fit_32_bits(T)
         act = self._b128_weights(w1_q, w2_q, w1_scale, w2_scale, activation)
         cfg = _select_config(self.E, self.k, score, n_groups, groups_kept, group_top, renormalize, scale)
-        T = x.shape[0]
         if y is None:
             y = self._new((T, self.D), self.torch_dtype)
         else:
@@ -811,7 +813,14 @@ def _current_gpu(t: torch.Tensor, name: str) -> int:
     return index
 
 
+def _fit_32_bits(*sizes: int) -> None:
+    """The library takes sizes in 32 bits; ctypes would pass the low ones of a larger one on."""
+    if max(sizes) > 0x7fffffff:
+        raise ValueError("sizes must fit 32 bits, not %d" % max(sizes))
+
+
 def _select_config(E: int, k: int, score: str, n_groups: int, groups_kept: int, group_top: int, renormalize: bool, scale: float) -> MoeSelectConfig:
+    _fit_32_bits(*map(abs, (E, k, n_groups, groups_kept, group_top, int(renormalize))))
     return MoeSelectConfig(E, k, _choice("score", score, {"softmax": MOE_SCORE_SOFTMAX, "sigmoid": MOE_SCORE_SIGMOID}), n_groups, groups_kept, group_top,
                            int(renormalize), scale)
 
@@ -822,10 +831,11 @@ def moe_select_experts(logits, k: int, bias=None, score: str = "sigmoid", n_grou
     if logits.dim() != 2 or logits.dtype not in (torch.float32, torch.bfloat16) or (logits.shape[1] > 1 and logits.stride(1) != 1):
         raise ValueError("logits must be [T, E] of float32 or bfloat16 with dense rows")
     T, E = logits.shape
+    _fit_32_bits(T)
+    cfg = _select_config(E, k, score, n_groups, groups_kept, group_top, renormalize, scale)
     index = _current_gpu(logits, "logits")
     if bias is not None and (tuple(bias.shape) != (E,) or bias.dtype != torch.float32 or bias.get_device() != index):
         raise ValueError("bias must be [%d] of float32 on %s" % (E, logits.device))
-    cfg = _select_config(E, k, score, n_groups, groups_kept, group_top, renormalize, scale)
     new = lambda dtype: torch.empty((T, max(k, 0)), dtype=dtype, device=logits.device)  # noqa: E731
     topk_idx = new(torch.int32) if topk_idx is None else _output(topk_idx, (T, k), torch.int32, index, "topk_idx")
     topk_w = new(torch.float32) if topk_w is None else _output(topk_w, (T, k), torch.float32, index, "topk_w")
@@ -856,11 +866,12 @@ def moe_quantize_b128(x, block_rows: int = 1, q=None, scale=None):
     bytes [..., rows or blocks of 128 rows, b128_scale_cols(cols)])."""
     if x.dim() < 2 or x.dtype not in (torch.float32, torch.bfloat16) or (x.shape[-1] > 1 and x.stride(-1) != 1):
         raise ValueError("x must be [..., rows, cols] of float32 or bfloat16 with dense rows")
-    index = _current_gpu(x, "x")
     lead, (rows, cols) = tuple(x.shape[:-2]), x.shape[-2:]
     matrices = 1
     for n in lead:
         matrices *= n
+    _fit_32_bits(matrices, rows, cols)
+    index = _current_gpu(x, "x")
     # all rows, of all matrices, at one stride
     outer = [(n, s) for n, s in zip(x.shape[:-1], x.stride()[:-1]) if n > 1] if x.numel() else []
     stride = outer[-1][1] if outer else cols
@@ -884,12 +895,13 @@ def moe_gemm_b128(a_q, a_scale, w_q, w_scale, offsets=None, a_rows=None, out_dty
     (None: all, in order); offsets [E + 1] int32: where every expert's rows begin (None: one expert)."""
     if a_q.dim() != 2 or w_q.dim() not in (2, 3):
         raise ValueError("a_q must be [rows, K], w_q [E, N, K]")
-    index = _current_gpu(a_q, "a_q")
     (count, K), N = a_q.shape, w_q.shape[-2]
     E = w_q.shape[0] if w_q.dim() == 3 else 1
+    rows = count if a_rows is None else a_rows.shape[0]
+    _fit_32_bits(count, rows, E, N, K)
+    index = _current_gpu(a_q, "a_q")
     _b128_operand(a_q, a_scale, (count, K), (), 1, index, "a")
     _b128_operand(w_q, w_scale, (*w_q.shape[:-1], K), tuple(w_q.shape[:-2]), 128, index, "w")
-    rows = count if a_rows is None else a_rows.shape[0]
     for name, t, shape in (("a_rows", a_rows, (rows,)), ("offsets", offsets, (E + 1,))):
         if t is not None and (tuple(t.shape) != shape or t.dtype != torch.int32 or t.get_device() != index):
             raise ValueError("%s must be %s of int32 on cuda:%d" % (name, list(shape), index))
