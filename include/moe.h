@@ -539,7 +539,7 @@ int64_t moe_b128_scale_cols(int32_t cols);
 
 /* Quantises x [matrices, rows, cols] (dtype F32 or BF16, row_stride elements from each row to the next, a multiple of 16 bytes) in blocks of block_rows
  * (1 or 128) rows and 128 columns: scale = the smallest power of two, at least 2^-126, that the largest finite |x| of the block does
- * not exceed 448 times (1 for a block of zeros), q = e4m3(x / scale), to nearest even; elements that are not finite become NaN.
+ * not exceed 448 times (1 for a block of zeros), q = e4m3(x / scale), to nearest even; elements that are not finite become NaN, and |x| >= 248 * 2^120 becomes 2^128.
  * q_out [matrices, rows, cols] bytes, scale_out [matrices, rows or ceil(rows / 128), moe_b128_scale_cols(cols)] bytes. */
 int moe_quantize_b128(const void *x, int32_t dtype, int64_t row_stride, int32_t matrices, int32_t rows, int32_t cols, int32_t block_rows,
                       void *q_out, void *scale_out, void *stream);
@@ -553,7 +553,8 @@ int moe_quantize_b128(const void *x, int32_t dtype, int64_t row_stride, int32_t 
  * Sums are formed in fp32.  With c_dtype BF16 the matrix cores' 8-bit instruction forms them, which aligns the products of 8 neighbouring k to
  * the largest of them and drops what is less than about 2^-14 of that; it is off by 1.4e-5 of the results' standard deviation on
  * normally distributed operands (their rounding to bf16: 1.7e-3).  With F32 nothing is dropped, at half the rate.  A scaled element
- * below 2^-126 may count as 0. */
+ * (its number times 2^(byte - 127)) below 2^-126 may count as 0.  One of 2^128 or more is infinite with F32, however small the numbers that it is multiplied by, and NaN times
+ * a zero; with BF16 the scales are exponents and it counts as it is. */
 int moe_gemm_b128(const void *a_q, const void *a_scale, int32_t a_count, const int32_t *a_rows, const void *w_q, const void *w_scale,
                   const int32_t *offsets, int32_t E, int32_t n_rows, int32_t N, int32_t K, void *c, int32_t c_dtype, void *stream);
 
@@ -565,7 +566,8 @@ int moe_gemm_b128(const void *a_q, const void *a_scale, int32_t a_count, const i
  *   MOE_ACT_SILU:  h = silu(g) * u, g = W1[e][0] x[src_tok[r]], u = W1[e][1] x[src_tok[r]],  w1_q [E, 2, F, D], scales [E, 2, ceil(F / 128), ..]
  *   yp[r] = W2[e] h',  h' = h quantised by rows,                                 w2_q [E, D, F]
  * src_tok [n_rows] int32 (as moe_route_counts writes it; clamped to [0, x_rows)) or NULL: row r of x.  Offsets as in moe_gemm_b128.  silu(g) = g / (1 +
- * exp(-g)); h in fp32, from the sums of the first product, and rounded to e4m3 only.  yp [n_rows, D] elem.  The handle's D and F are multiples of 16, up to
+ * exp(-g)), which may count as 0 where exp(-g) is 2^126 or more; h in fp32, from the sums of the first product, and rounded to e4m3 only.  Scaled
+ * elements of 2^128 or more, of x, h or weights, may be infinite, as in moe_gemm_b128 with F32.  yp [n_rows, D] elem.  The handle's D and F are multiples of 16, up to
  * 2^23; n_rows at most k * T_max, and x_rows with src_tok at most T_max, without it k * T_max.  The handle's device has to be the current one.
  * Workspace: moe_b128_workspace_bytes(). */
 int64_t moe_b128_workspace_bytes(const moe_handle_t *h);
