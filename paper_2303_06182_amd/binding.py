@@ -244,6 +244,14 @@ def _stream_on(index: int) -> int:
     return torch._C._cuda_getCurrentRawStream(index)
 
 
+def _gpu(device) -> torch.device:
+    """The GPU that a handle is for, by its number; without one the current GPU."""
+    device = torch.device(device)
+    if device.type != "cuda":
+        raise ValueError("device must be a GPU, not %s" % device)
+    return device if device.index is not None else torch.device("cuda", torch.cuda.current_device())
+
+
 def _output(t: torch.Tensor, shape: tuple, dtype: torch.dtype, index: int, name: str) -> torch.Tensor:
     """An output that the caller has allocated, as it has to be."""
     if tuple(t.shape) != shape or t.dtype != dtype or t.get_device() != index or not t.is_contiguous():
@@ -271,9 +279,7 @@ class MoeLayer:
         self.T_max, self.D, self.F, self.E, self.k = T_max, D, F, E, k
         self.dtype = dtype
         self.torch_dtype = torch.bfloat16 if dtype == "bf16" else torch.float32
-        self.device = torch.device(device)
-        if self.device.index is None:
-            self.device = torch.device("cuda", torch.cuda.current_device())
+        self.device = _gpu(device)
         h = ctypes.c_void_p()
         with torch.cuda.device(self.device):
             _check(self.lib.moe_create(ctypes.byref(self.cfg), ctypes.byref(h)))
@@ -680,9 +686,7 @@ class PagedAttention:
                                  MOE_DTYPE_BF16 if dtype == "bf16" else MOE_DTYPE_F32, rot_dim, int(interleaved))
         self.cache_shape = (num_pages, n_kv_heads, page_size, head_dim)
         self.torch_dtype = torch.bfloat16 if dtype == "bf16" else torch.float32
-        self.device = torch.device(device)
-        if self.device.index is None:
-            self.device = torch.device("cuda", torch.cuda.current_device())
+        self.device = _gpu(device)
         self.index = self.device.index
         h = ctypes.c_void_p()
         with torch.cuda.device(self.device):
