@@ -569,7 +569,7 @@ int moe_gemm_b128(const void *a_q, const void *a_scale, int32_t a_count, const i
  * exp(-g)), which may count as 0 where exp(-g) is 2^126 or more; h in fp32, from the sums of the first product, and rounded to e4m3 only.  Scaled
  * elements of 2^128 or more, of x, h or weights, may be infinite, as in moe_gemm_b128 with F32.  yp [n_rows, D] elem.  The handle's D and F are multiples of 16, up to
  * 2^23; n_rows at most k * T_max, and x_rows with src_tok at most T_max, without it k * T_max.  The handle's device has to be the current one.
- * Workspace: moe_b128_workspace_bytes(). */
+ * Workspace: moe_b128_workspace_bytes(), which is an error code for other D and F. */
 int64_t moe_b128_workspace_bytes(const moe_handle_t *h);
 int moe_expert_ffn_b128(moe_handle_t *h, const void *x, int32_t x_rows, const int32_t *src_tok, const int32_t *offsets, const void *w1_q,
                         const void *w2_q, const void *w1_scale, const void *w2_scale, int32_t activation, int32_t n_rows, void *yp,

@@ -448,7 +448,10 @@ class MoeLayer:
     def b128_workspace(self) -> torch.Tensor:
         """The workspace of the two calls below, allocated on first use (before a capture, so that no graph owns it)."""
         if self.workspace_b128 is None:
-            self.workspace_b128 = torch.empty(int(self.lib.moe_b128_workspace_bytes(self.h)), dtype=torch.uint8, device=self.device)
+            n = int(self.lib.moe_b128_workspace_bytes(self.h))
+            if n < 0:
+                _check(n)
+            self.workspace_b128 = torch.empty(n, dtype=torch.uint8, device=self.device)
         return self.workspace_b128
 
     def _b128_weights(self, w1_q, w2_q, w1_scale, w2_scale, activation: str) -> int:

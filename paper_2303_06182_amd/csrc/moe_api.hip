@@ -1115,13 +1115,20 @@ static B128Layout b128_layout(const moe_config_t &c)
     return L;
 }
 
-static int check_b128(const moe_handle_t *h, int32_t activation, const void *workspace, int64_t workspace_bytes)
+static int check_b128_sizes(const moe_config_t &c)
 {
-    const moe_config_t &c = h->cfg;
     if (c.D % 16 != 0 || c.F % 16 != 0 || c.D > 1 << 23 || c.F > 1 << 23) {
         set_error("experts in blocks of 128 need D and F that are multiples of 16, up to 2^23 (D = %d, F = %d)", c.D, c.F);
         return MOE_ERR_UNSUPPORTED;
     }
+    return MOE_OK;
+}
+
+static int check_b128(const moe_handle_t *h, int32_t activation, const void *workspace, int64_t workspace_bytes)
+{
+    const moe_config_t &c = h->cfg;
+    const int rc = check_b128_sizes(c);
+    if (rc != MOE_OK) return rc;
     if (activation != MOE_ACT_RELU && activation != MOE_ACT_SILU) {
         set_error("unsupported activation %d", activation);
         return MOE_ERR_UNSUPPORTED;
@@ -1210,7 +1217,8 @@ int64_t moe_b128_workspace_bytes(const moe_handle_t *h)
         set_error("handle is NULL");
         return MOE_ERR_INVALID_ARG;
     }
-    return b128_layout(h->cfg).total;
+    const int rc = check_b128_sizes(h->cfg);
+    return rc != MOE_OK ? rc : b128_layout(h->cfg).total;
 }
 
 int moe_expert_ffn_b128(moe_handle_t *h, const void *x, int32_t x_rows, const int32_t *src_tok, const int32_t *offsets, const void *w1_q,
