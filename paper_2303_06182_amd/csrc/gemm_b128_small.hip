@@ -165,7 +165,8 @@ int launch_gemm_b128_small(const GemmB128 &g, hipStream_t s)
     return g.precise ? launch_shape<true>(g, best_shape(g), s) : launch_shape<false>(g, best_shape(g), s);
 }
 
-// Which of the two takes less, this or tiles: rounds of tiles, of the height that suits best.  Measured, small / tiles, us, bf16 results: one expert 2048 -> 8192,
+// Which of the two takes less, this or tiles: rounds of tiles, of the height that suits best, each as long as nine K tiles more than it has (six for a tile's beginning and
+// end, as in gemm_b128_tile.hip, and three for the rest of a launch).  Measured, small / tiles, us, bf16 results: one expert 2048 -> 8192,
 // 16 rows 6.2 / 19, 64 rows 11 / 20, 128 rows 20 / 21.5, 192 rows 29 / 21; 8192 -> 2048, 16 rows 11.8 / 56, 64 rows 16 / 58, 256 rows 33 / 62, 512 rows 63 / 62; 8 experts of
 // 16 rows, 2048 -> 8192 38 / 28, 8192 -> 2048 44 / 70, of 48 rows 58 / 76 (tiles are taken), of 64 rows 91 / 77; 64 experts of 16 rows, 512 -> 4096 49 / 31.
 // fp32 results: 128 rows, 2048 -> 8192 21 / 28; 512 rows, 8192 -> 2048 65 / 82; 8 experts of 64 rows, 8192 -> 2048 92 / 107.

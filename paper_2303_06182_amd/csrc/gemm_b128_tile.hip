@@ -141,8 +141,9 @@ __global__ __launch_bounds__(kThreads, 1) void gemm_b128_tile_kernel(GemmB128 g)
         w_excl = (incl - w_cuts) * n_tiles;
         w_total = __builtin_amdgcn_readlane(incl, 63) * n_tiles;
     };
-    // The height at which the rounds of all blocks take least: a round costs a K loop, whose K tiles take about so many units by a tile's height,
-    // and as much as six K tiles of the least for its beginning and end.
+    // The height at which the rounds of all blocks take least: a round costs a K loop, whose K tiles take about so many units by a tile's height, and as much as six
+    // more of its K tiles for its beginning and end.  Only ratios count here, so what every height has alike is left out: the launch, and the work before the first tile
+    // (the choice between these tiles and gemm_b128_small.hip counts them, as three more).
     if (g.n_rows > 64) {
         int tiles[4] = {0, 0, 0, 0};
         for (w_base = 0; w_base < g.E; w_base += 64) {

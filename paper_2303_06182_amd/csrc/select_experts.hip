@@ -12,9 +12,11 @@
 // What the 32-bit keys may have decided wrongly -- the last group that stays against the first that does not, the k-th key against what fell
 // off the list -- is checked with their error bound; a token that fails is done again by the whole wave as above.  Of normally distributed
 // logits fewer than one in a thousand fail; of logits with many equal ones at the border, all may.
-// Bound by issuing vector instructions (the lists, mostly), not by memory.  One wave a token / four lanes a token, us: 65536 x 128 experts, 8 groups, k = 6
-// 167 / 39 (fp32, sigmoid), 168 / 55 (softmax), 201 / 64 (256 experts), 399 / 266 (512 experts, k = 8), 57 / 20 (no groups, k = 2); 4096 tokens
-// 16 / 15, 16 / 20, 18 / 23, 34 / 38, 9.4 / 9.8; 1024 tokens 10 / 15.  One lane a token, 64 a wave: 55 for the first, as it leaves a wave a SIMD.
+// Bound by issuing vector instructions (the lists, mostly), not by memory, and by how few waves LDS leaves a CU where there are many experts (16 rows of logits a wave: 16 waves
+// at 128 experts, 8 at 256, 4 at 512, 2 at 1024).  One wave a token / four lanes a token, us, launches of a graph one after the other: 65536 x 128 experts, 8 groups, k = 6
+// 156 / 32 (fp32, sigmoid), 170 / 44 (softmax), 203 / 63 (256 experts), 399 / 225 (512 experts, k = 8), 955 / 711 (1024 experts, k = 8), 58 / 17 (128 experts, no groups, k = 2);
+// 8192 tokens 24 / 19, 26 / 27, 30 / 24, 56 / 63, 119 / 115, 10.4 / 9.0; 6144 tokens 20 / 20, 21 / 23, 24 / 26, 43 / 61, 89 / 103, 8.6 / 9.0; 4096 tokens 15 / 17, 16 / 25, 17 / 24,
+// 33 / 62, 61 / 96, 6.8 / 7.8.  One lane a token, 64 a wave: 55 for the first, as it leaves a wave a SIMD.
 #include <mutex>
 #include <type_traits>
 
@@ -25,7 +27,7 @@ namespace moe355 {
 namespace {
 
 constexpr int kThreads = 256, kWaves = kThreads / 64;
-constexpr int kManyFrom = 6144;  // tokens, see above
+constexpr int kManyFrom = 6144;  // tokens: about where either takes as long with up to 256 experts; with more that is at 8192 and later
 constexpr int kManyTokens = 16;  // of a wave of select_many_kernel
 // words from row to row there: four lanes of a token read four neighbours, and the rows of 16 tokens lie four banks apart
 __host__ __device__ constexpr int many_row(int E) { return (E + 59) / 64 * 64 + 4; }
