@@ -284,3 +284,47 @@ def test_ffn_streams_what_tiles_cannot_address(activation, dtype):
     keep, at, values = m.some(offsets, 120)
     check_streamed(y[torch.tensor(keep, device=DEV)], x, src[keep], values, at, activation, dtype, D)
     assert torch.equal(m(x, offsets, src), y)
+
+
+@pytest.mark.parametrize("activation", ["relu", "silu"])
+@pytest.mark.parametrize("dtype", [BF16, F32])
+def test_layer_prefill(activation, dtype):
+    """A whole batch: the selection of many tokens, more than 64 experts, tiles, the weighted sum; a token that is not finite spoils itself alone; captured, the same."""
+    T, E, k, D, F = 7001, 96, 4, 272, 400
+    m = Experts(E, D, F, activation, dtype, T, seed=5)
+    layer = binding.MoeLayer(T, D, F, E, k, "bf16" if dtype == BF16 else "f32", alloc_workspace=False)
+    x = m.rows(T)
+    wg = (torch.randn((E, D), device=DEV, generator=m.g) * 40).to(dtype)
+    bias = torch.randn(E, device=DEV, generator=m.g) * 0.1
+    kw = dict(activation=activation, select_bias=bias, n_groups=8, groups_kept=3, scale=2.0)
+    run = lambda x, **more: layer.moe_layer_forward_b128(x, wg, m.w1, m.w2, m.s1, m.s2, **kw, **more)  # noqa: E731
+    r = layer.empty_routing(T)
+    names, y = kernels(lambda: run(x, routing_out=r))
+    assert any("select_many_kernel" in n for n in names) and any("gemm_b128_tile_kernel<true" in n for n in names), names
+    idx, w = b128.select(host(r["logits"]), k, bias=host(bias), n_groups=8, groups_kept=3, scale=2.0)
+    assert np.array_equal(r["topk_idx"].cpu().numpy(), idx)
+    order = np.argsort(idx.ravel(), kind="stable")
+    offsets = ends(np.bincount(idx.ravel(), minlength=E))
+    assert np.array_equal(r["src_tok"].cpu().numpy(), order // k) and r["offsets"].cpu().tolist() == offsets
+    yp = layer.moe_expert_ffn_b128(x, r["offsets"], m.w1, m.w2, m.s1, m.s2, activation=activation, src_tok=r["src_tok"])
+    keep, at, values = m.some(offsets, 200)
+    check_ffn(yp[torch.tensor(keep, device=DEV)], x, (order // k)[keep], values, at, activation, dtype, max(D, F))
+    parts = host(yp)[r["dst_row"].cpu().numpy()].reshape(T, k, D)
+    total, size = (parts * w[:, :, None]).sum(1), np.abs(parts * w[:, :, None]).sum(1)
+    half = 2.0 ** -8 if dtype == BF16 else 2.0 ** -24
+    assert (np.abs(host(y) - total) <= half * np.abs(total) + 2 * k * 2.0 ** -24 * size + 2.0 ** -120).all()
+    out, x2 = torch.empty_like(y), x.clone()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        run(x2, y=out)
+    x2[77, 5], x2[T - 1, 0] = math.nan, math.inf
+    others = torch.ones(T, dtype=torch.bool, device=DEV)
+    others[[77, T - 1]] = False
+    for spoiled in (True, False, True):
+        if not spoiled:
+            x2.copy_(x)
+        else:
+            x2[77, 5], x2[T - 1, 0] = math.nan, math.inf
+        graph.replay()
+        assert torch.equal(out[others], y[others])
+        assert out[~others].isnan().any(1).all() if spoiled else torch.equal(out, y)
